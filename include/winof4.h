@@ -44,7 +44,7 @@ extern "C" {
 typedef enum wino_status {
     WINO_OK = 0,
     WINO_EINVAL = -1,        /* null pointer, negative size, value out of range   */
-    WINO_EUNSUPPORTED = -2,  /* a size beyond the library's limits                */
+    WINO_EUNSUPPORTED = -2,  /* a size or alignment beyond the library's limits  */
     WINO_ERANGE = -3,        /* plan tables that no integer epilogue can hold     */
     WINO_ENOMEM = -4,        /* device or host allocation failed                  */
     WINO_EWORKSPACE = -5,    /* workspace pointer null or smaller than required   */
@@ -497,6 +497,158 @@ wino_status direct_conv_int8(const int8_t* x, const int8_t* w_ohwi, const int32_
 wino_status wino_f4_conv_float(const int8_t* x, const float* w_oihw, float* y, int32_t n,
                                int32_t cin, int32_t cout, int32_t h, int32_t w,
                                wino_layout layout, hipStream_t stream);
+
+/*
+ * ---- Decoder operators in 4 bits ------------------------------------------
+ *
+ * What a token decoder beside the convolutions runs: products of a few rows
+ * with a weight matrix, attention over whole prompts, and a cache of keys and
+ * values with the attention that reads it.  Weights and cache are held in 4
+ * bits with one power-of-two scale for 32 neighbours (the library's
+ * power-of-two rule, Sec. III-B, on groups instead of taps):
+ *   - scale byte s stands for 2^(s - 127); 255 stands for not-a-number, and a
+ *     group that holds a value that is not finite gets it (the whole group
+ *     then reads as NaN);
+ *   - e = s - 127 is the smallest exponent with max|x| <= 6 * 2^e (0 for 32
+ *     zeros; not below -127);
+ *   - a code is a sign (bit 3) over the magnitudes 0, 1/2, 1, 3/2, 2, 3, 4, 6
+ *     (bits 2..0); x becomes the code nearest to x / 2^e, ties to the even
+ *     code.  This rounding is the format's own and the one place where the
+ *     library does not round half up;
+ *   - two codes a byte, the lower index in the low half.
+ * Activations are bf16 or fp16 (wino_float_type, one type for a call); every
+ * sum, maximum and softmax statistic is held in fp32 and each result is
+ * rounded to the 16-bit type once.
+ *
+ * Tensors are row-major device memory; a stride is the distance between two
+ * rows (tokens) in elements, and a row itself is dense.  Base addresses of
+ * 16-bit tensors and of codes must be multiples of 16 bytes and strides
+ * multiples of 8 elements (WINO_EUNSUPPORTED otherwise).  Outputs must not
+ * overlap inputs.  Everything is asynchronous on `stream`, allocates nothing,
+ * keeps nothing, and can be captured into a graph.  Lengths, positions, slots
+ * and page numbers are device data that the host does not see: the kernels
+ * check them, and what lies outside its range is left out as each call says.
+ */
+typedef enum wino_float_type { WINO_BF16 = 0, WINO_FP16 = 1 } wino_float_type;
+
+/*
+ * w4_quantize_weights -- fp32 weights to the 4-bit format, exact host
+ * arithmetic (offline).  w: host [n][k]; codes: host uint8 [n][k/2]; scales:
+ * host uint8 [n][k/32].  k a multiple of 32; every weight finite
+ * (WINO_EINVAL otherwise).
+ */
+wino_status w4_quantize_weights(const float* w, int32_t n, int32_t k, uint8_t* codes, uint8_t* scales);
+
+/*
+ * w4_matvec -- y = x W^T + bias for a few rows x and a weight matrix W in the
+ * 4-bit format.
+ *   x        [m][k], row stride x_stride >= k;  y: [m][n], row stride
+ *            y_stride >= n (any alignment).
+ *   codes    uint8 [n][k/2], scales uint8 [n][k/32], dense.
+ *   bias     [n] in the type of x, or NULL.
+ *   m <= 65535 (made for m up to 64: more rows read the weights again for
+ *   every 64), n <= 2^24, k a multiple of 32 up to 2^20.
+ *   workspace  w4_matvec_workspace_bytes(m, n, k) bytes or more, 16-byte
+ *            aligned, scratch; NULL or a smaller one gives the same result
+ *            up to the order of the sum over k, more slowly.
+ */
+size_t w4_matvec_workspace_bytes(int32_t m, int32_t n, int32_t k);
+wino_status w4_matvec(const void* x, int64_t x_stride, const uint8_t* codes, const uint8_t* scales,
+                      const void* bias, void* y, int64_t y_stride, int32_t m, int32_t n, int32_t k,
+                      wino_float_type type, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * The paged cache: `pages` pages of page_size tokens (a multiple of 16), each
+ *   k_codes, v_codes    uint8 [pages][kv_heads][page_size][head_dim / 2]
+ *   k_scales, v_scales  uint8 [pages][kv_heads][page_size][head_dim / 32]
+ * in device memory of the caller.  Slot p * page_size + o is token o of page p.
+ */
+typedef struct kv4_cache {
+    uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    int64_t pages;
+    int32_t kv_heads, page_size, head_dim;
+} kv4_cache;
+
+/* Which dimensions a rotation pairs: (j, j + r/2) or (2j, 2j + 1). */
+typedef enum wino_rotary { WINO_ROTARY_HALVES = 0, WINO_ROTARY_PAIRS = 1 } wino_rotary;
+
+/* What k_out and v_out receive: the turned keys and the values as they came,
+ * or what the cache now holds for them. */
+typedef enum kv4_values { KV4_ROTATED = 0, KV4_CACHED = 1 } kv4_values;
+
+/*
+ * kv4_append -- turns new queries and keys by their positions, and puts keys
+ * and values into the cache.
+ *   q           [tokens][heads][head_dim], stride q_stride, or NULL with heads 0
+ *   k, v        [tokens][kv_heads][head_dim], strides k_stride, v_stride
+ *   cos_sin     fp32 [table_rows][rot], dense: rot / 2 cosines, then rot / 2
+ *               sines of a position; the first rot dimensions of a head turn
+ *               (rot a multiple of 16, at most head_dim; 0: none)
+ *   positions   int32 [tokens], rows of cos_sin.  A token whose position is
+ *               outside the table is not cached, and its outputs are NaN.
+ *   slots       int64 [tokens].  A slot below 0 or past the cache: the token is
+ *               not cached (padding); its outputs are written all the same.
+ *               Two tokens of a call must not share a slot.
+ *   q_out       [tokens][heads][head_dim], dense (NULL with heads 0)
+ *   k_out, v_out  [tokens][kv_heads][head_dim], dense, or NULL; see kv4_values.
+ *               A prompt whose attention reads KV4_CACHED values sees exactly
+ *               what later tokens will see.
+ * Rotation: (u, w) -> (u c - w s, w c + u s), every product and sum rounded
+ * once to fp32; keys and values are quantized from there, so equal inputs
+ * always give equal codes.  head_dim a multiple of 32, at most 256.
+ */
+wino_status kv4_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                       int64_t v_stride, int32_t tokens, int32_t heads, const float* cos_sin, int32_t table_rows,
+                       int32_t rot, const int32_t* positions, const int64_t* slots, const kv4_cache* cache,
+                       void* q_out, void* k_out, void* v_out, wino_rotary rotary, kv4_values values,
+                       wino_float_type type, hipStream_t stream);
+
+/*
+ * kv4_attention -- attention of the newest q_len tokens of each sequence over
+ * its cached tokens (theirs included), read through a table of pages.
+ *   q            [batch][q_len][heads][head_dim], token stride q_stride
+ *   block_table  int32 [batch][max_pages]: the pages of a sequence in order.
+ *                The tokens of an entry outside [0, pages) are not there.
+ *   lens         int32 [batch]: cached tokens of a sequence, at most
+ *                max_pages * page_size (what is beyond is not read).
+ *   out          [batch][q_len][heads][head_dim], dense.  Query i sees the
+ *                tokens before lens - q_len + 1 + i:
+ *                softmax_t(scale q.k_t) v_t; zeros where it sees none.
+ * heads is a multiple of cache->kv_heads: neighbours share a head of the
+ * cache.  head_dim 64, 96, 128, 192 or 256; scale finite.
+ *   workspace    kv4_attention_workspace_bytes() bytes or more, 16-byte
+ *                aligned, scratch: long sequences are split over it.  NULL or
+ *                a smaller one splits less.
+ */
+size_t kv4_attention_workspace_bytes(int32_t batch, int32_t q_len, int32_t heads, int32_t kv_heads,
+                                     int32_t head_dim, int32_t max_pages, int32_t page_size);
+wino_status kv4_attention(const void* q, int64_t q_stride, const kv4_cache* cache, const int32_t* block_table,
+                          int32_t max_pages, const int32_t* lens, void* out, int32_t batch, int32_t q_len,
+                          int32_t heads, float scale, wino_float_type type, void* workspace,
+                          size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * prompt_attention -- attention of whole prompts, sequences of different
+ * lengths packed one after the other, keys and values in 16 bits.
+ *   q          [total_q][heads][head_dim], stride q_stride
+ *   k, v       [total_k][kv_heads][head_dim], strides k_stride, v_stride
+ *   cu_q, cu_k int32 [seqs + 1] (may be the same): sequence s has the queries
+ *              cu_q[s] .. cu_q[s+1] - 1 and the keys cu_k[s] .. cu_k[s+1] - 1.
+ *              Offsets do not decrease; what lies past total_q or total_k is
+ *              left out.  A row of out that no sequence covers is not written.
+ *   max_q      the longest sequence's queries, a hint for the tile size
+ *   causal     1: the last query sees every key, the one before it one less,
+ *              and so on (a prompt behind a prefix has more keys than
+ *              queries); 0: all keys.
+ *   out        [total_q][heads][head_dim], dense; zeros where a query sees
+ *              no key.
+ * Sizes of heads as for kv4_attention.
+ */
+wino_status prompt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                             int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k, int32_t seqs,
+                             int32_t total_q, int32_t total_k, int32_t max_q, int32_t heads, int32_t kv_heads,
+                             int32_t head_dim, float scale, int32_t causal, void* out, wino_float_type type,
+                             hipStream_t stream);
 
 /* Static description of a status code; never NULL. */
 const char* wino_strerror(wino_status status);

@@ -13,6 +13,7 @@ Modules
   f4        transform matrices of F(4x4,3x3) and F(2x2,3x3) (Sec. II)
   quant     round / clamp / power-of-two exponent rules (Sec. III, Eq. quant)
   direct    direct 3x3 convolution: float64, integer, and brute force
+  decoder   the 4-bit format and the decoder operators in float64
   tapwise   the tap-wise quantized integer Winograd F4 pipeline (Sec. III),
             its offline plan, input/output calibration, and analytic bounds
 """

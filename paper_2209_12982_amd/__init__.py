@@ -22,4 +22,7 @@ from .binding import (  # noqa: F401
     wino_f4_calibrate_input, wino_f4_calibrate_output,
     wino_f4_debug_input_transform, wino_f4_debug_tap_gemm,
     direct_conv_quantize_weights, direct_conv_int8, wino_f4_conv_float, wino_probe_mfma_int8, wino_probe_conv_kernels, wino_strerror,
+    ROTARY_HALVES, ROTARY_PAIRS, KV4_ROTATED, KV4_CACHED,
+    w4_quantize_weights, w4_matvec_workspace_bytes, w4_matvec, kv4_append,
+    kv4_attention_workspace_bytes, kv4_attention, prompt_attention,
 )
