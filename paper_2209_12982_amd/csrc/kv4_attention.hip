@@ -1,104 +1,437 @@
 // Attention over the paged 4-bit cache (mx4.h) for one or a few query tokens
-// of each sequence.
+// of each sequence: o = sum_t softmax_t(scale q.k_t) v_t.
+//
+// The bytes of the cache bound it, so one pass reads each once, for up to 16
+// query rows (the heads that share a cache head, times the query tokens) at a
+// time.  A wave takes 16-token tiles: K codes go from global memory straight to
+// the registers of the matrix cores' first operand (a lane holds a quarter of
+// one token's head: consecutive bytes, one or two scales), two codes an
+// instruction, exact in bf16.  Scores come out transposed (tokens x rows), so
+// a lane keeps one row's statistics and its probabilities are already where
+// the second product wants them; that product's V must be read across tokens,
+// which LDS does: V is written there token by token and read back transposed.
+// The order of tokens inside a product is free, so V takes the order that the
+// scores have.  Each wave has its own part of LDS and its own running maximum
+// and sum; the waves, and the parts of a split sequence, are joined at the end.
+//
+// Precision: queries in fp16 and all probabilities are split into two bf16
+// numbers (16 bits), the matrix cores have time for both; the products are
+// then exact in fp32.
 #include <hip/hip_runtime.h>
+
+#include <algorithm>
 
 #include "mx4.h"
 #include "winof4.h"
+#include "winof4_internal.h"
 
 namespace {
 using namespace mx4;
+using winof4::FastDiv;
+
+constexpr int kWaves = 4;
+constexpr float kNever = -__builtin_inff();
 
 struct DecodeArgs {
     const void* q;
     void* out;
     const uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
     const int32_t *table, *lens;
+    float* part;            // [units * splits][16][dim + 2] partial sums, maxima and sums, or null
     int64_t q_stride, pages;
-    int32_t q_len, heads, kv_heads, dim, page, max_pages;
-    float scale;
+    int32_t q_len, heads, kv_heads, group, page, max_pages;
+    int32_t tiles;          // 16-row tiles of a sequence's rows at one cache head
+    int32_t units;          // batch * kv_heads * tiles
+    int32_t splits, chunk;  // parts of a sequence, tokens in each
+    int32_t room;           // tokens that a table has room for
+    FastDiv by_page;
+    float scale_log2;       // scale * log2(e): probabilities are powers of two
 };
 
-// One wave per query row and head, 64 tokens at a time: a lane scores one
-// token, then the lanes take dimensions.
-template <int TYPE>
-__global__ __launch_bounds__(64) void kv4_attention_kernel(DecodeArgs a) {
-    typedef typename Half<TYPE>::type T;
-    __shared__ float qs[256], ps[64];
-    __shared__ int64_t at_s[64];
-    const int lane = threadIdx.x, h = blockIdx.x % a.heads, kvh = h / (a.heads / a.kv_heads);
-    const int64_t row = blockIdx.x / a.heads;
-    const int b = (int)(row / a.q_len), i = (int)(row % a.q_len);
-    const int64_t room = (int64_t)a.max_pages * a.page;
-    int64_t len = a.lens[b];
-    len = len < 0 ? 0 : (len > room ? room : len);
-    const int64_t end = len - a.q_len + 1 + i;        // tokens that the row sees
-    const T* q = (const T*)a.q + row * a.q_stride + (int64_t)h * a.dim;
-    for (int d = lane; d < a.dim; d += 64) qs[d] = (float)q[d] * a.scale;
-    float top = -__builtin_inff(), sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t t0 = 0; t0 < end; t0 += 64) {
-        const int64_t t = t0 + lane;
-        int64_t pg = t < end ? a.table[(int64_t)b * a.max_pages + t / a.page] : -1;
-        const bool there = pg >= 0 && pg < a.pages;
-        const int64_t at = there ? (pg * a.kv_heads + kvh) * a.page + t % a.page : -1;
-        float z = -__builtin_inff();
-        __syncthreads();
-        if (there) {
-            z = 0.f;
-            for (int g = 0; g < a.dim / kGroup; ++g) {
-                float part = 0.f;
-                for (int d = 0; d < 16; ++d) {
-                    const uint32_t c = a.k_codes[at * (a.dim / 2) + g * 16 + d];
-                    part += code_value(c & 15u) * qs[g * 32 + 2 * d] + code_value(c >> 4) * qs[g * 32 + 2 * d + 1];
-                }
-                z += part * scale_value(a.k_scales[at * (a.dim / kGroup) + g]);
-            }
+__device__ inline int fast_div(int n, FastDiv f) {
+    return f.d == 1 ? n : (int)((uint32_t)(((uint64_t)(uint32_t)n * f.mul) >> 32) >> f.shr);
+}
+
+template <int DIM> struct Shape {
+    static constexpr int kSteps = DIM / 32;                 // products of 32 dimensions
+    static constexpr int kTok = DIM <= 128 ? 64 : 32;       // tokens of a wave's step
+    static constexpr int kTiles = kTok / 16;
+    static constexpr int kRow = DIM * 2 + 32;               // bytes of a token's V in LDS: 8 rows cover all banks once
+    static constexpr int kScales = DIM == 64 || DIM == 128 ? 1 : 2;   // scales in a lane's quarter
+    static constexpr int kStage = 32 * kRow;                // a wave's V in LDS, 32 tokens at a time
+    static constexpr int kJoin = 16 * (DIM + 2) * 4;        // a wave's results in LDS
+    static constexpr int kLds = kWaves * (kStage > kJoin ? kStage : kJoin);
+};
+
+// One step's codes and scales: lane (t, g) has quarter g of token t of each tile.
+template <int DIM> struct Codes {
+    uint32_t w[Shape<DIM>::kTiles][Shape<DIM>::kSteps];
+    uint32_t s[Shape<DIM>::kTiles][Shape<DIM>::kScales];
+};
+
+template <int DIM>
+__device__ inline void load_codes(Codes<DIM>& c, const uint8_t* codes, const uint8_t* scales, const int64_t (&at)[Shape<DIM>::kTiles],
+                                  int lane) {
+    typedef Shape<DIM> S;
+    const int t = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < S::kTiles; ++i) {
+        if (at[i] < 0) {                                    // wave-uniform: no such tokens
+#pragma unroll
+            for (int j = 0; j < S::kSteps; ++j) c.w[i][j] = 0;
+#pragma unroll
+            for (int j = 0; j < S::kScales; ++j) c.s[i][j] = 0;
+            continue;
         }
-        float m = z;
-        for (int s = 32; s; s >>= 1) m = fmaxf(m, __shfl_xor(m, s));
-        m = fmaxf(m, top);
-        const float base = m == -__builtin_inff() ? 0.f : m;
-        const float p = there ? expf(z - base) : 0.f, alpha = expf(top - base);
-        top = m;
-        ps[lane] = p;
-        at_s[lane] = at;
-        float s = p;
-        for (int k = 32; k; k >>= 1) s += __shfl_xor(s, k);
-        sum = sum * alpha + s;
-        __syncthreads();
-        for (int e = 0; e < 4; ++e) {
-            const int d = lane + 64 * e;
-            if (d >= a.dim) break;
-            float acc = o[e] * alpha;
-            for (int k = 0; k < 64; ++k) {
-                if (at_s[k] < 0) continue;
-                const uint32_t c = a.v_codes[at_s[k] * (a.dim / 2) + d / 2] >> (4 * (d & 1));
-                acc += ps[k] * (code_value(c) * scale_value(a.v_scales[at_s[k] * (a.dim / kGroup) + d / kGroup]));
+        const uint8_t* p = codes + (at[i] + t) * (DIM / 2) + g * (DIM / 8);
+        if constexpr (S::kSteps % 4 == 0) {
+#pragma unroll
+            for (int j = 0; j < S::kSteps; j += 4) {
+                const u32x4 x = *(const u32x4*)(p + 4 * j);
+                c.w[i][j] = x[0], c.w[i][j + 1] = x[1], c.w[i][j + 2] = x[2], c.w[i][j + 3] = x[3];
             }
-            o[e] = acc;
+        } else if constexpr (S::kSteps % 2 == 0) {
+#pragma unroll
+            for (int j = 0; j < S::kSteps; j += 2) {
+                const u32x2 x = *(const u32x2*)(p + 4 * j);
+                c.w[i][j] = x[0], c.w[i][j + 1] = x[1];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < S::kSteps; ++j) c.w[i][j] = *(const uint32_t*)(p + 4 * j);
         }
-    }
-    T* out = (T*)a.out + (row * a.heads + h) * a.dim;
-    for (int e = 0; e < 4; ++e) {
-        const int d = lane + 64 * e;
-        if (d < a.dim) out[d] = (T)(sum == 0.f ? 0.f : o[e] / sum);
+        const uint8_t* s = scales + (at[i] + t) * (DIM / 32);
+        const int first = g * (DIM / 4) / 32;
+        c.s[i][0] = s[first];
+        if constexpr (S::kScales == 2) c.s[i][1] = s[first + 1 < DIM / 32 ? first + 1 : first];
     }
 }
 
+// Scale of the eight dimensions j of a lane's quarter.
+template <int DIM> __device__ inline float piece_scale(const uint32_t (&s)[Shape<DIM>::kScales], int j, int g) {
+    if constexpr (Shape<DIM>::kScales == 1) return scale_bits(s[0]);
+    const int first = g * (DIM / 4) / 32, mine = (g * (DIM / 4) + 8 * j) / 32;
+    return scale_bits(mine == first ? s[0] : s[Shape<DIM>::kScales - 1]);
+}
+
+template <int TYPE, int DIM>
+__global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void kv4_attention_kernel(DecodeArgs a) {
+    typedef typename Half<TYPE>::type T;
+    typedef Shape<DIM> S;
+    typedef T T8 __attribute__((ext_vector_type(8)));
+    constexpr int kParts = TYPE == WINO_FP16 ? 2 : 1;       // bf16 numbers of a query element
+    __shared__ __attribute__((aligned(16))) uint8_t lds[S::kLds];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int split = blockIdx.x / a.units;
+    int unit = blockIdx.x - split * a.units;
+    const int tile = unit % a.tiles;
+    unit /= a.tiles;
+    const int kvh = unit % a.kv_heads, b = unit / a.kv_heads;
+
+    const int len = min(max(a.lens[b], 0), a.room);
+    const int first_end = len - a.q_len + 1;                // tokens that query 0 sees; every row sees those
+    const int begin = split * a.chunk;
+    const int end = len - begin < a.chunk ? len : begin + a.chunk;
+    if (begin >= len && split > 0) return;                  // the join knows it from the length
+
+    // this lane's row: query i, head h
+    const int row = tile * 16 + r;
+    const int i = row / a.group, h = kvh * a.group + row % a.group;
+    const bool real = i < a.q_len;
+    const int row_end = real ? (first_end + i < len ? first_end + i : len) : 0;
+
+    bf16x8 q[kParts][S::kSteps];
+    {
+        const T* p = (const T*)a.q + ((int64_t)b * a.q_len + (real ? i : 0)) * a.q_stride + (int64_t)(real ? h : 0) * DIM +
+                     g * (DIM / 4);
+#pragma unroll
+        for (int j = 0; j < S::kSteps; ++j) {
+            const T8 x = *(const T8*)(p + 8 * j);
+            if constexpr (TYPE == WINO_BF16) {
+                q[0][j] = x;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const __bf16 hi = (__bf16)(float)x[e];
+                    q[0][j][e] = hi;
+                    q[kParts - 1][j][e] = (__bf16)((float)x[e] - (float)hi);
+                }
+            }
+        }
+    }
+
+    f32x4 o[DIM / 16];                                      // lane: dimensions 16 n + 4 g + e of row r
+#pragma unroll
+    for (int n = 0; n < DIM / 16; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float ref = kNever, sum = 0.f;                          // ref: the power of two that o and sum are held against
+    uint8_t* stage = lds + wave * S::kStage;
+
+    const int32_t* pages = a.table + (int64_t)b * a.max_pages;
+    // first slots of a step's tiles (-1: none of its tokens is there)
+    auto place = [&](int t0, int64_t (&at)[S::kTiles]) {
+#pragma unroll
+        for (int n = 0; n < S::kTiles; ++n) {
+            const int t = t0 + 16 * n;
+            at[n] = -1;
+            if (t < end) {
+                const int pg = fast_div(t, a.by_page);
+                const int64_t id = pages[pg];
+                if (id >= 0 && id < a.pages) at[n] = (id * a.kv_heads + kvh) * a.page + (t - pg * a.page);
+            }
+        }
+    };
+
+    int t0 = begin + wave * S::kTok;
+    int64_t at[S::kTiles];
+    Codes<DIM> kc, vc;
+    if (t0 < end) {
+        place(t0, at);
+        load_codes<DIM>(kc, a.k_codes, a.k_scales, at, lane);
+        load_codes<DIM>(vc, a.v_codes, a.v_scales, at, lane);
+    }
+    for (; t0 < end; t0 += kWaves * S::kTok) {
+        // the next step's codes are on their way while this one is computed
+        int64_t at_next[S::kTiles];
+        Codes<DIM> kn, vn;
+        const int tn = t0 + kWaves * S::kTok;
+        if (tn < end) {
+            place(tn, at_next);
+            load_codes<DIM>(kn, a.k_codes, a.k_scales, at_next, lane);
+            load_codes<DIM>(vn, a.v_codes, a.v_scales, at_next, lane);
+        }
+
+        // scores, transposed: lane has tokens 16 n + 4 g + e of row r
+        f32x4 z[S::kTiles];
+#pragma unroll
+        for (int n = 0; n < S::kTiles; ++n) {
+            z[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < S::kSteps; ++j) {
+                const bf16x8 k = decode8(kc.w[n][j], piece_scale<DIM>(kc.s[n], j, g));
+#pragma unroll
+                for (int p = 0; p < kParts; ++p)
+                    z[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[p][j], z[n], 0, 0, 0);
+            }
+            z[n] *= a.scale_log2;
+        }
+        // tokens that some row does not see
+        bool whole = t0 + S::kTok <= (first_end < end ? first_end : end);
+#pragma unroll
+        for (int n = 0; n < S::kTiles; ++n) whole = whole && at[n] >= 0;
+        if (!whole) {
+#pragma unroll
+            for (int n = 0; n < S::kTiles; ++n) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (at[n] < 0 || t0 + 16 * n + 4 * g + e >= row_end) z[n][e] = kNever;
+                // what lies past the length was never written; its scale may say NaN
+                const int t = t0 + 16 * n + r;
+#pragma unroll
+                for (int j = 0; j < S::kScales; ++j) {
+                    // A value that is not finite would spoil the rows that do not see its token too (0 times it is
+                    // NaN): it leaves the product, and the rows that see it are marked here.
+                    uint64_t spoilt = __ballot(t < end && t >= first_end && vc.s[n][j] >= 253u);
+                    if (t >= end || ((spoilt >> lane) & 1)) vc.s[n][j] = 0;
+                    for (; spoilt; spoilt &= spoilt - 1) {
+                        const int l = __builtin_ctzll(spoilt), quarter = l >> 4;
+                        if (t0 + 16 * n + (l & 15) >= row_end) continue;
+                        const int group = min(quarter * (DIM / 4) / 32 + j, DIM / 32 - 1);
+#pragma unroll
+                        for (int m = 0; m < DIM / 16; ++m)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int d = 16 * m + 4 * g + e;
+                                if (d / (DIM / 4) == quarter && d / 32 == group) o[m][e] = __builtin_nanf("");
+                            }
+                    }
+                }
+            }
+        }
+        float top = kNever;
+#pragma unroll
+        for (int n = 0; n < S::kTiles; ++n)
+            top = __builtin_fmaxf(__builtin_fmaxf(top, __builtin_fmaxf(z[n][0], z[n][1])), __builtin_fmaxf(z[n][2], z[n][3]));
+        top = max_rows(top);
+        // o and sum move to a new reference only where the maximum has outgrown the old one by 2^8
+        if (__any(top > ref + 8.f)) {
+            const float to = __builtin_fmaxf(ref, top);
+            const float alpha = to == kNever ? 1.f : __builtin_amdgcn_exp2f(ref - to);
+            ref = to;
+            sum *= alpha;
+#pragma unroll
+            for (int n = 0; n < DIM / 16; ++n) o[n] *= alpha;
+        }
+        const float base = ref == kNever ? 0.f : ref;
+        uint32_t hi[S::kTiles][2], lo[S::kTiles][2];
+#pragma unroll
+        for (int n = 0; n < S::kTiles; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(z[n][e] - base), p1 = __builtin_amdgcn_exp2f(z[n][e + 1] - base);
+                sum += p0 + p1;
+                const bf16x2 x = {(__bf16)p0, (__bf16)p1};
+                const bf16x2 y = {(__bf16)(p0 - (float)x[0]), (__bf16)(p1 - (float)x[1])};
+                hi[n][e / 2] = __builtin_bit_cast(uint32_t, x);
+                lo[n][e / 2] = __builtin_bit_cast(uint32_t, y);
+            }
+
+        // 32 tokens at a time: V to LDS by tokens, back by dimensions
+#pragma unroll
+        for (int m = 0; m < S::kTiles / 2; ++m) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int j = 0; j < S::kSteps; ++j)
+                    *(bf16x8*)(stage + (16 * n + r) * S::kRow + g * (DIM / 2) + 16 * j) =
+                        decode8(vc.w[2 * m + n][j], piece_scale<DIM>(vc.s[2 * m + n], j, g));
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            const u32x4 ph = {hi[2 * m][0], hi[2 * m][1], hi[2 * m + 1][0], hi[2 * m + 1][1]};
+            const u32x4 pl = {lo[2 * m][0], lo[2 * m][1], lo[2 * m + 1][0], lo[2 * m + 1][1]};
+            // lane l of 16 gives the address of four dimensions of token l / 4 and gets dimension l of four tokens
+            const uint8_t* from = stage + (4 * g + (r >> 2)) * S::kRow + (r & 3) * 8;
+#pragma unroll
+            for (int n = 0; n < DIM / 16; ++n) {
+                typedef __attribute__((ext_vector_type(4))) short s4;
+                typedef __attribute__((address_space(3))) s4* lds4;
+                const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(from + 32 * n)));
+                const u32x2 y = __builtin_bit_cast(
+                    u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(from + 16 * S::kRow + 32 * n)));
+                const bf16x8 v = __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]});
+                o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, ph), o[n], 0, 0, 0);
+                o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, pl), o[n], 0, 0, 0);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+        kc = kn;
+        vc = vn;
+#pragma unroll
+        for (int n = 0; n < S::kTiles; ++n) at[n] = at_next[n];
+    }
+    sum = sum_rows(sum);
+
+    // join the waves: [wave][row][dim + 2]
+    __syncthreads();
+    float* mine = (float*)lds + (wave * 16 + r) * (DIM + 2);
+#pragma unroll
+    for (int n = 0; n < DIM / 16; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine[16 * n + 4 * g + e] = o[n][e];
+    if (g == 0) {
+        mine[DIM] = ref;
+        mine[DIM + 1] = sum;
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < 16 * DIM; x += 64 * kWaves) {
+        const int rr = x / DIM, d = x % DIM;
+        const float* w = (const float*)lds + rr * (DIM + 2);
+        float m = kNever;
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) m = __builtin_fmaxf(m, w[k * 16 * (DIM + 2) + DIM]);
+        const float base = m == kNever ? 0.f : m;
+        float total = 0.f, acc = 0.f;
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) {
+            const float f = __builtin_amdgcn_exp2f(w[k * 16 * (DIM + 2) + DIM] - base);
+            total += f * w[k * 16 * (DIM + 2) + DIM + 1];
+            acc += f * w[k * 16 * (DIM + 2) + d];
+        }
+        if (a.part) {
+            float* p = a.part + ((int64_t)blockIdx.x * 16 + rr) * (DIM + 2);
+            p[d] = acc;
+            if (d == 0) p[DIM] = m, p[DIM + 1] = total;
+        } else {
+            const int ro = tile * 16 + rr, io = ro / a.group;
+            if (io < a.q_len)
+                ((T*)a.out)[(((int64_t)b * a.q_len + io) * a.heads + kvh * a.group + ro % a.group) * DIM + d] =
+                    (T)(total == 0.f ? 0.f : acc / total);
+        }
+    }
+}
+
+// Joins the parts of split sequences: one block per query row and head.
+template <int TYPE, int DIM> __global__ __launch_bounds__(DIM) void kv4_join_kernel(DecodeArgs a) {
+    typedef typename Half<TYPE>::type T;
+    const int d = threadIdx.x, h = blockIdx.x % a.heads;
+    const int64_t token = blockIdx.x / a.heads;
+    const int b = (int)(token / a.q_len), i = (int)(token % a.q_len);
+    const int row = i * a.group + h % a.group;
+    const int unit = (b * a.kv_heads + h / a.group) * a.tiles + row / 16;
+    const int len = min(max(a.lens[b], 0), a.room);
+    int parts = (len + a.chunk - 1) / a.chunk;
+    parts = parts < 1 ? 1 : parts;
+    const int64_t step = (int64_t)a.units * 16 * (DIM + 2);
+    const float* p = a.part + ((int64_t)unit * 16 + row % 16) * (DIM + 2);
+    float m = kNever, total = 0.f, acc = 0.f;
+    for (int s = 0; s < parts; ++s) m = __builtin_fmaxf(m, p[s * step + DIM]);
+    const float base = m == kNever ? 0.f : m;
+    for (int s = 0; s < parts; ++s) {
+        const float f = __builtin_amdgcn_exp2f(p[s * step + DIM] - base);
+        total += f * p[s * step + DIM + 1];
+        acc += f * p[s * step + d];
+    }
+    ((T*)a.out)[(token * a.heads + h) * DIM + d] = (T)(total == 0.f ? 0.f : acc / total);
+}
+
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+struct Cut {
+    int64_t tiles, units, chunk, splits;
+    size_t bytes(int dim) const { return splits > 1 ? (size_t)(splits * units * 16 * (dim + 2) * 4) : 0; }
+};
+
+// Parts of a sequence: enough workgroups for four on each compute unit when
+// every sequence fills its table, no part under 256 tokens.
+Cut cut(int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int dim, int64_t room, size_t have) {
+    Cut c;
+    c.tiles = (q_len * (heads / kv_heads) + 15) / 16;
+    c.units = batch * kv_heads * c.tiles;
+    const int64_t want = 1024;
+    c.chunk = std::max<int64_t>(256, (room * c.units / want + 255) / 256 * 256);
+    c.splits = std::max<int64_t>(1, (room + c.chunk - 1) / c.chunk);
+    if (c.bytes(dim) > have) {
+        const int64_t fit = (int64_t)(have / (size_t)(c.units * 16 * (dim + 2) * 4));
+        c.splits = std::max<int64_t>(1, fit);
+        c.chunk = std::max<int64_t>(256, ((room + c.splits - 1) / c.splits + 255) / 256 * 256);
+        c.splits = std::max<int64_t>(1, (room + c.chunk - 1) / c.chunk);
+    }
+    return c;
+}
+
+template <int TYPE, int DIM> wino_status launch(const DecodeArgs& a, int64_t rows, hipStream_t stream) {
+    hipLaunchKernelGGL((kv4_attention_kernel<TYPE, DIM>), dim3((unsigned)((int64_t)a.units * a.splits)), dim3(64 * kWaves), 0,
+                       stream, a);
+    if (hipGetLastError() != hipSuccess) return WINO_EHIP;
+    if (!a.part) return WINO_OK;
+    hipLaunchKernelGGL((kv4_join_kernel<TYPE, DIM>), dim3((unsigned)rows), dim3(DIM), 0, stream, a);
+    return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
+}
+
+template <int TYPE> wino_status launch_dim(int dim, const DecodeArgs& a, int64_t rows, hipStream_t stream) {
+    switch (dim) {
+        case 64: return launch<TYPE, 64>(a, rows, stream);
+        case 96: return launch<TYPE, 96>(a, rows, stream);
+        case 128: return launch<TYPE, 128>(a, rows, stream);
+        case 192: return launch<TYPE, 192>(a, rows, stream);
+        default: return launch<TYPE, 256>(a, rows, stream);
+    }
+}
 
 }  // namespace
 
 extern "C" size_t kv4_attention_workspace_bytes(int32_t batch, int32_t q_len, int32_t heads, int32_t kv_heads,
                                                 int32_t head_dim, int32_t max_pages, int32_t page_size) {
-    (void)batch, (void)q_len, (void)heads, (void)kv_heads, (void)head_dim, (void)max_pages, (void)page_size;
-    return 0;
+    if (batch < 1 || q_len < 1 || heads < 1 || kv_heads < 1 || head_dim < 1 || max_pages < 1 || page_size < 1) return 0;
+    if (heads % kv_heads || (int64_t)batch * q_len * heads > 0x7fffffffll) return 0;
+    return cut(batch, q_len, heads, kv_heads, head_dim, (int64_t)max_pages * page_size, (size_t)-1).bytes(head_dim);
 }
 
 extern "C" wino_status kv4_attention(const void* q, int64_t q_stride, const kv4_cache* cache,
                                      const int32_t* block_table, int32_t max_pages, const int32_t* lens, void* out,
                                      int32_t batch, int32_t q_len, int32_t heads, float scale, wino_float_type type,
                                      void* workspace, size_t workspace_bytes, hipStream_t stream) {
-    (void)workspace, (void)workspace_bytes;
     if (!cache || (type != WINO_BF16 && type != WINO_FP16)) return WINO_EINVAL;
     const kv4_cache& c = *cache;
     if (c.pages < 0 || c.kv_heads < 1 || c.page_size < 1 || c.head_dim < 1 || batch < 0 || q_len < 0 || heads < 1 ||
@@ -114,15 +447,19 @@ extern "C" wino_status kv4_attention(const void* q, int64_t q_stride, const kv4_
     if (c.pages > 0 && (!c.k_codes || !c.k_scales || !c.v_codes || !c.v_scales)) return WINO_EINVAL;
     const bool many = (int64_t)batch * q_len > 1;
     if (many && q_stride < (int64_t)heads * c.head_dim) return WINO_EINVAL;
-    if ((many && (q_stride & 7)) || !aligned16(q) || !aligned16(out) || !aligned16(c.k_codes) || !aligned16(c.v_codes))
+    if ((many && (q_stride & 7)) || !aligned16(q) || !aligned16(out) || !aligned16(c.k_codes) || !aligned16(c.v_codes) ||
+        !aligned16(workspace))
         return WINO_EUNSUPPORTED;
-    const int64_t blocks = (int64_t)batch * q_len * heads;
-    if (blocks > 0x7fffffffll) return WINO_EUNSUPPORTED;
-    DecodeArgs a = {q, out, c.k_codes, c.k_scales, c.v_codes, c.v_scales, block_table, lens, q_stride, c.pages,
-                    q_len, heads, c.kv_heads, c.head_dim, c.page_size, max_pages, scale};
-    if (type == WINO_BF16)
-        hipLaunchKernelGGL(kv4_attention_kernel<WINO_BF16>, dim3((unsigned)blocks), dim3(64), 0, stream, a);
-    else
-        hipLaunchKernelGGL(kv4_attention_kernel<WINO_FP16>, dim3((unsigned)blocks), dim3(64), 0, stream, a);
-    return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
+    const int64_t rows = (int64_t)batch * q_len * heads;
+    if (rows > 0x7fffffffll) return WINO_EUNSUPPORTED;
+    const int64_t room = std::min<int64_t>((int64_t)max_pages * c.page_size, 0x7fffffff - 4096);
+    const Cut k = cut(batch, q_len, heads, c.kv_heads, c.head_dim, room, workspace ? workspace_bytes : 0);
+    if (k.units * k.splits > 0x7fffffffll) return WINO_EUNSUPPORTED;
+    DecodeArgs a = {q, out, c.k_codes, c.k_scales, c.v_codes, c.v_scales, block_table, lens,
+                    k.splits > 1 ? (float*)workspace : nullptr, q_stride, c.pages, q_len, heads, c.kv_heads,
+                    heads / c.kv_heads, c.page_size, max_pages, (int32_t)k.tiles, (int32_t)k.units, (int32_t)k.splits,
+                    (int32_t)std::min<int64_t>(k.chunk, 0x7fffffff - 4096), (int32_t)room, winof4::make_fastdiv((uint32_t)c.page_size),
+                    scale * 1.44269504088896340736f};
+    return type == WINO_BF16 ? launch_dim<WINO_BF16>(c.head_dim, a, rows, stream)
+                             : launch_dim<WINO_FP16>(c.head_dim, a, rows, stream);
 }

@@ -63,6 +63,39 @@ __device__ inline float inverse_scale(uint32_t s) {
                      : __builtin_bit_cast(float, (254u - s) << 23);
 }
 
+// Eight codes (one word) to bf16 with their scale, exactly: the converter reads
+// only the exponent bits of its scale operand, so the byte shifted into place
+// is 2^(s - 127) down to s = 0, and s = 255 gives NaN.
+__device__ inline bf16x8 decode8(uint32_t word, float scale_bits) {
+    const bf16x2 a = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale_bits, 0));
+    const bf16x2 b = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale_bits, 1));
+    const bf16x2 c = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale_bits, 2));
+    const bf16x2 d = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale_bits, 3));
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+__device__ inline float scale_bits(uint32_t s) { return __builtin_bit_cast(float, s << 23); }
+
+// Both halves (rows) of a wave beside each other: x of this lane's half-wave
+// (row) and of the other one, in some order.
+template <int ROWS> __device__ inline f32x2 swap_rows(float x) {
+    const uint32_t a = __builtin_bit_cast(uint32_t, x);
+    const auto s = ROWS == 2 ? __builtin_amdgcn_permlane32_swap(a, a, false, false)
+                             : __builtin_amdgcn_permlane16_swap(a, a, false, false);
+    const uint32_t u = s[0], v = s[1];      // scalars: a bit cast of a vector's element reads element 0
+    return f32x2{__builtin_bit_cast(float, u), __builtin_bit_cast(float, v)};
+}
+// Maximum and sum over the four 16-lane rows of a wave, lane by lane.
+__device__ inline float max_rows(float x) {
+    const f32x2 a = swap_rows<2>(x);
+    const f32x2 b = swap_rows<1>(__builtin_fmaxf(a[0], a[1]));
+    return __builtin_fmaxf(b[0], b[1]);
+}
+__device__ inline float sum_rows(float x) {
+    const f32x2 a = swap_rows<2>(x);
+    const f32x2 b = swap_rows<1>(a[0] + a[1]);
+    return b[0] + b[1];
+}
+
 // 16-bit floating types at the edges of a kernel.
 template <int TYPE> struct Half;
 template <> struct Half<WINO_BF16> {
