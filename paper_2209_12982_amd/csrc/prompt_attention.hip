@@ -1,5 +1,13 @@
 // Causal attention over whole prompts: packed sequences of different lengths,
-// grouped heads, keys and values in 16 bits.
+// grouped heads, keys and values in 16 bits: o = sum_t softmax_t(scale q.k_t) v_t.
+//
+// The matrix cores bound it.  A workgroup takes 128 queries of one head, a wave
+// 32 of them, and walks over the keys 64 at a time with a running maximum and
+// sum.  Scores come out transposed (keys x queries), so a lane keeps one
+// query's statistics, half of its keys in the lane 32 further on, and its
+// probabilities are already the second operand of the second product: the
+// order of keys inside a product is free, and V, read across keys by the
+// transposing LDS read, takes the order that the scores have.
 #include <hip/hip_runtime.h>
 
 #include "mx4.h"
@@ -8,68 +16,276 @@
 namespace {
 using namespace mx4;
 
+constexpr int kWaves = 4, kRows = 32 * kWaves, kKeys = 64;
+constexpr float kNever = -__builtin_inff();
+
 struct PromptArgs {
     const void *q, *k, *v;
     void* out;
     const int32_t *cu_q, *cu_k;
     int64_t q_stride, k_stride, v_stride;
-    int32_t seqs, total_q, total_k, heads, kv_heads, dim, causal;
-    float scale;
+    int32_t seqs, total_q, total_k, heads, kv_heads, causal;
+    float scale_log2;       // scale * log2(e): probabilities are powers of two
 };
 
-// One wave per query row and head, 64 keys at a time.
-template <int TYPE>
-__global__ __launch_bounds__(64) void prompt_attention_kernel(PromptArgs a) {
-    typedef typename Half<TYPE>::type T;
-    __shared__ float qs[256], ps[64];
-    const int lane = threadIdx.x, h = blockIdx.x % a.heads, kvh = h / (a.heads / a.kv_heads);
-    const int row = blockIdx.x / a.heads;
-    int s = 0;
-    while (s < a.seqs && !(row >= a.cu_q[s] && row < a.cu_q[s + 1])) ++s;
-    T* out = (T*)a.out + ((int64_t)row * a.heads + h) * a.dim;
-    if (s == a.seqs) return;
-    const int q0 = max(0, a.cu_q[s]), q1 = min(a.cu_q[s + 1], a.total_q);
-    const int k0 = max(0, min(a.cu_k[s], a.total_k)), n = max(0, min(a.cu_k[s + 1], a.total_k) - k0);
-    const int end = a.causal ? n - (q1 - q0) + 1 + (row - q0) : n;
-    const T* q = (const T*)a.q + (int64_t)row * a.q_stride + (int64_t)h * a.dim;
-    for (int d = lane; d < a.dim; d += 64) qs[d] = (float)q[d] * a.scale;
-    float top = -__builtin_inff(), sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int t0 = 0; t0 < end; t0 += 64) {
-        const int t = t0 + lane;
-        __syncthreads();
-        float z = -__builtin_inff();
-        if (t < end) {
-            const T* k = (const T*)a.k + (int64_t)(k0 + t) * a.k_stride + (int64_t)kvh * a.dim;
-            z = 0.f;
-            for (int d = 0; d < a.dim; ++d) z += qs[d] * (float)k[d];
+template <int DIM> struct Shape {
+    // bytes of a row in LDS: 16 rows of K start in 16 different 16-byte columns of the 256-byte banks, 4 rows of V
+    // in four different 64-byte ones
+    static constexpr int kRowK = DIM * 2 + 16;
+    static constexpr int kRowV = DIM * 2 % 256 == 192 ? DIM * 2 : DIM * 2 + 64;
+    static constexpr int kTileK = kKeys * kRowK, kTileV = kKeys * kRowV;
+    static constexpr int kPieces = kKeys * DIM / 8 / (64 * kWaves);     // 16-byte pieces of a tile for a thread
+};
+
+template <int TYPE> struct Mfma;
+template <> struct Mfma<WINO_BF16> {
+    typedef bf16x8 T8;
+    typedef bf16x2 T2;
+    static __device__ f32x16 mul(T8 a, T8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Mfma<WINO_FP16> {
+    typedef f16x8 T8;
+    typedef f16x2 T2;
+    static __device__ f32x16 mul(T8 a, T8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+
+// The sequence and the tile of its queries that workgroup `index` takes, or false past the last.  Offsets are cut
+// to the tensor.
+struct Work {
+    int q0, nq, k0, nk, tile;
+};
+__device__ inline bool find(const PromptArgs& a, int index, Work& w) {
+    const int lane = threadIdx.x & 63;
+    for (int s0 = 0; s0 < a.seqs; s0 += 64) {
+        const int s = s0 + lane;
+        int from = 0, n = 0;
+        if (s < a.seqs) {
+            from = max(a.cu_q[s], 0);
+            n = max(min(a.cu_q[s + 1], a.total_q) - from, 0);
         }
-        float m = z;
-        for (int i = 32; i; i >>= 1) m = fmaxf(m, __shfl_xor(m, i));
-        m = fmaxf(m, top);
-        const float base = m == -__builtin_inff() ? 0.f : m;
-        const float p = t < end ? expf(z - base) : 0.f, alpha = expf(top - base);
-        top = m;
-        ps[lane] = p;
-        float part = p;
-        for (int i = 32; i; i >>= 1) part += __shfl_xor(part, i);
-        sum = sum * alpha + part;
-        __syncthreads();
-        for (int e = 0; e < 4; ++e) {
-            const int d = lane + 64 * e;
-            if (d >= a.dim) break;
-            float acc = o[e] * alpha;
-            for (int i = 0; i < 64 && t0 + i < end; ++i)
-                acc += ps[i] * (float)((const T*)a.v)[(int64_t)(k0 + t0 + i) * a.v_stride + (int64_t)kvh * a.dim + d];
-            o[e] = acc;
+        const int count = (n + kRows - 1) / kRows;
+        int before = count;                                 // tiles of this and the sequences before, in the 64
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(before, o);
+            if (lane >= o) before += x;
+        }
+        const int all = __shfl(before, 63);
+        if (index < all) {
+            const uint64_t past = __ballot(index < before);
+            const int l = __builtin_ctzll(past);
+            w.q0 = __builtin_amdgcn_readfirstlane(__shfl(from, l));
+            w.nq = __builtin_amdgcn_readfirstlane(__shfl(n, l));
+            w.tile = __builtin_amdgcn_readfirstlane(index - __shfl(before - count, l));
+            const int at = s0 + __builtin_amdgcn_readfirstlane(l);
+            w.k0 = max(min(a.cu_k[at], a.total_k), 0);
+            w.nk = max(min(a.cu_k[at + 1], a.total_k) - w.k0, 0);
+            return true;
+        }
+        index -= all;
+    }
+    return false;
+}
+
+template <int TYPE, int DIM>
+__global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attention_kernel(PromptArgs a) {
+    typedef typename Half<TYPE>::type T;
+    typedef Mfma<TYPE> M;
+    typedef typename M::T8 T8;
+    typedef typename M::T2 T2;
+    typedef Shape<DIM> S;
+    // probabilities are held 2^6 higher in fp16, whose small numbers end at 2^-24
+    constexpr float kLift = TYPE == WINO_FP16 ? 6.f : 0.f;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2][S::kTileK + S::kTileV];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = lane & 31, half = lane >> 5;
+
+    // workgroups that follow each other run on different XCDs: the heads that share a K and V are kv_heads apart, and
+    // late tiles, which see the most keys, come first
+    const int turn = blockIdx.x % a.heads;
+    const int group = a.heads / a.kv_heads, kvh = turn % a.kv_heads, h = kvh * group + turn / a.kv_heads;
+    const int tiles = gridDim.x / a.heads;
+    Work w;
+    if (!find(a, tiles - 1 - (int)(blockIdx.x / a.heads), w)) return;
+
+    const int i0 = w.tile * kRows;                          // first query of the workgroup, in its sequence
+    const int shift = a.causal ? w.nk - w.nq + 1 : w.nk;    // query i sees shift + i keys (all, where not causal)
+    auto sees = [&](int i) { return max(0, a.causal ? min(shift + i, w.nk) : w.nk); };
+    const int every = sees(i0);                             // keys that all rows of the workgroup see
+    const int end = sees(min(i0 + kRows, w.nq) - 1);        // keys that some row sees
+    const int iw = i0 + 32 * wave;
+    const int wave_every = sees(iw), wave_end = iw < w.nq ? sees(min(iw + 32, w.nq) - 1) : 0;
+    const int i = iw + c;                                   // this lane's query
+    const int row_end = i < w.nq ? sees(i) : 0;
+
+    T8 q[DIM / 16];
+    {
+        const T* p = (const T*)a.q + (int64_t)(w.q0 + min(i, w.nq - 1)) * a.q_stride + (int64_t)h * DIM + 8 * half;
+#pragma unroll
+        for (int s = 0; s < DIM / 16; ++s) q[s] = *(const T8*)(p + 16 * s);
+    }
+    f32x16 o[DIM / 32];                                     // lane: dimensions 32 n + 8 (e / 4) + 4 half + e % 4 of query c
+#pragma unroll
+    for (int n = 0; n < DIM / 32; ++n)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[n][e] = 0.f;
+    float ref = kNever, sum = 0.f;                          // ref: the power of two that o and sum are held against
+
+    const T* kbase = (const T*)a.k + (int64_t)w.k0 * a.k_stride + (int64_t)kvh * DIM;
+    const T* vbase = (const T*)a.v + (int64_t)w.k0 * a.v_stride + (int64_t)kvh * DIM;
+    u32x4 ks[S::kPieces], vs[S::kPieces];
+    auto fetch = [&](int t0) {
+#pragma unroll
+        for (int x = 0; x < S::kPieces; ++x) {
+            const int piece = threadIdx.x + 64 * kWaves * x, r = piece / (DIM / 8), d = piece % (DIM / 8) * 8;
+            ks[x] = vs[x] = u32x4{0, 0, 0, 0};
+            if (t0 + r < w.nk) {
+                ks[x] = *(const u32x4*)(kbase + (int64_t)(t0 + r) * a.k_stride + d);
+                vs[x] = *(const u32x4*)(vbase + (int64_t)(t0 + r) * a.v_stride + d);
+            }
+        }
+    };
+    if (end > 0) fetch(0);
+    int buf = 0;
+    for (int t0 = 0; t0 < end; t0 += kKeys, buf ^= 1) {
+        uint8_t* lk = lds[buf];
+        uint8_t* lv = lk + S::kTileK;
+        // A value that is not finite would spoil the rows that do not see its key too (0 times it is NaN): in tiles that
+        // some row sees in part it leaves the product, and is added to the rows that see it.
+        bool spoilt = false;
+        const bool partly = t0 + kKeys > every;
+        if (partly) {
+            constexpr uint32_t kExp = TYPE == WINO_BF16 ? 0x7f80u : 0x7c00u;
+#pragma unroll
+            for (int x = 0; x < S::kPieces; ++x)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t v = vs[x][e];
+                    const bool lo = (v & kExp) == kExp, hi = ((v >> 16) & kExp) == kExp;
+                    spoilt = spoilt || lo || hi;
+                    vs[x][e] = (lo ? 0u : v & 0xffffu) | (hi ? 0u : v & 0xffff0000u);
+                }
+        }
+#pragma unroll
+        for (int x = 0; x < S::kPieces; ++x) {
+            const int piece = threadIdx.x + 64 * kWaves * x, r = piece / (DIM / 8), d = piece % (DIM / 8) * 16;
+            *(u32x4*)(lk + r * S::kRowK + d) = ks[x];
+            *(u32x4*)(lv + r * S::kRowV + d) = vs[x];
+        }
+        if (partly)
+            spoilt = __syncthreads_or(spoilt);
+        else
+            __syncthreads();
+        if (t0 + kKeys < end) fetch(t0 + kKeys);            // the next tile is on its way while this one is computed
+        if (t0 >= wave_end) continue;
+
+        f32x16 z[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) z[b][e] = 0.f;
+            const uint8_t* p = lk + (32 * b + c) * S::kRowK + 16 * half;
+#pragma unroll
+            for (int s = 0; s < DIM / 16; ++s) z[b] = M::mul(*(const T8*)(p + 32 * s), q[s], z[b]);
+        }
+        if (t0 + kKeys > wave_every) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (t0 + 32 * b + 8 * (e / 4) + 4 * half + e % 4 >= row_end) z[b][e] = kNever;
+                    else z[b][e] *= a.scale_log2;
+        } else {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) z[b] *= a.scale_log2;
+        }
+        float top = kNever;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) top = __builtin_fmaxf(__builtin_fmaxf(z[b][e], z[b][e + 1]), top);
+        {
+            const f32x2 x = swap_rows<2>(top);
+            top = __builtin_fmaxf(x[0], x[1]);
+        }
+        // o and sum move to a new reference only where the maximum has outgrown the old one by 2^8
+        if (__any(top > ref + 8.f)) {
+            const float to = __builtin_fmaxf(ref, top);
+            const float alpha = to == kNever ? 1.f : __builtin_amdgcn_exp2f(ref - to);
+            ref = to;
+            sum *= alpha;
+#pragma unroll
+            for (int n = 0; n < DIM / 32; ++n) o[n] *= alpha;
+        }
+        const float base = ref == kNever ? 0.f : ref - kLift;
+        uint32_t p[2][8];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(z[b][e] - base), p1 = __builtin_amdgcn_exp2f(z[b][e + 1] - base);
+                sum += p0 + p1;
+                p[b][e / 2] = __builtin_bit_cast(uint32_t, T2{(T)p0, (T)p1});
+            }
+        // lane l of 16 gives the address of four dimensions of key l / 4 and gets dimension l of four keys
+        const int l = lane & 15;
+        const uint8_t* from = lv + (4 * half + (l >> 2)) * S::kRowV + ((lane >> 4) & 1) * 32 + (l & 3) * 8;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const T8 pp = __builtin_bit_cast(T8, u32x4{p[b][4 * s], p[b][4 * s + 1], p[b][4 * s + 2], p[b][4 * s + 3]});
+#pragma unroll
+                for (int n = 0; n < DIM / 32; ++n) {
+                    typedef __attribute__((ext_vector_type(4))) short s4;
+                    typedef __attribute__((address_space(3))) s4* lds4;
+                    const uint8_t* f = from + (32 * b + 16 * s) * S::kRowV + 64 * n;
+                    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)f));
+                    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(f + 8 * S::kRowV)));
+                    o[n] = M::mul(__builtin_bit_cast(T8, u32x4{x[0], x[1], y[0], y[1]}), pp, o[n]);
+                }
+            }
+        if (spoilt) {
+            for (int t = t0; t < min(t0 + kKeys, row_end); ++t) {
+                const T* v = vbase + (int64_t)t * a.v_stride + 4 * half;
+#pragma unroll
+                for (int n = 0; n < DIM / 32; ++n)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float x = (float)v[32 * n + 8 * (e / 4) + e % 4];
+                        if (!(__builtin_fabsf(x) < __builtin_inff())) o[n][e] += x;
+                    }
+            }
         }
     }
-    for (int e = 0; e < 4; ++e) {
-        const int d = lane + 64 * e;
-        if (d < a.dim) out[d] = (T)(sum == 0.f ? 0.f : o[e] / sum);
+    {
+        const f32x2 x = swap_rows<2>(sum);
+        sum = x[0] + x[1];
+    }
+    if (i < w.nq) {
+        typedef T T4 __attribute__((ext_vector_type(4)));
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        T* out = (T*)a.out + ((int64_t)(w.q0 + i) * a.heads + h) * DIM + 4 * half;
+#pragma unroll
+        for (int n = 0; n < DIM / 32; ++n)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *(T4*)(out + 32 * n + 2 * e) =
+                    sum == 0.f ? T4{} : T4{(T)(o[n][e] * inv), (T)(o[n][e + 1] * inv), (T)(o[n][e + 2] * inv), (T)(o[n][e + 3] * inv)};
     }
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+template <int TYPE> void launch(int dim, dim3 grid, hipStream_t stream, const PromptArgs& a) {
+    const dim3 block(64 * kWaves);
+    switch (dim) {
+        case 64: hipLaunchKernelGGL((prompt_attention_kernel<TYPE, 64>), grid, block, 0, stream, a); break;
+        case 96: hipLaunchKernelGGL((prompt_attention_kernel<TYPE, 96>), grid, block, 0, stream, a); break;
+        case 128: hipLaunchKernelGGL((prompt_attention_kernel<TYPE, 128>), grid, block, 0, stream, a); break;
+        case 192: hipLaunchKernelGGL((prompt_attention_kernel<TYPE, 192>), grid, block, 0, stream, a); break;
+        default: hipLaunchKernelGGL((prompt_attention_kernel<TYPE, 256>), grid, block, 0, stream, a); break;
+    }
+}
 
 }  // namespace
 
@@ -83,21 +299,23 @@ extern "C" wino_status prompt_attention(const void* q, int64_t q_stride, const v
     if (heads % kv_heads || (causal != 0 && causal != 1) || !(scale == scale) || scale - scale != 0.f) return WINO_EINVAL;
     if (head_dim != 64 && head_dim != 96 && head_dim != 128 && head_dim != 192 && head_dim != 256)
         return WINO_EUNSUPPORTED;
-    if (seqs > 65536 || heads > 65536) return WINO_EUNSUPPORTED;
-    if (total_q == 0) return WINO_OK;
-    if (!q || !out || (total_k > 0 && (!k || !v)) || (seqs > 0 && (!cu_q || !cu_k))) return WINO_EINVAL;
+    if (seqs > 65536 || heads > 65536 || total_q > 0x7fffffff - 4096 || total_k > 0x7fffffff - 4096) return WINO_EUNSUPPORTED;
+    if (total_q == 0 || seqs == 0) return WINO_OK;
+    if (!q || !out || (total_k > 0 && (!k || !v)) || !cu_q || !cu_k) return WINO_EINVAL;
     const int64_t dim = head_dim;
     if ((total_q > 1 && q_stride < heads * dim) || (total_k > 1 && (k_stride < kv_heads * dim || v_stride < kv_heads * dim)))
         return WINO_EINVAL;
-    if ((total_q > 1 && (q_stride & 7)) || (total_k > 1 && ((k_stride | v_stride) & 7)) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
+    if ((total_q > 1 && (q_stride & 7)) || (total_k > 1 && ((k_stride | v_stride) & 7)) ||
+        !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
         return WINO_EUNSUPPORTED;
-    const int64_t blocks = (int64_t)total_q * heads;
+    // whole tiles, and one started by each sequence
+    const int64_t blocks = ((int64_t)total_q / kRows + seqs) * heads;
     if (blocks > 0x7fffffffll) return WINO_EUNSUPPORTED;
     PromptArgs a = {q, k, v, out, cu_q, cu_k, q_stride, k_stride, v_stride, seqs, total_q, total_k,
-                    heads, kv_heads, head_dim, causal, scale};
+                    heads, kv_heads, causal, scale * 1.44269504088896340736f};
     if (type == WINO_BF16)
-        hipLaunchKernelGGL(prompt_attention_kernel<WINO_BF16>, dim3((unsigned)blocks), dim3(64), 0, stream, a);
+        launch<WINO_BF16>(head_dim, dim3((unsigned)blocks), stream, a);
     else
-        hipLaunchKernelGGL(prompt_attention_kernel<WINO_FP16>, dim3((unsigned)blocks), dim3(64), 0, stream, a);
+        launch<WINO_FP16>(head_dim, dim3((unsigned)blocks), stream, a);
     return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
 }
