@@ -73,6 +73,14 @@ __device__ inline bf16x8 decode8(uint32_t word, float scale_bits) {
     const bf16x2 d = __builtin_bit_cast(bf16x2, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale_bits, 3));
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+// The same to fp16, exact while 2^(s - 127) lies between 2^-23 and 2^13.
+__device__ inline f16x8 decode8_f16(uint32_t word, float scale_bits) {
+    const f16x2 a = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word, scale_bits, 0));
+    const f16x2 b = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word, scale_bits, 1));
+    const f16x2 c = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word, scale_bits, 2));
+    const f16x2 d = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word, scale_bits, 3));
+    return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
 __device__ inline float scale_bits(uint32_t s) { return __builtin_bit_cast(float, s << 23); }
 
 // Both halves (rows) of a wave beside each other: x of this lane's half-wave
