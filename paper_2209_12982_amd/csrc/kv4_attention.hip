@@ -29,7 +29,8 @@ namespace {
 using namespace mx4;
 using winof4::FastDiv;
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4, kBlock = 256;     // tokens of a workgroup's step
+constexpr int kGroups = 768;                // workgroups that fit on the device at once (heads up to 128)
 constexpr float kNever = -__builtin_inff();
 
 struct DecodeArgs {
@@ -37,12 +38,14 @@ struct DecodeArgs {
     void* out;
     const uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
     const int32_t *table, *lens;
-    float* part;            // [units * splits][16][dim + 2] partial sums, maxima and sums, or null
+    float* part;            // [2 * workgroups][16][dim] sums of parts, then [2 * workgroups][16][2] their references and
+                            // totals; null: a workgroup takes a whole sequence
     int64_t q_stride, pages;
     int32_t q_len, heads, kv_heads, group, page, max_pages;
     int32_t tiles;          // 16-row tiles of a sequence's rows at one cache head
-    int32_t units;          // batch * kv_heads * tiles
-    int32_t splits, chunk;  // parts of a sequence, tokens in each
+    int32_t batch;
+    int32_t units;          // of a sequence: kv_heads * tiles
+    int32_t groups;         // workgroups
     int32_t room;           // tokens that a table has room for
     FastDiv by_page;
     float scale_log2;       // scale * log2(e): probabilities are powers of two
@@ -74,16 +77,10 @@ __device__ inline void load_codes(Codes<DIM>& c, const uint8_t* codes, const uin
                                   int lane) {
     typedef Shape<DIM> S;
     const int t = lane & 15, g = lane >> 4;
+    const int code_at = t * (DIM / 2) + g * (DIM / 8), first = g * (DIM / 4) / 32, scale_at = t * (DIM / 32) + first;
 #pragma unroll
     for (int i = 0; i < S::kTiles; ++i) {
-        if (at[i] < 0) {                                    // wave-uniform: no such tokens
-#pragma unroll
-            for (int j = 0; j < S::kSteps; ++j) c.w[i][j] = 0;
-#pragma unroll
-            for (int j = 0; j < S::kScales; ++j) c.s[i][j] = 0;
-            continue;
-        }
-        const uint8_t* p = codes + (at[i] + t) * (DIM / 2) + g * (DIM / 8);
+        const uint8_t* p = codes + at[i] * (DIM / 2) + code_at;
         if constexpr (S::kSteps % 4 == 0) {
 #pragma unroll
             for (int j = 0; j < S::kSteps; j += 4) {
@@ -100,10 +97,9 @@ __device__ inline void load_codes(Codes<DIM>& c, const uint8_t* codes, const uin
 #pragma unroll
             for (int j = 0; j < S::kSteps; ++j) c.w[i][j] = *(const uint32_t*)(p + 4 * j);
         }
-        const uint8_t* s = scales + (at[i] + t) * (DIM / 32);
-        const int first = g * (DIM / 4) / 32;
-        c.s[i][0] = s[first];
-        if constexpr (S::kScales == 2) c.s[i][1] = s[first + 1 < DIM / 32 ? first + 1 : first];
+        const uint8_t* s = scales + at[i] * (DIM / 32) + scale_at;
+        c.s[i][0] = s[0];
+        if constexpr (S::kScales == 2) c.s[i][1] = s[first + 1 < DIM / 32 ? 1 : 0];
     }
 }
 
@@ -114,8 +110,60 @@ template <int DIM> __device__ inline float piece_scale(const uint32_t (&s)[Shape
     return scale_bits(mine == first ? s[0] : s[Shape<DIM>::kScales - 1]);
 }
 
+// The work of a call is the blocks of 256 tokens of all units in a row: sequence by sequence, its units one after the
+// other, the blocks of a unit in order.  Each workgroup takes an equal share of the row, so long and short sequences
+// keep all of them busy alike; units that it holds whole go straight to the output, the two at its ends may be parts.
+__device__ inline int length(const DecodeArgs& a, int b) { return min(max(a.lens[b], 0), a.room); }
+__device__ inline int blocks(int len) { return max(1, (len + kBlock - 1) / kBlock); }
+
+struct Place {
+    int64_t share, before;      // blocks of a workgroup; blocks of all units of the sequences before b
+    int b;
+};
+// The share of a workgroup, and the sequence that block `at(share)` of the row belongs to (or that sequence `want`
+// begins with, where at is below 0).
+template <class AT> __device__ inline Place find(const DecodeArgs& a, int want, AT at) {
+    const int lane = threadIdx.x & 63;
+    int64_t total = 0;
+    int n = 0, first = 0;                                   // blocks of this lane's sequence, and of the 64 up to it
+    for (int b0 = 0; b0 < a.batch; b0 += 64) {
+        n = b0 + lane < a.batch ? blocks(length(a, b0 + lane)) : 0;
+        first = n;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(first, o);
+            if (lane >= o) first += x;
+        }
+        total += __shfl(first, 63);
+    }
+    Place p;
+    p.share = (total * a.units + a.groups - 1) / a.groups;
+    p.b = a.batch;
+    p.before = 0;
+    int64_t f = at(p.share);
+    for (int b0 = 0; b0 < a.batch; b0 += 64) {
+        if (a.batch > 64) {
+            n = b0 + lane < a.batch ? blocks(length(a, b0 + lane)) : 0;
+            first = n;
+            for (int o = 1; o < 64; o <<= 1) {
+                const int x = __shfl_up(first, o);
+                if (lane >= o) first += x;
+            }
+        }
+        const int all = __shfl(first, 63);
+        const uint64_t hit = f >= 0 ? __ballot(f < (p.before + first) * a.units) : (want < b0 + 64 ? 1ull << (want - b0) : 0);
+        if (hit) {
+            const int l = __builtin_ctzll(hit);
+            p.b = __builtin_amdgcn_readfirstlane(b0 + l);
+            p.before += __builtin_amdgcn_readfirstlane(__shfl(first - n, l));
+            break;
+        }
+        p.before += all;
+    }
+    return p;
+}
+
 template <int TYPE, int DIM>
-__global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void kv4_attention_kernel(DecodeArgs a) {
+__global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 3 : 2) void kv4_attention_kernel(DecodeArgs a) {
     typedef typename Half<TYPE>::type T;
     typedef Shape<DIM> S;
     typedef T T8 __attribute__((ext_vector_type(8)));
@@ -123,17 +171,32 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void kv4_attention
     __shared__ __attribute__((aligned(16))) uint8_t lds[S::kLds];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
-    const int split = blockIdx.x / a.units;
-    int unit = blockIdx.x - split * a.units;
-    const int tile = unit % a.tiles;
-    unit /= a.tiles;
-    const int kvh = unit % a.kv_heads, b = unit / a.kv_heads;
 
-    const int len = min(max(a.lens[b], 0), a.room);
+    int b, unit, blk, left;                                 // left: blocks of the share still to do
+    if (a.part) {
+        const Place p = find(a, 0, [&](int64_t share) { return share * blockIdx.x; });
+        if (p.b >= a.batch) return;
+        b = p.b;
+        const int n = __builtin_amdgcn_readfirstlane(blocks(length(a, b)));
+        const int64_t in = p.share * blockIdx.x - p.before * a.units;
+        unit = __builtin_amdgcn_readfirstlane((int)(in / n));
+        blk = __builtin_amdgcn_readfirstlane((int)(in - (int64_t)unit * n));
+        left = __builtin_amdgcn_readfirstlane((int)p.share);
+    } else {
+        b = blockIdx.x / a.units;
+        unit = blockIdx.x % a.units;
+        blk = 0;
+        left = __builtin_amdgcn_readfirstlane(blocks(length(a, b)));
+    }
+    bool opening = true;                                    // the first unit of the share
+    for (;;) {
+    const int len = __builtin_amdgcn_readfirstlane(length(a, b)), n_blocks = blocks(len);
+    const int take = min(left, n_blocks - blk);
+    const bool is_part = take < n_blocks;
+    const int tile = unit % a.tiles, kvh = unit / a.tiles;
     const int first_end = len - a.q_len + 1;                // tokens that query 0 sees; every row sees those
-    const int begin = split * a.chunk;
-    const int end = len - begin < a.chunk ? len : begin + a.chunk;
-    if (begin >= len && split > 0) return;                  // the join knows it from the length
+    const int begin = blk * kBlock;
+    const int end = a.pages == 0 ? begin : (len - begin < take * kBlock ? len : begin + take * kBlock);
 
     // this lane's row: query i, head h
     const int row = tile * 16 + r;
@@ -167,40 +230,47 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void kv4_attention
     float ref = kNever, sum = 0.f;                          // ref: the power of two that o and sum are held against
     uint8_t* stage = lds + wave * S::kStage;
 
+    // First slots of the tiles to come: lane l has tile l % kTiles of step `listed` + l / kTiles.  A tile whose tokens
+    // are not there has a bit in `there` missing, and stands at slot 0.
+    constexpr int kListed = 64 / S::kTiles;
     const int32_t* pages = a.table + (int64_t)b * a.max_pages;
-    // first slots of a step's tiles (-1: none of its tokens is there)
-    auto place = [&](int t0, int64_t (&at)[S::kTiles]) {
+    const int w0 = begin + wave * S::kTok;                  // the wave's first token
+    uint64_t slot = 0, there = 0;
+    auto list = [&](int step) {
+        const int t = w0 + (step + lane / S::kTiles) * (kWaves * S::kTok) + 16 * (lane % S::kTiles);
+        int64_t id = -1;
+        int pg = 0;
+        if (t < end) {
+            pg = fast_div(t, a.by_page);
+            id = pages[pg];
+        }
+        const bool ok = id >= 0 && id < a.pages;
+        slot = ok ? (id * a.kv_heads + kvh) * a.page + (t - pg * a.page) : 0;
+        there = __ballot(ok);
+    };
+    auto place = [&](int step, int64_t (&at)[S::kTiles]) {
 #pragma unroll
         for (int n = 0; n < S::kTiles; ++n) {
-            const int t = t0 + 16 * n;
-            at[n] = -1;
-            if (t < end) {
-                const int pg = fast_div(t, a.by_page);
-                const int64_t id = pages[pg];
-                if (id >= 0 && id < a.pages) at[n] = (id * a.kv_heads + kvh) * a.page + (t - pg * a.page);
-            }
+            const int l = step % kListed * S::kTiles + n;
+            at[n] = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(slot >> 32), l) << 32 |
+                              (uint32_t)__builtin_amdgcn_readlane((int)slot, l));
         }
     };
+    auto tiles_there = [&](int step) { return (uint32_t)(there >> (step % kListed * S::kTiles)) & ((1u << S::kTiles) - 1); };
 
-    int t0 = begin + wave * S::kTok;
-    int64_t at[S::kTiles];
+    int t0 = w0, step = 0;
+    uint32_t have = 0;                                      // tiles of this step that are there
     Codes<DIM> kc, vc;
     if (t0 < end) {
-        place(t0, at);
+        list(0);
+        int64_t at[S::kTiles];
+        place(0, at);
+        have = tiles_there(0);
         load_codes<DIM>(kc, a.k_codes, a.k_scales, at, lane);
         load_codes<DIM>(vc, a.v_codes, a.v_scales, at, lane);
     }
     for (; t0 < end; t0 += kWaves * S::kTok) {
-        // the next step's codes are on their way while this one is computed
-        int64_t at_next[S::kTiles];
-        Codes<DIM> kn, vn;
-        const int tn = t0 + kWaves * S::kTok;
-        if (tn < end) {
-            place(tn, at_next);
-            load_codes<DIM>(kn, a.k_codes, a.k_scales, at_next, lane);
-            load_codes<DIM>(vn, a.v_codes, a.v_scales, at_next, lane);
-        }
-
+        const bool more = t0 + kWaves * S::kTok < end;
         // scores, transposed: lane has tokens 16 n + 4 g + e of row r
         f32x4 z[S::kTiles];
 #pragma unroll
@@ -215,18 +285,25 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void kv4_attention
             }
             z[n] *= a.scale_log2;
         }
+        // the next step's codes are on their way as soon as the registers of this one's are free
+        int64_t at[S::kTiles];
+        uint32_t have_next = 0;
+        if (more) {
+            ++step;
+            if (step % kListed == 0) list(step);
+            place(step, at);
+            have_next = tiles_there(step);
+            load_codes<DIM>(kc, a.k_codes, a.k_scales, at, lane);
+        }
         // tokens that some row does not see
-        bool whole = t0 + S::kTok <= (first_end < end ? first_end : end);
-#pragma unroll
-        for (int n = 0; n < S::kTiles; ++n) whole = whole && at[n] >= 0;
-        if (!whole) {
+        if (t0 + S::kTok > (first_end < end ? first_end : end) || have != (1u << S::kTiles) - 1) {
 #pragma unroll
             for (int n = 0; n < S::kTiles; ++n) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (at[n] < 0 || t0 + 16 * n + 4 * g + e >= row_end) z[n][e] = kNever;
+                    if (!((have >> n) & 1) || t0 + 16 * n + 4 * g + e >= row_end) z[n][e] = kNever;
                 // what lies past the length was never written; its scale may say NaN
-                const int t = t0 + 16 * n + r;
+                const int t = (have >> n) & 1 ? t0 + 16 * n + r : end;
 #pragma unroll
                 for (int j = 0; j < S::kScales; ++j) {
                     // A value that is not finite would spoil the rows that do not see its token too (0 times it is
@@ -285,6 +362,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void kv4_attention
                 for (int j = 0; j < S::kSteps; ++j)
                     *(bf16x8*)(stage + (16 * n + r) * S::kRow + g * (DIM / 2) + 16 * j) =
                         decode8(vc.w[2 * m + n][j], piece_scale<DIM>(vc.s[2 * m + n], j, g));
+            if (m == S::kTiles / 2 - 1 && more) load_codes<DIM>(vc, a.v_codes, a.v_scales, at, lane);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
             const u32x4 ph = {hi[2 * m][0], hi[2 * m][1], hi[2 * m + 1][0], hi[2 * m + 1][1]};
@@ -305,10 +383,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void kv4_attention
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         }
-        kc = kn;
-        vc = vn;
-#pragma unroll
-        for (int n = 0; n < S::kTiles; ++n) at[n] = at_next[n];
+        have = have_next;
     }
     sum = sum_rows(sum);
 
@@ -338,10 +413,13 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void kv4_attention
             total += f * w[k * 16 * (DIM + 2) + DIM + 1];
             acc += f * w[k * 16 * (DIM + 2) + d];
         }
-        if (a.part) {
-            float* p = a.part + ((int64_t)blockIdx.x * 16 + rr) * (DIM + 2);
-            p[d] = acc;
-            if (d == 0) p[DIM] = m, p[DIM + 1] = total;
+        if (is_part) {
+            const int64_t p = ((int64_t)2 * blockIdx.x + (opening ? 0 : 1)) * 16 + rr;
+            a.part[p * DIM + d] = acc;
+            if (d == 0) {
+                float* ml = a.part + (int64_t)2 * a.groups * 16 * DIM + 2 * p;
+                ml[0] = m, ml[1] = total;
+            }
         } else {
             const int ro = tile * 16 + rr, io = ro / a.group;
             if (io < a.q_len)
@@ -349,63 +427,100 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void kv4_attention
                     (T)(total == 0.f ? 0.f : acc / total);
         }
     }
+    left -= take;
+    if (left == 0) return;
+    opening = false;
+    blk = 0;                                                // the unit is done: the share goes on with the next one
+    if (++unit == a.units) {
+        unit = 0;
+        if (++b == a.batch) return;
+    }
+    __syncthreads();
+    }
 }
 
-// Joins the parts of split sequences: one block per query row and head.
-template <int TYPE, int DIM> __global__ __launch_bounds__(DIM) void kv4_join_kernel(DecodeArgs a) {
+// Joins the parts of units that several workgroups shared: one workgroup per query row and head; groups of DIM / 4
+// threads take the parts in turn.
+template <int TYPE, int DIM> __global__ __launch_bounds__(256) void kv4_join_kernel(DecodeArgs a) {
     typedef typename Half<TYPE>::type T;
-    const int d = threadIdx.x, h = blockIdx.x % a.heads;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    constexpr int kCols = DIM / 4, kTeams = 256 / kCols;
+    __shared__ f32x4 acc_s[kTeams][kCols];
+    __shared__ float m_s[kTeams], total_s[kTeams];
+    const int h = blockIdx.x % a.heads;
     const int64_t token = blockIdx.x / a.heads;
     const int b = (int)(token / a.q_len), i = (int)(token % a.q_len);
     const int row = i * a.group + h % a.group;
-    const int unit = (b * a.kv_heads + h / a.group) * a.tiles + row / 16;
-    const int len = min(max(a.lens[b], 0), a.room);
-    int parts = (len + a.chunk - 1) / a.chunk;
-    parts = parts < 1 ? 1 : parts;
-    const int64_t step = (int64_t)a.units * 16 * (DIM + 2);
-    const float* p = a.part + ((int64_t)unit * 16 + row % 16) * (DIM + 2);
-    float m = kNever, total = 0.f, acc = 0.f;
-    for (int s = 0; s < parts; ++s) m = __builtin_fmaxf(m, p[s * step + DIM]);
-    const float base = m == kNever ? 0.f : m;
-    for (int s = 0; s < parts; ++s) {
-        const float f = __builtin_amdgcn_exp2f(p[s * step + DIM] - base);
-        total += f * p[s * step + DIM + 1];
-        acc += f * p[s * step + d];
+    const int unit = h / a.group * a.tiles + row / 16;
+    const Place p = find(a, b, [](int64_t) { return (int64_t)-1; });
+    const int n = blocks(length(a, b));
+    const int64_t from = p.before * a.units + (int64_t)unit * n;        // the unit's blocks in the row
+    const int64_t w0 = from / p.share, w1 = (from + n - 1) / p.share;    // and the workgroups that have them
+    if (w0 == w1) return;
+    const int team = threadIdx.x / kCols, col = threadIdx.x % kCols;
+    const float* ml = a.part + (int64_t)2 * a.groups * 16 * DIM;
+    float m = kNever, total = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    if (team < kTeams)
+        for (int64_t w = w0 + team; w <= w1; w += kTeams) {
+            // in all workgroups but the first the unit opens the share; in the first only if it begins there
+            const int64_t at = (2 * w + (w == w0 && from > w0 * p.share ? 1 : 0)) * 16 + row % 16;
+            const float mw = ml[2 * at], tw = ml[2 * at + 1];
+            const f32x4 x = *(const f32x4*)(a.part + at * DIM + 4 * col);
+            const float to = __builtin_fmaxf(m, mw), base = to == kNever ? 0.f : to;
+            const float f = __builtin_amdgcn_exp2f(m - base), fw = __builtin_amdgcn_exp2f(mw - base);
+            total = total * f + tw * fw;
+            acc = acc * f + x * fw;
+            m = to;
+        }
+    if (team < kTeams) {
+        acc_s[team][col] = acc;
+        if (col == 0) m_s[team] = m, total_s[team] = total;
     }
-    ((T*)a.out)[(token * a.heads + h) * DIM + d] = (T)(total == 0.f ? 0.f : acc / total);
+    __syncthreads();
+    if (threadIdx.x >= kCols) return;
+    float top = kNever;
+#pragma unroll
+    for (int t = 0; t < kTeams; ++t) top = __builtin_fmaxf(top, m_s[t]);
+    const float base = top == kNever ? 0.f : top;
+    total = 0.f;
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < kTeams; ++t) {
+        const float f = __builtin_amdgcn_exp2f(m_s[t] - base);
+        total += f * total_s[t];
+        acc += f * acc_s[t][threadIdx.x];
+    }
+    const T4 y = total == 0.f ? T4{} : T4{(T)(acc[0] / total), (T)(acc[1] / total), (T)(acc[2] / total), (T)(acc[3] / total)};
+    *(T4*)((T*)a.out + (token * a.heads + h) * DIM + 4 * threadIdx.x) = y;
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 struct Cut {
-    int64_t tiles, units, chunk, splits;
-    size_t bytes(int dim) const { return splits > 1 ? (size_t)(splits * units * 16 * (dim + 2) * 4) : 0; }
+    int64_t tiles, units, groups;
+    bool split;
+    size_t bytes;
 };
 
-// Parts of a sequence: enough workgroups for four on each compute unit when
-// every sequence fills its table, no part under 256 tokens.
-Cut cut(int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int dim, int64_t room, size_t have) {
+// A call's workgroups.  Sequences are split where that spares a workgroup more than three blocks of tokens: the join
+// is a launch of its own (777 tokens of two heads: 8 us in one launch, 10 us in two).
+Cut cut(int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int dim, int64_t room) {
     Cut c;
     c.tiles = (q_len * (heads / kv_heads) + 15) / 16;
-    c.units = batch * kv_heads * c.tiles;
-    const int64_t want = 1024;
-    c.chunk = std::max<int64_t>(256, (room * c.units / want + 255) / 256 * 256);
-    c.splits = std::max<int64_t>(1, (room + c.chunk - 1) / c.chunk);
-    if (c.bytes(dim) > have) {
-        const int64_t fit = (int64_t)(have / (size_t)(c.units * 16 * (dim + 2) * 4));
-        c.splits = std::max<int64_t>(1, fit);
-        c.chunk = std::max<int64_t>(256, ((room + c.splits - 1) / c.splits + 255) / 256 * 256);
-        c.splits = std::max<int64_t>(1, (room + c.chunk - 1) / c.chunk);
-    }
+    c.units = kv_heads * c.tiles;
+    const int64_t blocks = std::max<int64_t>(1, (room + kBlock - 1) / kBlock), all = batch * c.units * blocks;
+    c.groups = std::min<int64_t>(all, dim <= 128 ? kGroups : kGroups * 2 / 3);
+    c.split = blocks - (all + c.groups - 1) / c.groups > 3;
+    c.bytes = c.split ? (size_t)(2 * c.groups * 16 * (dim + 2) * 4) : 0;
     return c;
 }
 
 template <int TYPE, int DIM> wino_status launch(const DecodeArgs& a, int64_t rows, hipStream_t stream) {
-    hipLaunchKernelGGL((kv4_attention_kernel<TYPE, DIM>), dim3((unsigned)((int64_t)a.units * a.splits)), dim3(64 * kWaves), 0,
-                       stream, a);
+    hipLaunchKernelGGL((kv4_attention_kernel<TYPE, DIM>), dim3((unsigned)a.groups), dim3(64 * kWaves), 0, stream, a);
     if (hipGetLastError() != hipSuccess) return WINO_EHIP;
     if (!a.part) return WINO_OK;
-    hipLaunchKernelGGL((kv4_join_kernel<TYPE, DIM>), dim3((unsigned)rows), dim3(DIM), 0, stream, a);
+    hipLaunchKernelGGL((kv4_join_kernel<TYPE, DIM>), dim3((unsigned)rows), dim3(256), 0, stream, a);
     return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
 }
 
@@ -425,7 +540,7 @@ extern "C" size_t kv4_attention_workspace_bytes(int32_t batch, int32_t q_len, in
                                                 int32_t head_dim, int32_t max_pages, int32_t page_size) {
     if (batch < 1 || q_len < 1 || heads < 1 || kv_heads < 1 || head_dim < 1 || max_pages < 1 || page_size < 1) return 0;
     if (heads % kv_heads || (int64_t)batch * q_len * heads > 0x7fffffffll) return 0;
-    return cut(batch, q_len, heads, kv_heads, head_dim, (int64_t)max_pages * page_size, (size_t)-1).bytes(head_dim);
+    return cut(batch, q_len, heads, kv_heads, head_dim, (int64_t)max_pages * page_size).bytes;
 }
 
 extern "C" wino_status kv4_attention(const void* q, int64_t q_stride, const kv4_cache* cache,
@@ -453,13 +568,14 @@ extern "C" wino_status kv4_attention(const void* q, int64_t q_stride, const kv4_
     const int64_t rows = (int64_t)batch * q_len * heads;
     if (rows > 0x7fffffffll) return WINO_EUNSUPPORTED;
     const int64_t room = std::min<int64_t>((int64_t)max_pages * c.page_size, 0x7fffffff - 4096);
-    const Cut k = cut(batch, q_len, heads, c.kv_heads, c.head_dim, room, workspace ? workspace_bytes : 0);
-    if (k.units * k.splits > 0x7fffffffll) return WINO_EUNSUPPORTED;
+    const Cut k = cut(batch, q_len, heads, c.kv_heads, c.head_dim, room);
+    if (batch * k.units > 0x7fffffffll) return WINO_EUNSUPPORTED;
+    const bool split = k.split && workspace && workspace_bytes >= k.bytes;
     DecodeArgs a = {q, out, c.k_codes, c.k_scales, c.v_codes, c.v_scales, block_table, lens,
-                    k.splits > 1 ? (float*)workspace : nullptr, q_stride, c.pages, q_len, heads, c.kv_heads,
-                    heads / c.kv_heads, c.page_size, max_pages, (int32_t)k.tiles, (int32_t)k.units, (int32_t)k.splits,
-                    (int32_t)std::min<int64_t>(k.chunk, 0x7fffffff - 4096), (int32_t)room, winof4::make_fastdiv((uint32_t)c.page_size),
-                    scale * 1.44269504088896340736f};
+                    split ? (float*)workspace : nullptr, q_stride, c.pages, q_len, heads, c.kv_heads,
+                    heads / c.kv_heads, c.page_size, max_pages, (int32_t)k.tiles, batch, (int32_t)k.units,
+                    (int32_t)(split ? k.groups : batch * k.units), (int32_t)room,
+                    winof4::make_fastdiv((uint32_t)c.page_size), scale * 1.44269504088896340736f};
     return type == WINO_BF16 ? launch_dim<WINO_BF16>(c.head_dim, a, rows, stream)
                              : launch_dim<WINO_FP16>(c.head_dim, a, rows, stream);
 }
