@@ -62,7 +62,7 @@ template <int DIM> struct Shape {
     static constexpr int kRow = DIM * 2 + 32;               // bytes of a token's V in LDS: 8 rows cover all banks once
     static constexpr int kScales = DIM == 64 || DIM == 128 ? 1 : 2;   // scales in a lane's quarter
     static constexpr int kStage = 32 * kRow;                // a wave's V in LDS, 32 tokens at a time
-    static constexpr int kJoin = 16 * (DIM + 2) * 4;        // a wave's results in LDS
+    static constexpr int kJoin = 16 * (DIM + 4) * 4;        // a wave's results in LDS: sums, reference, total
     static constexpr int kLds = kWaves * (kStage > kJoin ? kStage : kJoin);
 };
 
@@ -113,8 +113,10 @@ template <int DIM> __device__ inline float piece_scale(const uint32_t (&s)[Shape
 // The work of a call is the blocks of 256 tokens of all units in a row: sequence by sequence, its units one after the
 // other, the blocks of a unit in order.  Each workgroup takes an equal share of the row, so long and short sequences
 // keep all of them busy alike; units that it holds whole go straight to the output, the two at its ends may be parts.
+// What a unit costs beside its tokens (its queries, the wait for its first codes, the join of the waves) counts as a
+// block too: block 0 of each unit holds no tokens.
 __device__ inline int length(const DecodeArgs& a, int b) { return min(max(a.lens[b], 0), a.room); }
-__device__ inline int blocks(int len) { return max(1, (len + kBlock - 1) / kBlock); }
+__device__ inline int blocks(int len) { return 1 + (len + kBlock - 1) / kBlock; }
 
 struct Place {
     int64_t share, before;      // blocks of a workgroup; blocks of all units of the sequences before b
@@ -195,8 +197,8 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 3 : 2) void kv4_attention
     const bool is_part = take < n_blocks;
     const int tile = unit % a.tiles, kvh = unit / a.tiles;
     const int first_end = len - a.q_len + 1;                // tokens that query 0 sees; every row sees those
-    const int begin = blk * kBlock;
-    const int end = a.pages == 0 ? begin : (len - begin < take * kBlock ? len : begin + take * kBlock);
+    const int begin = max(blk - 1, 0) * kBlock;
+    const int end = a.pages == 0 ? begin : min((int64_t)len, (int64_t)(blk + take - 1) * kBlock);
 
     // this lane's row: query i, head h
     const int row = tile * 16 + r;
@@ -370,15 +372,23 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 3 : 2) void kv4_attention
             // lane l of 16 gives the address of four dimensions of token l / 4 and gets dimension l of four tokens
             const uint8_t* from = stage + (4 * g + (r >> 2)) * S::kRow + (r & 3) * 8;
 #pragma unroll
-            for (int n = 0; n < DIM / 16; ++n) {
+            for (int n = 0; n < DIM / 16; n += 2) {         // two at a time: no product waits for the one before it
                 typedef __attribute__((ext_vector_type(4))) short s4;
                 typedef __attribute__((address_space(3))) s4* lds4;
-                const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(from + 32 * n)));
-                const u32x2 y = __builtin_bit_cast(
-                    u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(from + 16 * S::kRow + 32 * n)));
-                const bf16x8 v = __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]});
-                o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, ph), o[n], 0, 0, 0);
-                o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, pl), o[n], 0, 0, 0);
+                bf16x8 v[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint8_t* f = from + 32 * (n + k);
+                    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)f));
+                    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(f + 16 * S::kRow)));
+                    v[k] = __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]});
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    o[n + k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[k], __builtin_bit_cast(bf16x8, ph), o[n + k], 0, 0, 0);
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    o[n + k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[k], __builtin_bit_cast(bf16x8, pl), o[n + k], 0, 0, 0);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
@@ -387,44 +397,47 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 3 : 2) void kv4_attention
     }
     sum = sum_rows(sum);
 
-    // join the waves: [wave][row][dim + 2]
+    // join the waves: [wave][row][dim + 4]
+    const int rows = min(16, a.q_len * a.group - tile * 16);
+    constexpr int kRowJ = DIM + 4;
     __syncthreads();
-    float* mine = (float*)lds + (wave * 16 + r) * (DIM + 2);
+    if (r < rows) {
+        float* mine = (float*)lds + (wave * 16 + r) * kRowJ;
 #pragma unroll
-    for (int n = 0; n < DIM / 16; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) mine[16 * n + 4 * g + e] = o[n][e];
-    if (g == 0) {
-        mine[DIM] = ref;
-        mine[DIM + 1] = sum;
+        for (int n = 0; n < DIM / 16; ++n) *(f32x4*)(mine + 16 * n + 4 * g) = o[n];
+        if (g == 0) {
+            mine[DIM] = ref;
+            mine[DIM + 1] = sum;
+        }
     }
     __syncthreads();
-    for (int x = threadIdx.x; x < 16 * DIM; x += 64 * kWaves) {
-        const int rr = x / DIM, d = x % DIM;
-        const float* w = (const float*)lds + rr * (DIM + 2);
+    for (int x = threadIdx.x; x < rows * (DIM / 4); x += 64 * kWaves) {
+        const int rr = x / (DIM / 4), d = x % (DIM / 4) * 4;
+        const float* w = (const float*)lds + rr * kRowJ;
         float m = kNever;
 #pragma unroll
-        for (int k = 0; k < kWaves; ++k) m = __builtin_fmaxf(m, w[k * 16 * (DIM + 2) + DIM]);
+        for (int k = 0; k < kWaves; ++k) m = __builtin_fmaxf(m, w[k * 16 * kRowJ + DIM]);
         const float base = m == kNever ? 0.f : m;
-        float total = 0.f, acc = 0.f;
+        float total = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < kWaves; ++k) {
-            const float f = __builtin_amdgcn_exp2f(w[k * 16 * (DIM + 2) + DIM] - base);
-            total += f * w[k * 16 * (DIM + 2) + DIM + 1];
-            acc += f * w[k * 16 * (DIM + 2) + d];
+            const float f = __builtin_amdgcn_exp2f(w[k * 16 * kRowJ + DIM] - base);
+            total += f * w[k * 16 * kRowJ + DIM + 1];
+            acc += f * *(const f32x4*)(w + k * 16 * kRowJ + d);
         }
         if (is_part) {
             const int64_t p = ((int64_t)2 * blockIdx.x + (opening ? 0 : 1)) * 16 + rr;
-            a.part[p * DIM + d] = acc;
+            *(f32x4*)(a.part + p * DIM + d) = acc;
             if (d == 0) {
                 float* ml = a.part + (int64_t)2 * a.groups * 16 * DIM + 2 * p;
                 ml[0] = m, ml[1] = total;
             }
         } else {
-            const int ro = tile * 16 + rr, io = ro / a.group;
-            if (io < a.q_len)
-                ((T*)a.out)[(((int64_t)b * a.q_len + io) * a.heads + kvh * a.group + ro % a.group) * DIM + d] =
-                    (T)(total == 0.f ? 0.f : acc / total);
+            typedef T T4 __attribute__((ext_vector_type(4)));
+            const int ro = tile * 16 + rr;
+            const T4 y = total == 0.f ? T4{} : T4{(T)(acc[0] / total), (T)(acc[1] / total), (T)(acc[2] / total), (T)(acc[3] / total)};
+            *(T4*)((T*)a.out + (((int64_t)b * a.q_len + ro / a.group) * a.heads + kvh * a.group + ro % a.group) * DIM + d) = y;
         }
     }
     left -= take;
@@ -462,15 +475,30 @@ template <int TYPE, int DIM> __global__ __launch_bounds__(256) void kv4_join_ker
     float m = kNever, total = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     if (team < kTeams)
-        for (int64_t w = w0 + team; w <= w1; w += kTeams) {
-            // in all workgroups but the first the unit opens the share; in the first only if it begins there
-            const int64_t at = (2 * w + (w == w0 && from > w0 * p.share ? 1 : 0)) * 16 + row % 16;
-            const float mw = ml[2 * at], tw = ml[2 * at + 1];
-            const f32x4 x = *(const f32x4*)(a.part + at * DIM + 4 * col);
-            const float to = __builtin_fmaxf(m, mw), base = to == kNever ? 0.f : to;
-            const float f = __builtin_amdgcn_exp2f(m - base), fw = __builtin_amdgcn_exp2f(mw - base);
-            total = total * f + tw * fw;
-            acc = acc * f + x * fw;
+        for (int64_t w = w0 + team; w <= w1; w += 4 * kTeams) {
+            float mw[4], tw[4];
+            f32x4 x[4];
+            float to = m;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                // in all workgroups but the first the unit opens the share; in the first only if it begins there
+                const int64_t v = w + k * kTeams <= w1 ? w + k * kTeams : w;
+                const int64_t at = (2 * v + (v == w0 && from > w0 * p.share ? 1 : 0)) * 16 + row % 16;
+                mw[k] = w + k * kTeams <= w1 ? ml[2 * at] : kNever, tw[k] = ml[2 * at + 1];
+                x[k] = *(const f32x4*)(a.part + at * DIM + 4 * col);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) to = __builtin_fmaxf(to, mw[k]);
+            const float base = to == kNever ? 0.f : to, f = __builtin_amdgcn_exp2f(m - base);
+            total *= f;
+            acc *= f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (mw[k] == kNever) continue;              // also what stands in for a part that is not there
+                const float fw = __builtin_amdgcn_exp2f(mw[k] - base);
+                total += tw[k] * fw;
+                acc += x[k] * fw;
+            }
             m = to;
         }
     if (team < kTeams) {
