@@ -39,7 +39,7 @@ struct DecodeArgs {
     const uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
     const int32_t *table, *lens;
     float* part;            // [2 * workgroups][16][dim] sums of parts, then [2 * workgroups][16][2] their references and
-                            // totals; null: a workgroup takes a whole sequence
+                            // totals, then [batch * units] where a unit's parts are; null: a workgroup takes a whole unit
     int64_t q_stride, pages;
     int32_t q_len, heads, kv_heads, group, page, max_pages;
     int32_t tiles;          // 16-row tiles of a sequence's rows at one cache head
@@ -122,47 +122,46 @@ struct Place {
     int64_t share, before;      // blocks of a workgroup; blocks of all units of the sequences before b
     int b;
 };
-// The share of a workgroup, and the sequence that block `at(share)` of the row belongs to (or that sequence `want`
-// begins with, where at is below 0).
-template <class AT> __device__ inline Place find(const DecodeArgs& a, int want, AT at) {
+// The share of workgroup w, and the sequence that it begins in (batch: it has none).
+__device__ inline Place find(const DecodeArgs& a, int w) {
     const int lane = threadIdx.x & 63;
-    int64_t total = 0;
-    int n = 0, first = 0;                                   // blocks of this lane's sequence, and of the 64 up to it
-    for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    int n = 0, upto = 0;                                    // blocks of this lane's sequence, and of the 64 up to it
+    auto scan = [&](int b0) {
         n = b0 + lane < a.batch ? blocks(length(a, b0 + lane)) : 0;
-        first = n;
+        upto = n;
         for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(first, o);
-            if (lane >= o) first += x;
+            const int x = __shfl_up(upto, o);
+            if (lane >= o) upto += x;
         }
-        total += __shfl(first, 63);
-    }
+        return __shfl(upto, 63);
+    };
+    int64_t total = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 64) total += scan(b0);
     Place p;
     p.share = (total * a.units + a.groups - 1) / a.groups;
     p.b = a.batch;
     p.before = 0;
-    int64_t f = at(p.share);
+    const int64_t first = p.share * w;
     for (int b0 = 0; b0 < a.batch; b0 += 64) {
-        if (a.batch > 64) {
-            n = b0 + lane < a.batch ? blocks(length(a, b0 + lane)) : 0;
-            first = n;
-            for (int o = 1; o < 64; o <<= 1) {
-                const int x = __shfl_up(first, o);
-                if (lane >= o) first += x;
-            }
-        }
-        const int all = __shfl(first, 63);
-        const uint64_t hit = f >= 0 ? __ballot(f < (p.before + first) * a.units) : (want < b0 + 64 ? 1ull << (want - b0) : 0);
-        if (hit) {
-            const int l = __builtin_ctzll(hit);
+        const int all = a.batch > 64 ? scan(b0) : (int)total;
+        const uint64_t past = __ballot(first < (p.before + upto) * a.units);
+        if (past) {
+            const int l = __builtin_ctzll(past);
             p.b = __builtin_amdgcn_readfirstlane(b0 + l);
-            p.before += __builtin_amdgcn_readfirstlane(__shfl(first - n, l));
+            p.before += __builtin_amdgcn_readfirstlane(__shfl(upto - n, l));
             break;
         }
         p.before += all;
     }
     return p;
 }
+
+// Where the parts of a unit are: workgroups first .. last; the first one's is its second part where `second`.
+struct Parts {
+    int32_t first, last, second, pad;
+};
+__device__ inline float* part_ml(const DecodeArgs& a, int dim) { return a.part + (int64_t)2 * a.groups * 16 * dim; }
+__device__ inline Parts* unit_parts(const DecodeArgs& a, int dim) { return (Parts*)(part_ml(a, dim) + (int64_t)2 * a.groups * 16 * 2); }
 
 template <int TYPE, int DIM>
 __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 3 : 2) void kv4_attention_kernel(DecodeArgs a) {
@@ -174,16 +173,16 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 3 : 2) void kv4_attention
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
 
-    int b, unit, blk, left;                                 // left: blocks of the share still to do
+    int b, unit, blk, left, share = 0;                      // left: blocks of the share still to do
     if (a.part) {
-        const Place p = find(a, 0, [&](int64_t share) { return share * blockIdx.x; });
+        const Place p = find(a, blockIdx.x);
         if (p.b >= a.batch) return;
         b = p.b;
         const int n = __builtin_amdgcn_readfirstlane(blocks(length(a, b)));
         const int64_t in = p.share * blockIdx.x - p.before * a.units;
         unit = __builtin_amdgcn_readfirstlane((int)(in / n));
         blk = __builtin_amdgcn_readfirstlane((int)(in - (int64_t)unit * n));
-        left = __builtin_amdgcn_readfirstlane((int)p.share);
+        share = left = __builtin_amdgcn_readfirstlane((int)p.share);
     } else {
         b = blockIdx.x / a.units;
         unit = blockIdx.x % a.units;
@@ -195,6 +194,9 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 3 : 2) void kv4_attention
     const int len = __builtin_amdgcn_readfirstlane(length(a, b)), n_blocks = blocks(len);
     const int take = min(left, n_blocks - blk);
     const bool is_part = take < n_blocks;
+    if (a.part && blk == 0 && threadIdx.x == 0)
+        unit_parts(a, DIM)[(int64_t)b * a.units + unit] =
+            Parts{(int)blockIdx.x, (int)blockIdx.x + (n_blocks - take + share - 1) / share, opening ? 0 : 1, 0};
     const int tile = unit % a.tiles, kvh = unit / a.tiles;
     const int first_end = len - a.q_len + 1;                // tokens that query 0 sees; every row sees those
     const int begin = max(blk - 1, 0) * kBlock;
@@ -430,7 +432,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 3 : 2) void kv4_attention
             const int64_t p = ((int64_t)2 * blockIdx.x + (opening ? 0 : 1)) * 16 + rr;
             *(f32x4*)(a.part + p * DIM + d) = acc;
             if (d == 0) {
-                float* ml = a.part + (int64_t)2 * a.groups * 16 * DIM + 2 * p;
+                float* ml = part_ml(a, DIM) + 2 * p;
                 ml[0] = m, ml[1] = total;
             }
         } else {
@@ -465,25 +467,22 @@ template <int TYPE, int DIM> __global__ __launch_bounds__(256) void kv4_join_ker
     const int b = (int)(token / a.q_len), i = (int)(token % a.q_len);
     const int row = i * a.group + h % a.group;
     const int unit = h / a.group * a.tiles + row / 16;
-    const Place p = find(a, b, [](int64_t) { return (int64_t)-1; });
-    const int n = blocks(length(a, b));
-    const int64_t from = p.before * a.units + (int64_t)unit * n;        // the unit's blocks in the row
-    const int64_t w0 = from / p.share, w1 = (from + n - 1) / p.share;    // and the workgroups that have them
-    if (w0 == w1) return;
+    const Parts p = unit_parts(a, DIM)[(int64_t)b * a.units + unit];
+    const int w0 = p.first, w1 = p.last;
+    if (w0 == w1) return;                                   // whole, and in the output already
     const int team = threadIdx.x / kCols, col = threadIdx.x % kCols;
-    const float* ml = a.part + (int64_t)2 * a.groups * 16 * DIM;
+    const float* ml = part_ml(a, DIM);
     float m = kNever, total = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     if (team < kTeams)
-        for (int64_t w = w0 + team; w <= w1; w += 4 * kTeams) {
+        for (int w = w0 + team; w <= w1; w += 4 * kTeams) {
             float mw[4], tw[4];
             f32x4 x[4];
             float to = m;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                // in all workgroups but the first the unit opens the share; in the first only if it begins there
-                const int64_t v = w + k * kTeams <= w1 ? w + k * kTeams : w;
-                const int64_t at = (2 * v + (v == w0 && from > w0 * p.share ? 1 : 0)) * 16 + row % 16;
+                const int v = w + k * kTeams <= w1 ? w + k * kTeams : w;
+                const int64_t at = ((int64_t)2 * v + (v == w0 ? p.second : 0)) * 16 + row % 16;
                 mw[k] = w + k * kTeams <= w1 ? ml[2 * at] : kNever, tw[k] = ml[2 * at + 1];
                 x[k] = *(const f32x4*)(a.part + at * DIM + 4 * col);
             }
@@ -540,7 +539,7 @@ Cut cut(int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int dim, 
     const int64_t blocks = std::max<int64_t>(1, (room + kBlock - 1) / kBlock), all = batch * c.units * blocks;
     c.groups = std::min<int64_t>(all, dim <= 128 ? kGroups : kGroups * 2 / 3);
     c.split = blocks - (all + c.groups - 1) / c.groups > 3;
-    c.bytes = c.split ? (size_t)(2 * c.groups * 16 * (dim + 2) * 4) : 0;
+    c.bytes = c.split ? (size_t)(2 * c.groups * 16 * (dim + 2) * 4 + batch * c.units * sizeof(Parts)) : 0;
     return c;
 }
 
