@@ -203,9 +203,10 @@ def _stream(stream):
         import torch
         if _RAW_STREAM is None:
             torch.cuda.current_stream()          # initializes the device state
-            _RAW_STREAM = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
-                lambda device: torch.cuda.current_stream(device).cuda_stream)
-        return _RAW_STREAM(torch.cuda.current_device())
+            raw, device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+            _RAW_STREAM = (lambda: raw(device())) if raw and device else (
+                lambda: torch.cuda.current_stream().cuda_stream)
+        return _RAW_STREAM()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -599,7 +600,7 @@ def _float_type(t, what):
         import torch
         _FLOAT_TYPES = {torch.bfloat16: 0, torch.float16: 1}
     code = _FLOAT_TYPES.get(getattr(t, "dtype", None))
-    if code is None or not t.is_cuda:
+    if code is None:
         raise ValueError(f"{what}: expected a bf16 or fp16 tensor on the GPU")
     return code
 
@@ -607,7 +608,7 @@ def _float_type(t, what):
 def _rows(t, dtype, shape, what):
     """(address, row stride) of a GPU tensor of `shape` whose rows (all
     dimensions but the first) are dense; the rows may lie apart."""
-    if not t.is_cuda or t.dtype != dtype or t.shape != shape:
+    if not (t.shape == shape and t.dtype is dtype and t.is_cuda):
         raise ValueError(f"{what}: expected {dtype} {tuple(shape)} on the GPU, got {t.dtype} {tuple(t.shape)} on "
                          f"{t.device}")
     st = t.stride()
@@ -623,10 +624,17 @@ def _rows(t, dtype, shape, what):
 
 def _dense(t, dtype, shape, what):
     """Address of a dense GPU tensor of `shape`."""
-    if t.is_cuda and t.dtype == dtype and t.shape == shape and t.is_contiguous():
+    if t.shape == shape and t.dtype is dtype and t.is_cuda and t.is_contiguous():
         return t.data_ptr()
     raise ValueError(f"{what}: expected dense {dtype} {tuple(shape)} on the GPU, got {t.dtype} {tuple(t.shape)} on "
                      f"{t.device}")
+
+
+def _scratch(t):
+    """(address, bytes) of a workspace: any dense GPU tensor, or None."""
+    if t is None:
+        return None, 0
+    return _dptr(t, None, 0, "workspace"), t.numel() * t.element_size()
 
 
 def _cache_struct(cache):
@@ -669,8 +677,9 @@ def w4_matvec(x, codes, scales, y, bias=None, workspace=None, stream=None):
     st = lib.w4_matvec(xp, xs, _dense(codes, torch.uint8, (n, k // 2), "codes"),
                        _dense(scales, torch.uint8, (n, k // 32), "scales"),
                        None if bias is None else _dense(bias, x.dtype, (n,), "bias"), yp, ys, m, n, k, kind,
-                       _dptr(workspace, None, 0, "workspace"), _nbytes(workspace), _stream(stream))
-    _check(st, "w4_matvec")
+                       *_scratch(workspace), _stream(stream))
+    if st:
+        _check(st, "w4_matvec")
 
 
 def kv4_append(q, k, v, cos_sin, positions, slots, cache, q_out=None, k_out=None, v_out=None, rotary=ROTARY_HALVES,
@@ -724,8 +733,9 @@ def kv4_attention(q, cache, block_table, lens, out, scale, workspace=None, strea
     st = lib.kv4_attention(qp, qs, ctypes.byref(c), _dense(block_table, torch.int32, (batch, max_pages), "block_table"),
                            max_pages, _dense(lens, torch.int32, (batch,), "lens"),
                            _dense(out, q.dtype, (rows, hq, d), "out"), batch, rows // batch if batch else 0, hq, scale,
-                           kind, _dptr(workspace, None, 0, "workspace"), _nbytes(workspace), _stream(stream))
-    _check(st, "kv4_attention")
+                           kind, *_scratch(workspace), _stream(stream))
+    if st:
+        _check(st, "kv4_attention")
 
 
 def prompt_attention(q, k, v, cu_q, cu_k, max_q, out, scale, causal=True, stream=None):

@@ -29,7 +29,7 @@ namespace {
 using namespace mx4;
 using winof4::FastDiv;
 
-constexpr int kWaves = 4, kBlock = 256;     // tokens of a workgroup's step
+constexpr int kBlock = 256;                 // tokens that the work is shared out in
 constexpr int kGroups = 768;                // workgroups that fit on the device at once (heads up to 128)
 constexpr float kNever = -__builtin_inff();
 
@@ -55,7 +55,7 @@ __device__ inline int fast_div(int n, FastDiv f) {
     return f.d == 1 ? n : (int)((uint32_t)(((uint64_t)(uint32_t)n * f.mul) >> 32) >> f.shr);
 }
 
-template <int DIM> struct Shape {
+template <int DIM, int WAVES = 4> struct Shape {
     static constexpr int kSteps = DIM / 32;                 // products of 32 dimensions
     static constexpr int kTok = DIM <= 128 ? 64 : 32;       // tokens of a wave's step
     static constexpr int kTiles = kTok / 16;
@@ -63,7 +63,7 @@ template <int DIM> struct Shape {
     static constexpr int kScales = DIM == 64 || DIM == 128 ? 1 : 2;   // scales in a lane's quarter
     static constexpr int kStage = 32 * kRow;                // a wave's V in LDS, 32 tokens at a time
     static constexpr int kJoin = 16 * (DIM + 4) * 4;        // a wave's results in LDS: sums, reference, total
-    static constexpr int kLds = kWaves * (kStage > kJoin ? kStage : kJoin);
+    static constexpr int kLds = WAVES * (kStage > kJoin ? kStage : kJoin);
 };
 
 // One step's codes and scales: lane (t, g) has quarter g of token t of each tile.
@@ -163,10 +163,12 @@ struct Parts {
 __device__ inline float* part_ml(const DecodeArgs& a, int dim) { return a.part + (int64_t)2 * a.groups * 16 * dim; }
 __device__ inline Parts* unit_parts(const DecodeArgs& a, int dim) { return (Parts*)(part_ml(a, dim) + (int64_t)2 * a.groups * 16 * 2); }
 
-template <int TYPE, int DIM>
-__global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 3 : 2) void kv4_attention_kernel(DecodeArgs a) {
+// WAVES: 4 where the work is shared out (three workgroups a compute unit), 8 where a workgroup takes one unit, which is
+// short then.
+template <int TYPE, int DIM, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void kv4_attention_kernel(DecodeArgs a) {
     typedef typename Half<TYPE>::type T;
-    typedef Shape<DIM> S;
+    typedef Shape<DIM, WAVES> S;
     typedef T T8 __attribute__((ext_vector_type(8)));
     constexpr int kParts = TYPE == WINO_FP16 ? 2 : 1;       // bf16 numbers of a query element
     __shared__ __attribute__((aligned(16))) uint8_t lds[S::kLds];
@@ -241,7 +243,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 3 : 2) void kv4_attention
     const int w0 = begin + wave * S::kTok;                  // the wave's first token
     uint64_t slot = 0, there = 0;
     auto list = [&](int step) {
-        const int t = w0 + (step + lane / S::kTiles) * (kWaves * S::kTok) + 16 * (lane % S::kTiles);
+        const int t = w0 + (step + lane / S::kTiles) * (WAVES * S::kTok) + 16 * (lane % S::kTiles);
         int64_t id = -1;
         int pg = 0;
         if (t < end) {
@@ -273,8 +275,8 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 3 : 2) void kv4_attention
         load_codes<DIM>(kc, a.k_codes, a.k_scales, at, lane);
         load_codes<DIM>(vc, a.v_codes, a.v_scales, at, lane);
     }
-    for (; t0 < end; t0 += kWaves * S::kTok) {
-        const bool more = t0 + kWaves * S::kTok < end;
+    for (; t0 < end; t0 += WAVES * S::kTok) {
+        const bool more = t0 + WAVES * S::kTok < end;
         // scores, transposed: lane has tokens 16 n + 4 g + e of row r
         f32x4 z[S::kTiles];
 #pragma unroll
@@ -413,17 +415,17 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 3 : 2) void kv4_attention
         }
     }
     __syncthreads();
-    for (int x = threadIdx.x; x < rows * (DIM / 4); x += 64 * kWaves) {
+    for (int x = threadIdx.x; x < rows * (DIM / 4); x += 64 * WAVES) {
         const int rr = x / (DIM / 4), d = x % (DIM / 4) * 4;
         const float* w = (const float*)lds + rr * kRowJ;
         float m = kNever;
 #pragma unroll
-        for (int k = 0; k < kWaves; ++k) m = __builtin_fmaxf(m, w[k * 16 * kRowJ + DIM]);
+        for (int k = 0; k < WAVES; ++k) m = __builtin_fmaxf(m, w[k * 16 * kRowJ + DIM]);
         const float base = m == kNever ? 0.f : m;
         float total = 0.f;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < kWaves; ++k) {
+        for (int k = 0; k < WAVES; ++k) {
             const float f = __builtin_amdgcn_exp2f(w[k * 16 * kRowJ + DIM] - base);
             total += f * w[k * 16 * kRowJ + DIM + 1];
             acc += f * *(const f32x4*)(w + k * 16 * kRowJ + d);
@@ -544,9 +546,13 @@ Cut cut(int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int dim, 
 }
 
 template <int TYPE, int DIM> wino_status launch(const DecodeArgs& a, int64_t rows, hipStream_t stream) {
-    hipLaunchKernelGGL((kv4_attention_kernel<TYPE, DIM>), dim3((unsigned)a.groups), dim3(64 * kWaves), 0, stream, a);
+    const dim3 grid((unsigned)a.groups);
+    if (!a.part) {
+        hipLaunchKernelGGL((kv4_attention_kernel<TYPE, DIM, 8>), grid, dim3(512), 0, stream, a);
+        return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
+    }
+    hipLaunchKernelGGL((kv4_attention_kernel<TYPE, DIM, 4>), grid, dim3(256), 0, stream, a);
     if (hipGetLastError() != hipSuccess) return WINO_EHIP;
-    if (!a.part) return WINO_OK;
     hipLaunchKernelGGL((kv4_join_kernel<TYPE, DIM>), dim3((unsigned)rows), dim3(256), 0, stream, a);
     return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
 }
