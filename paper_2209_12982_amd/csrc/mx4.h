@@ -92,6 +92,13 @@ template <int ROWS> __device__ inline f32x2 swap_rows(float x) {
     const uint32_t u = s[0], v = s[1];      // scalars: a bit cast of a vector's element reads element 0
     return f32x2{__builtin_bit_cast(float, u), __builtin_bit_cast(float, v)};
 }
+// The largest of three; the compiler's own maximum first quiets operands that
+// it does not know to be numbers, an instruction each.  A NaN loses.
+__device__ inline float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
 // Maximum and sum over the four 16-lane rows of a wave, lane by lane.
 __device__ inline float max_rows(float x) {
     const f32x2 a = swap_rows<2>(x);

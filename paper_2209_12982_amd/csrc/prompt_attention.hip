@@ -25,7 +25,8 @@ struct PromptArgs {
     const int32_t *cu_q, *cu_k;
     int64_t q_stride, k_stride, v_stride;
     int32_t seqs, total_q, total_k, heads, kv_heads, causal;
-    float scale_log2;       // scale * log2(e): probabilities are powers of two
+    float scale_log2;       // |scale| * log2(e), 1 for a scale of 0: probabilities are powers of two
+    uint32_t q_and, q_xor;  // the scale's sign, or its being 0, put into pairs of query elements
 };
 
 template <int DIM> struct Shape {
@@ -41,11 +42,17 @@ template <int TYPE> struct Mfma;
 template <> struct Mfma<WINO_BF16> {
     typedef bf16x8 T8;
     typedef bf16x2 T2;
+    static __device__ float pair_sum(T2 p, float c) {
+        return __builtin_amdgcn_fdot2_f32_bf16(p, T2{(__bf16)1.f, (__bf16)1.f}, c, false);
+    }
     static __device__ f32x16 mul(T8 a, T8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 template <> struct Mfma<WINO_FP16> {
     typedef f16x8 T8;
     typedef f16x2 T2;
+    static __device__ float pair_sum(T2 p, float c) {
+        return __builtin_amdgcn_fdot2(p, T2{(_Float16)1.f, (_Float16)1.f}, c, false);
+    }
     static __device__ f32x16 mul(T8 a, T8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
@@ -121,7 +128,10 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
     {
         const T* p = (const T*)a.q + (int64_t)(w.q0 + min(i, w.nq - 1)) * a.q_stride + (int64_t)h * DIM + 8 * half;
 #pragma unroll
-        for (int s = 0; s < DIM / 16; ++s) q[s] = *(const T8*)(p + 16 * s);
+        for (int s = 0; s < DIM / 16; ++s) {
+            const u32x4 x = *(const u32x4*)(p + 16 * s);
+            q[s] = __builtin_bit_cast(T8, (x & a.q_and) ^ a.q_xor);
+        }
     }
     f32x16 o[DIM / 32];                                     // lane: dimensions 32 n + 8 (e / 4) + 4 half + e % 4 of query c
 #pragma unroll
@@ -193,19 +203,17 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if (t0 + 32 * b + 8 * (e / 4) + 4 * half + e % 4 >= row_end) z[b][e] = kNever;
-                    else z[b][e] *= a.scale_log2;
-        } else {
-#pragma unroll
-            for (int b = 0; b < 2; ++b) z[b] *= a.scale_log2;
         }
-        float top = kNever;
+        float top = max3(z[0][0], z[0][1], z[0][2]), top1 = max3(z[1][0], z[1][1], z[1][2]);
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int e = 0; e < 16; e += 2) top = __builtin_fmaxf(__builtin_fmaxf(z[b][e], z[b][e + 1]), top);
+        for (int e = 3; e < 15; e += 2) {
+            top = max3(z[0][e], z[0][e + 1], top);
+            top1 = max3(z[1][e], z[1][e + 1], top1);
+        }
+        top = max3(top, z[0][15], top1);
         {
-            const f32x2 x = swap_rows<2>(top);
-            top = __builtin_fmaxf(x[0], x[1]);
+            const f32x2 x = swap_rows<2>(max3(top, top, z[1][15]));
+            top = max3(x[0], x[1], x[1]) * a.scale_log2;
         }
         // o and sum move to a new reference only where the maximum has outgrown the old one by 2^8
         if (__any(top > ref + 8.f)) {
@@ -216,16 +224,22 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
 #pragma unroll
             for (int n = 0; n < DIM / 32; ++n) o[n] *= alpha;
         }
-        const float base = ref == kNever ? 0.f : ref - kLift;
+        const float base = ref == kNever ? 0.f : kLift - ref;
         uint32_t p[2][8];
+        float sum1 = 0.f;                                   // of the rounded probabilities: they are the weights
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
-                const float p0 = __builtin_amdgcn_exp2f(z[b][e] - base), p1 = __builtin_amdgcn_exp2f(z[b][e + 1] - base);
-                sum += p0 + p1;
-                p[b][e / 2] = __builtin_bit_cast(uint32_t, T2{(T)p0, (T)p1});
+                const T2 x = {(T)__builtin_amdgcn_exp2f(__builtin_fmaf(z[b][e], a.scale_log2, base)),
+                              (T)__builtin_amdgcn_exp2f(__builtin_fmaf(z[b][e + 1], a.scale_log2, base))};
+                if (b == 0)
+                    sum = M::pair_sum(x, sum);
+                else
+                    sum1 = M::pair_sum(x, sum1);
+                p[b][e / 2] = __builtin_bit_cast(uint32_t, x);
             }
+        sum += sum1;
         // lane l of 16 gives the address of four dimensions of key l / 4 and gets dimension l of four keys
         const int l = lane & 15;
         const uint8_t* from = lv + (4 * half + (l >> 2)) * S::kRowV + ((lane >> 4) & 1) * 32 + (l & 3) * 8;
@@ -312,7 +326,9 @@ extern "C" wino_status prompt_attention(const void* q, int64_t q_stride, const v
     const int64_t blocks = ((int64_t)total_q / kRows + seqs) * heads;
     if (blocks > 0x7fffffffll) return WINO_EUNSUPPORTED;
     PromptArgs a = {q, k, v, out, cu_q, cu_k, q_stride, k_stride, v_stride, seqs, total_q, total_k,
-                    heads, kv_heads, causal, scale * 1.44269504088896340736f};
+                    heads, kv_heads, causal, 0.f, scale == 0.f ? 0u : 0xffffffffu, scale < 0.f ? 0x80008000u : 0u};
+    a.scale_log2 = scale == 0.f ? 1.f : __builtin_fabsf(scale) * 1.44269504088896340736f;
+    if (a.scale_log2 - a.scale_log2 != 0.f) return WINO_EUNSUPPORTED;       // past fp32's range
     if (type == WINO_BF16)
         launch<WINO_BF16>(head_dim, dim3((unsigned)blocks), stream, a);
     else
