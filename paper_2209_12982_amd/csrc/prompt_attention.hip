@@ -11,6 +11,7 @@
 #include <hip/hip_runtime.h>
 
 #include "mx4.h"
+#include "wino_device.h"
 #include "winof4.h"
 
 namespace {
@@ -29,14 +30,27 @@ struct PromptArgs {
     uint32_t q_and, q_xor;  // the scale's sign, or its being 0, put into pairs of query elements
 };
 
+// A tile of K or V in LDS: 64 dense rows whose 16-byte pieces are exchanged inside a row, because copies from memory
+// straight to LDS fill it from one end to the other.  The banks are 256 bytes wide.
 template <int DIM> struct Shape {
-    // bytes of a row in LDS: 16 rows of K start in 16 different 16-byte columns of the 256-byte banks, 4 rows of V
-    // in four different 64-byte ones
-    static constexpr int kRowK = DIM * 2 + 16;
-    static constexpr int kRowV = DIM * 2 % 256 == 192 ? DIM * 2 : DIM * 2 + 64;
-    static constexpr int kTileK = kKeys * kRowK, kTileV = kKeys * kRowV;
-    static constexpr int kPieces = kKeys * DIM / 8 / (64 * kWaves);     // 16-byte pieces of a tile for a thread
+    static constexpr int kRow = DIM * 2, kPiecesRow = kRow / 16;
+    static constexpr int kTile = kKeys * kRow;
+    static constexpr int kPieces = kKeys * kPiecesRow / (64 * kWaves);  // of a tile, for a thread
+    // K is read 16 rows at a time, the same piece of each: they have to stand in 16 different columns.  Of a row's
+    // pieces, 2^kBits in a row can be exchanged.
+    static constexpr int kBits = DIM == 96 ? 2 : (DIM == 64 || DIM == 192 ? 3 : 4);
+    static __device__ int swap_k(int row) { return (row >> (4 - kBits)) & ((1 << kBits) - 1); }
+    // V is read four rows at a time, 64 bytes of each: four different quarters of the banks.
+    static __device__ int swap_v(int row) {
+        return DIM == 96 ? 0 : (DIM == 64 || DIM == 192 ? (row >> 1 & 1) << 2 : (row & 3) << 2);
+    }
 };
+
+// 16 bytes a lane from base + off to LDS at dst + 16 lane, which is on its way until vmcnt says otherwise; in assembly
+// for the reason that lds_copy16 gives.
+__device__ inline void copy16(const void* base, uint32_t off, uint32_t dst) {
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(dst) : "memory");
+}
 
 template <int TYPE> struct Mfma;
 template <> struct Mfma<WINO_BF16> {
@@ -80,12 +94,11 @@ __device__ inline bool find(const PromptArgs& a, int index, Work& w) {
         if (index < all) {
             const uint64_t past = __ballot(index < before);
             const int l = __builtin_ctzll(past);
-            w.q0 = __builtin_amdgcn_readfirstlane(__shfl(from, l));
-            w.nq = __builtin_amdgcn_readfirstlane(__shfl(n, l));
-            w.tile = __builtin_amdgcn_readfirstlane(index - __shfl(before - count, l));
-            const int at = s0 + __builtin_amdgcn_readfirstlane(l);
-            w.k0 = max(min(a.cu_k[at], a.total_k), 0);
-            w.nk = max(min(a.cu_k[at + 1], a.total_k) - w.k0, 0);
+            w.q0 = __shfl(from, l);
+            w.nq = __shfl(n, l);
+            w.tile = index - __shfl(before - count, l);
+            w.k0 = max(min(a.cu_k[s0 + l], a.total_k), 0);
+            w.nk = max(min(a.cu_k[s0 + l + 1], a.total_k) - w.k0, 0);
             return true;
         }
         index -= all;
@@ -102,7 +115,8 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
     typedef Shape<DIM> S;
     // probabilities are held 2^6 higher in fp16, whose small numbers end at 2^-24
     constexpr float kLift = TYPE == WINO_FP16 ? 6.f : 0.f;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2][S::kTileK + S::kTileV];
+    constexpr int kBlocks = DIM <= 128 ? 2 : 1;             // 32-key blocks whose K is read before they are multiplied
+    __shared__ __attribute__((aligned(256))) uint8_t lds[2][2 * S::kTile];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 31, half = lane >> 5;
 
@@ -113,6 +127,9 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
     const int tiles = gridDim.x / a.heads;
     Work w;
     if (!find(a, tiles - 1 - (int)(blockIdx.x / a.heads), w)) return;
+    w.q0 = __builtin_amdgcn_readfirstlane(w.q0), w.nq = __builtin_amdgcn_readfirstlane(w.nq);
+    w.k0 = __builtin_amdgcn_readfirstlane(w.k0), w.nk = __builtin_amdgcn_readfirstlane(w.nk);
+    w.tile = __builtin_amdgcn_readfirstlane(w.tile);
 
     const int i0 = w.tile * kRows;                          // first query of the workgroup, in its sequence
     const int shift = a.causal ? w.nk - w.nq + 1 : w.nk;    // query i sees shift + i keys (all, where not causal)
@@ -142,60 +159,84 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
 
     const T* kbase = (const T*)a.k + (int64_t)w.k0 * a.k_stride + (int64_t)kvh * DIM;
     const T* vbase = (const T*)a.v + (int64_t)w.k0 * a.v_stride + (int64_t)kvh * DIM;
-    u32x4 ks[S::kPieces], vs[S::kPieces];
-    auto fetch = [&](int t0) {
+    // pieces of a tile that this thread copies: where they come from
+    uint32_t off_k[S::kPieces], off_v[S::kPieces];
+    auto offsets = [&](int rows) {
 #pragma unroll
         for (int x = 0; x < S::kPieces; ++x) {
-            const int piece = threadIdx.x + 64 * kWaves * x, r = piece / (DIM / 8), d = piece % (DIM / 8) * 8;
-            ks[x] = vs[x] = u32x4{0, 0, 0, 0};
-            if (t0 + r < w.nk) {
-                ks[x] = *(const u32x4*)(kbase + (int64_t)(t0 + r) * a.k_stride + d);
-                vs[x] = *(const u32x4*)(vbase + (int64_t)(t0 + r) * a.v_stride + d);
-            }
+            const int piece = threadIdx.x + 64 * kWaves * x, row = piece / S::kPiecesRow, at = piece % S::kPiecesRow;
+            const int from = min(row, rows - 1);            // rows past the end: the last one again
+            off_k[x] = (uint32_t)(from * (int)a.k_stride + (at ^ S::swap_k(row)) * 8) * 2u;
+            off_v[x] = (uint32_t)(from * (int)a.v_stride + (at ^ S::swap_v(row)) * 8) * 2u;
         }
     };
-    if (end > 0) fetch(0);
-    int buf = 0;
-    for (int t0 = 0; t0 < end; t0 += kKeys, buf ^= 1) {
-        uint8_t* lk = lds[buf];
-        uint8_t* lv = lk + S::kTileK;
-        // A value that is not finite would spoil the rows that do not see its key too (0 times it is NaN): in tiles that
-        // some row sees in part it leaves the product, and is added to the rows that see it.
-        bool spoilt = false;
-        const bool partly = t0 + kKeys > every;
-        if (partly) {
-            constexpr uint32_t kExp = TYPE == WINO_BF16 ? 0x7f80u : 0x7c00u;
-#pragma unroll
-            for (int x = 0; x < S::kPieces; ++x)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t v = vs[x][e];
-                    const bool lo = (v & kExp) == kExp, hi = ((v >> 16) & kExp) == kExp;
-                    spoilt = spoilt || lo || hi;
-                    vs[x][e] = (lo ? 0u : v & 0xffffu) | (hi ? 0u : v & 0xffff0000u);
-                }
-        }
+    auto copy = [&](int t0, int buf) {
+        if (t0 + kKeys > w.nk) offsets(w.nk - t0);
+        const T* k = kbase + (int64_t)t0 * a.k_stride;
+        const T* v = vbase + (int64_t)t0 * a.v_stride;
+        const uint32_t dst = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds[buf] + wave * 1024;
 #pragma unroll
         for (int x = 0; x < S::kPieces; ++x) {
-            const int piece = threadIdx.x + 64 * kWaves * x, r = piece / (DIM / 8), d = piece % (DIM / 8) * 16;
-            *(u32x4*)(lk + r * S::kRowK + d) = ks[x];
-            *(u32x4*)(lv + r * S::kRowV + d) = vs[x];
+            copy16(k, off_k[x], dst + x * (1024 * kWaves));
+            copy16(v, off_v[x], dst + x * (1024 * kWaves) + S::kTile);
         }
-        if (partly)
+    };
+    offsets(kKeys);
+    if (end > 0) copy(0, 0);
+    int buf = 0;
+    for (int t0 = 0; t0 < end; t0 += kKeys, buf ^= 1) {
+        const uint8_t* lk = lds[buf];
+        uint8_t* lv = lds[buf] + S::kTile;
+        WINO_WAIT_VM_LDS(0);
+        winof4::ring_barrier();                                     // the tile is there, and nobody reads the other one any more
+        if (t0 + kKeys < end) copy(t0 + kKeys, buf ^ 1);    // on its way while this one is computed
+        // A value that is not finite would spoil the rows that do not see its key too (0 times it is NaN): in tiles that
+        // some row sees in part it leaves the product, and is added to the rows that see it.  Rows of V past the end go
+        // as well.
+        bool spoilt = false;
+        if (t0 + kKeys > every) {
+            constexpr uint32_t kExp = TYPE == WINO_BF16 ? 0x7f80u : 0x7c00u;
+#pragma unroll
+            for (int x = 0; x < S::kPieces; ++x) {
+                const int piece = threadIdx.x + 64 * kWaves * x;
+                u32x4 v = *(u32x4*)(lv + 16 * piece);
+                const bool past = t0 + piece / S::kPiecesRow >= w.nk;
+                bool bad = past;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t u = v[e];
+                    const bool lo = past || (u & kExp) == kExp, hi = past || ((u >> 16) & kExp) == kExp;
+                    bad = bad || lo || hi;
+                    v[e] = (lo ? 0u : u & 0xffffu) | (hi ? 0u : u & 0xffff0000u);
+                }
+                if (bad) *(u32x4*)(lv + 16 * piece) = v;
+                spoilt = spoilt || (bad && !past);
+            }
             spoilt = __syncthreads_or(spoilt);
-        else
-            __syncthreads();
-        if (t0 + kKeys < end) fetch(t0 + kKeys);            // the next tile is on its way while this one is computed
+        }
         if (t0 >= wave_end) continue;
 
         f32x16 z[2];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b0 = 0; b0 < 2; b0 += kBlocks) {
+            T8 k[kBlocks][DIM / 16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) z[b][e] = 0.f;
-            const uint8_t* p = lk + (32 * b + c) * S::kRowK + 16 * half;
+            for (int b = 0; b < kBlocks; ++b) {
+                const int row = 32 * (b0 + b) + c;
 #pragma unroll
-            for (int s = 0; s < DIM / 16; ++s) z[b] = M::mul(*(const T8*)(p + 32 * s), q[s], z[b]);
+                for (int s = 0; s < DIM / 16; ++s)
+                    k[b][s] = *(const T8*)(lk + row * S::kRow + (((2 * s + half) ^ S::swap_k(row)) * 16));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) z[b0 + b][e] = 0.f;
+            }
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int s = 0; s < DIM / 16; ++s) z[b0 + b] = M::mul(k[b][s], q[s], z[b0 + b]);
         }
         if (t0 + kKeys > wave_every) {
 #pragma unroll
@@ -241,22 +282,25 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
             }
         sum += sum1;
         // lane l of 16 gives the address of four dimensions of key l / 4 and gets dimension l of four keys
-        const int l = lane & 15;
-        const uint8_t* from = lv + (4 * half + (l >> 2)) * S::kRowV + ((lane >> 4) & 1) * 32 + (l & 3) * 8;
+        const int l = lane & 15, vrow = 4 * half + (l >> 2), piece = 2 * ((lane >> 4) & 1) + ((l & 3) >> 1);
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const T8 pp = __builtin_bit_cast(T8, u32x4{p[b][4 * s], p[b][4 * s + 1], p[b][4 * s + 2], p[b][4 * s + 3]});
+                T8 v[DIM / 32];
 #pragma unroll
                 for (int n = 0; n < DIM / 32; ++n) {
                     typedef __attribute__((ext_vector_type(4))) short s4;
                     typedef __attribute__((address_space(3))) s4* lds4;
-                    const uint8_t* f = from + (32 * b + 16 * s) * S::kRowV + 64 * n;
+                    // rows 8 apart exchange their pieces alike
+                    const uint8_t* f = lv + (32 * b + 16 * s + vrow) * S::kRow + ((4 * n + piece) ^ S::swap_v(vrow)) * 16 + (l & 1) * 8;
                     const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)f));
-                    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(f + 8 * S::kRowV)));
-                    o[n] = M::mul(__builtin_bit_cast(T8, u32x4{x[0], x[1], y[0], y[1]}), pp, o[n]);
+                    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(f + 8 * S::kRow)));
+                    v[n] = __builtin_bit_cast(T8, u32x4{x[0], x[1], y[0], y[1]});
                 }
+#pragma unroll
+                for (int n = 0; n < DIM / 32; ++n) o[n] = M::mul(v[n], pp, o[n]);
             }
         if (spoilt) {
             for (int t = t0; t < min(t0 + kKeys, row_end); ++t) {
@@ -319,6 +363,7 @@ extern "C" wino_status prompt_attention(const void* q, int64_t q_stride, const v
     const int64_t dim = head_dim;
     if ((total_q > 1 && q_stride < heads * dim) || (total_k > 1 && (k_stride < kv_heads * dim || v_stride < kv_heads * dim)))
         return WINO_EINVAL;
+    if (total_k > 1 && (k_stride > 1 << 24 || v_stride > 1 << 24)) return WINO_EUNSUPPORTED;
     if ((total_q > 1 && (q_stride & 7)) || (total_k > 1 && ((k_stride | v_stride) & 7)) ||
         !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
         return WINO_EUNSUPPORTED;
