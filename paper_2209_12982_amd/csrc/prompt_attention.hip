@@ -115,7 +115,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
     typedef Shape<DIM> S;
     // probabilities are held 2^6 higher in fp16, whose small numbers end at 2^-24
     constexpr float kLift = TYPE == WINO_FP16 ? 6.f : 0.f;
-    constexpr int kBlocks = DIM <= 128 ? 2 : 1;             // 32-key blocks whose K is read before they are multiplied
+    constexpr int kAhead = DIM <= 128 ? DIM / 8 : (DIM == 192 ? 12 : 8);    // pieces of K read before they are multiplied
     __shared__ __attribute__((aligned(256))) uint8_t lds[2][2 * S::kTile];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 31, half = lane >> 5;
@@ -218,25 +218,44 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
 
         f32x16 z[2];
 #pragma unroll
-        for (int b0 = 0; b0 < 2; b0 += kBlocks) {
-            T8 k[kBlocks][DIM / 16];
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) {
-                const int row = 32 * (b0 + b) + c;
+            for (int e = 0; e < 16; ++e) z[b][e] = 0.f;
 #pragma unroll
-                for (int s = 0; s < DIM / 16; ++s)
-                    k[b][s] = *(const T8*)(lk + row * S::kRow + (((2 * s + half) ^ S::swap_k(row)) * 16));
+        for (int f0 = 0; f0 < DIM / 8; f0 += kAhead) {
+            T8 k[kAhead];
+#pragma unroll
+            for (int f = 0; f < kAhead; ++f) {
+                const int row = (f0 + f) / (DIM / 16) * 32 + c, s = (f0 + f) % (DIM / 16);
+                k[f] = *(const T8*)(lk + row * S::kRow + (((2 * s + half) ^ S::swap_k(row)) * 16));
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) z[b0 + b][e] = 0.f;
+            for (int f = 0; f < kAhead; ++f) {
+                const int b = (f0 + f) / (DIM / 16);
+                z[b] = M::mul(k[f], q[(f0 + f) % (DIM / 16)], z[b]);
             }
+        }
+        // the first half of V is read while the scores are turned into probabilities
+        const int l = lane & 15, vrow = 4 * half + (l >> 2), piece = 2 * ((lane >> 4) & 1) + ((l & 3) >> 1);
+        auto read_v = [&](int b, int s, T8 (&v)[DIM / 32]) {
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                for (int s = 0; s < DIM / 16; ++s) z[b0 + b] = M::mul(k[b][s], q[s], z[b0 + b]);
+            for (int n = 0; n < DIM / 32; ++n) {
+                // lane l of 16 gives the address of four dimensions of key l / 4 and gets dimension l of four keys;
+                // rows 8 apart exchange their pieces alike
+                typedef __attribute__((ext_vector_type(4))) short s4;
+                typedef __attribute__((address_space(3))) s4* lds4;
+                const uint8_t* f = lv + (32 * b + 16 * s + vrow) * S::kRow + ((4 * n + piece) ^ S::swap_v(vrow)) * 16 + (l & 1) * 8;
+                const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)f));
+                const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(f + 8 * S::kRow)));
+                v[n] = __builtin_bit_cast(T8, u32x4{x[0], x[1], y[0], y[1]});
+            }
+        };
+        T8 v[2][DIM / 32];
+        if constexpr (DIM <= 128) {
+            read_v(0, 0, v[0]);
+            read_v(0, 1, v[1]);
+            __builtin_amdgcn_sched_barrier(0);
         }
         if (t0 + kKeys > wave_every) {
 #pragma unroll
@@ -281,26 +300,14 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
                 p[b][e / 2] = __builtin_bit_cast(uint32_t, x);
             }
         sum += sum1;
-        // lane l of 16 gives the address of four dimensions of key l / 4 and gets dimension l of four keys
-        const int l = lane & 15, vrow = 4 * half + (l >> 2), piece = 2 * ((lane >> 4) & 1) + ((l & 3) >> 1);
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const T8 pp = __builtin_bit_cast(T8, u32x4{p[b][4 * s], p[b][4 * s + 1], p[b][4 * s + 2], p[b][4 * s + 3]});
-                T8 v[DIM / 32];
+                if (b == 1 || DIM > 128) read_v(b, s, v[s]);
 #pragma unroll
-                for (int n = 0; n < DIM / 32; ++n) {
-                    typedef __attribute__((ext_vector_type(4))) short s4;
-                    typedef __attribute__((address_space(3))) s4* lds4;
-                    // rows 8 apart exchange their pieces alike
-                    const uint8_t* f = lv + (32 * b + 16 * s + vrow) * S::kRow + ((4 * n + piece) ^ S::swap_v(vrow)) * 16 + (l & 1) * 8;
-                    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)f));
-                    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(f + 8 * S::kRow)));
-                    v[n] = __builtin_bit_cast(T8, u32x4{x[0], x[1], y[0], y[1]});
-                }
-#pragma unroll
-                for (int n = 0; n < DIM / 32; ++n) o[n] = M::mul(v[n], pp, o[n]);
+                for (int n = 0; n < DIM / 32; ++n) o[n] = M::mul(v[s][n], pp, o[n]);
             }
         if (spoilt) {
             for (int t = t0; t < min(t0 + kKeys, row_end); ++t) {
