@@ -17,7 +17,7 @@
 namespace {
 using namespace mx4;
 
-constexpr int kWaves = 4, kRows = 32 * kWaves, kKeys = 64;
+constexpr int kRows = 128, kKeys = 64;
 constexpr float kNever = -__builtin_inff();
 
 struct PromptArgs {
@@ -35,6 +35,9 @@ struct PromptArgs {
 template <int DIM> struct Shape {
     static constexpr int kRow = DIM * 2, kPiecesRow = kRow / 16;
     static constexpr int kTile = kKeys * kRow;
+    // Wide heads: two waves share 32 queries, each with half the dimensions of the result.  Both work out the scores,
+    // half again as many products in all, but the registers of one wave do not hold the whole result.
+    static constexpr int kShare = DIM > 128 ? 2 : 1, kWaves = 4 * kShare, kOut = DIM / 32 / kShare;
     static constexpr int kPieces = kKeys * kPiecesRow / (64 * kWaves);  // of a tile, for a thread
     // K is read 16 rows at a time, the same piece of each: they have to stand in 16 different columns.  Of a row's
     // pieces, 2^kBits in a row can be exchanged.
@@ -107,7 +110,7 @@ __device__ inline bool find(const PromptArgs& a, int index, Work& w) {
 }
 
 template <int TYPE, int DIM>
-__global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attention_kernel(PromptArgs a) {
+__global__ __launch_bounds__(64 * Shape<DIM>::kWaves, 2) void prompt_attention_kernel(PromptArgs a) {
     typedef typename Half<TYPE>::type T;
     typedef Mfma<TYPE> M;
     typedef typename M::T8 T8;
@@ -115,10 +118,10 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
     typedef Shape<DIM> S;
     // probabilities are held 2^6 higher in fp16, whose small numbers end at 2^-24
     constexpr float kLift = TYPE == WINO_FP16 ? 6.f : 0.f;
-    constexpr int kAhead = DIM <= 128 ? DIM / 8 : (DIM == 192 ? 12 : 8);    // pieces of K read before they are multiplied
+    constexpr int kAhead = DIM <= 128 ? DIM / 8 : 8;    // pieces of K read before they are multiplied
     __shared__ __attribute__((aligned(256))) uint8_t lds[2][2 * S::kTile];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int c = lane & 31, half = lane >> 5;
+    const int c = lane & 31, half = lane >> 5, d0 = wave / 4 * (S::kOut * 32);      // d0: the wave's first dimension
 
     // workgroups that follow each other run on different XCDs: the heads that share a K and V are kv_heads apart, and
     // late tiles, which see the most keys, come first
@@ -136,7 +139,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
     auto sees = [&](int i) { return max(0, a.causal ? min(shift + i, w.nk) : w.nk); };
     const int every = sees(i0);                             // keys that all rows of the workgroup see
     const int end = sees(min(i0 + kRows, w.nq) - 1);        // keys that some row sees
-    const int iw = i0 + 32 * wave;
+    const int iw = i0 + 32 * (wave % 4);
     const int wave_every = sees(iw), wave_end = iw < w.nq ? sees(min(iw + 32, w.nq) - 1) : 0;
     const int i = iw + c;                                   // this lane's query
     const int row_end = i < w.nq ? sees(i) : 0;
@@ -150,9 +153,9 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
             q[s] = __builtin_bit_cast(T8, (x & a.q_and) ^ a.q_xor);
         }
     }
-    f32x16 o[DIM / 32];                                     // lane: dimensions 32 n + 8 (e / 4) + 4 half + e % 4 of query c
+    f32x16 o[S::kOut];                                      // lane: dimensions d0 + 32 n + 8 (e / 4) + 4 half + e % 4 of query c
 #pragma unroll
-    for (int n = 0; n < DIM / 32; ++n)
+    for (int n = 0; n < S::kOut; ++n)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[n][e] = 0.f;
     float ref = kNever, sum = 0.f;                          // ref: the power of two that o and sum are held against
@@ -164,7 +167,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
     auto offsets = [&](int rows) {
 #pragma unroll
         for (int x = 0; x < S::kPieces; ++x) {
-            const int piece = threadIdx.x + 64 * kWaves * x, row = piece / S::kPiecesRow, at = piece % S::kPiecesRow;
+            const int piece = threadIdx.x + 64 * S::kWaves * x, row = piece / S::kPiecesRow, at = piece % S::kPiecesRow;
             const int from = min(row, rows - 1);            // rows past the end: the last one again
             off_k[x] = (uint32_t)(from * (int)a.k_stride + (at ^ S::swap_k(row)) * 8) * 2u;
             off_v[x] = (uint32_t)(from * (int)a.v_stride + (at ^ S::swap_v(row)) * 8) * 2u;
@@ -177,8 +180,8 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
         const uint32_t dst = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds[buf] + wave * 1024;
 #pragma unroll
         for (int x = 0; x < S::kPieces; ++x) {
-            copy16(k, off_k[x], dst + x * (1024 * kWaves));
-            copy16(v, off_v[x], dst + x * (1024 * kWaves) + S::kTile);
+            copy16(k, off_k[x], dst + x * (1024 * S::kWaves));
+            copy16(v, off_v[x], dst + x * (1024 * S::kWaves) + S::kTile);
         }
     };
     offsets(kKeys);
@@ -198,7 +201,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
             constexpr uint32_t kExp = TYPE == WINO_BF16 ? 0x7f80u : 0x7c00u;
 #pragma unroll
             for (int x = 0; x < S::kPieces; ++x) {
-                const int piece = threadIdx.x + 64 * kWaves * x;
+                const int piece = threadIdx.x + 64 * S::kWaves * x;
                 u32x4 v = *(u32x4*)(lv + 16 * piece);
                 const bool past = t0 + piece / S::kPiecesRow >= w.nk;
                 bool bad = past;
@@ -215,6 +218,10 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
             spoilt = __syncthreads_or(spoilt);
         }
         if (t0 >= wave_end) continue;
+        // Addresses of a wave's pieces differ by exchanged bits.  Wide heads have no registers to keep them all: there
+        // they are made anew from the row in each tile.
+        int ck = c, lane_v = lane;
+        if constexpr (DIM > 128) asm("" : "+v"(ck), "+v"(lane_v));
 
         f32x16 z[2];
 #pragma unroll
@@ -226,7 +233,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
             T8 k[kAhead];
 #pragma unroll
             for (int f = 0; f < kAhead; ++f) {
-                const int row = (f0 + f) / (DIM / 16) * 32 + c, s = (f0 + f) % (DIM / 16);
+                const int row = (f0 + f) / (DIM / 16) * 32 + ck, s = (f0 + f) % (DIM / 16);
                 k[f] = *(const T8*)(lk + row * S::kRow + (((2 * s + half) ^ S::swap_k(row)) * 16));
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -237,26 +244,24 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
             }
         }
         // the first half of V is read while the scores are turned into probabilities
-        const int l = lane & 15, vrow = 4 * half + (l >> 2), piece = 2 * ((lane >> 4) & 1) + ((l & 3) >> 1);
-        auto read_v = [&](int b, int s, T8 (&v)[DIM / 32]) {
+        const int l = lane_v & 15, vrow = 4 * half + (l >> 2), piece = 2 * ((lane_v >> 4) & 1) + ((l & 3) >> 1);
+        auto read_v = [&](int b, int s, T8 (&v)[S::kOut]) {
 #pragma unroll
-            for (int n = 0; n < DIM / 32; ++n) {
+            for (int n = 0; n < S::kOut; ++n) {
                 // lane l of 16 gives the address of four dimensions of key l / 4 and gets dimension l of four keys;
                 // rows 8 apart exchange their pieces alike
                 typedef __attribute__((ext_vector_type(4))) short s4;
                 typedef __attribute__((address_space(3))) s4* lds4;
-                const uint8_t* f = lv + (32 * b + 16 * s + vrow) * S::kRow + ((4 * n + piece) ^ S::swap_v(vrow)) * 16 + (l & 1) * 8;
+                const uint8_t* f = lv + (32 * b + 16 * s + vrow) * S::kRow + ((d0 / 8 + 4 * n + piece) ^ S::swap_v(vrow)) * 16 + (l & 1) * 8;
                 const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)f));
                 const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(f + 8 * S::kRow)));
                 v[n] = __builtin_bit_cast(T8, u32x4{x[0], x[1], y[0], y[1]});
             }
         };
-        T8 v[2][DIM / 32];
-        if constexpr (DIM <= 128) {
-            read_v(0, 0, v[0]);
-            read_v(0, 1, v[1]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
+        T8 v[2][S::kOut];
+        read_v(0, 0, v[0]);
+        read_v(0, 1, v[1]);
+        __builtin_amdgcn_sched_barrier(0);
         if (t0 + kKeys > wave_every) {
 #pragma unroll
             for (int b = 0; b < 2; ++b)
@@ -282,7 +287,7 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
             ref = to;
             sum *= alpha;
 #pragma unroll
-            for (int n = 0; n < DIM / 32; ++n) o[n] *= alpha;
+            for (int n = 0; n < S::kOut; ++n) o[n] *= alpha;
         }
         const float base = ref == kNever ? 0.f : kLift - ref;
         uint32_t p[2][8];
@@ -305,20 +310,22 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const T8 pp = __builtin_bit_cast(T8, u32x4{p[b][4 * s], p[b][4 * s + 1], p[b][4 * s + 2], p[b][4 * s + 3]});
-                if (b == 1 || DIM > 128) read_v(b, s, v[s]);
+                if (b == 1) read_v(b, s, v[s]);
 #pragma unroll
-                for (int n = 0; n < DIM / 32; ++n) o[n] = M::mul(v[s][n], pp, o[n]);
+                for (int n = 0; n < S::kOut; ++n) o[n] = M::mul(v[s][n], pp, o[n]);
             }
         if (spoilt) {
             for (int t = t0; t < min(t0 + kKeys, row_end); ++t) {
-                const T* v = vbase + (int64_t)t * a.v_stride + 4 * half;
+                const T* v = vbase + (int64_t)t * a.v_stride + d0 + 4 * half;
 #pragma unroll
-                for (int n = 0; n < DIM / 32; ++n)
+                for (int n = 0; n < S::kOut; ++n) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const float x = (float)v[32 * n + 8 * (e / 4) + e % 4];
                         if (!(__builtin_fabsf(x) < __builtin_inff())) o[n][e] += x;
                     }
+                    __builtin_amdgcn_sched_barrier(0);      // a rare path: few registers rather than speed
+                }
             }
         }
     }
@@ -329,9 +336,9 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
     if (i < w.nq) {
         typedef T T4 __attribute__((ext_vector_type(4)));
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        T* out = (T*)a.out + ((int64_t)(w.q0 + i) * a.heads + h) * DIM + 4 * half;
+        T* out = (T*)a.out + ((int64_t)(w.q0 + i) * a.heads + h) * DIM + d0 + 4 * half;
 #pragma unroll
-        for (int n = 0; n < DIM / 32; ++n)
+        for (int n = 0; n < S::kOut; ++n)
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
                 *(T4*)(out + 32 * n + 2 * e) =
@@ -341,14 +348,16 @@ __global__ __launch_bounds__(64 * kWaves, DIM <= 128 ? 2 : 1) void prompt_attent
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
-template <int TYPE> void launch(int dim, dim3 grid, hipStream_t stream, const PromptArgs& a) {
-    const dim3 block(64 * kWaves);
+template <int TYPE, int DIM> void launch(dim3 grid, hipStream_t stream, const PromptArgs& a) {
+    hipLaunchKernelGGL((prompt_attention_kernel<TYPE, DIM>), grid, dim3(64 * Shape<DIM>::kWaves), 0, stream, a);
+}
+template <int TYPE> void launch_dim(int dim, dim3 grid, hipStream_t stream, const PromptArgs& a) {
     switch (dim) {
-        case 64: hipLaunchKernelGGL((prompt_attention_kernel<TYPE, 64>), grid, block, 0, stream, a); break;
-        case 96: hipLaunchKernelGGL((prompt_attention_kernel<TYPE, 96>), grid, block, 0, stream, a); break;
-        case 128: hipLaunchKernelGGL((prompt_attention_kernel<TYPE, 128>), grid, block, 0, stream, a); break;
-        case 192: hipLaunchKernelGGL((prompt_attention_kernel<TYPE, 192>), grid, block, 0, stream, a); break;
-        default: hipLaunchKernelGGL((prompt_attention_kernel<TYPE, 256>), grid, block, 0, stream, a); break;
+        case 64: return launch<TYPE, 64>(grid, stream, a);
+        case 96: return launch<TYPE, 96>(grid, stream, a);
+        case 128: return launch<TYPE, 128>(grid, stream, a);
+        case 192: return launch<TYPE, 192>(grid, stream, a);
+        default: return launch<TYPE, 256>(grid, stream, a);
     }
 }
 
@@ -382,8 +391,8 @@ extern "C" wino_status prompt_attention(const void* q, int64_t q_stride, const v
     a.scale_log2 = scale == 0.f ? 1.f : __builtin_fabsf(scale) * 1.44269504088896340736f;
     if (a.scale_log2 - a.scale_log2 != 0.f) return WINO_EUNSUPPORTED;       // past fp32's range
     if (type == WINO_BF16)
-        launch<WINO_BF16>(head_dim, dim3((unsigned)blocks), stream, a);
+        launch_dim<WINO_BF16>(head_dim, dim3((unsigned)blocks), stream, a);
     else
-        launch<WINO_FP16>(head_dim, dim3((unsigned)blocks), stream, a);
+        launch_dim<WINO_FP16>(head_dim, dim3((unsigned)blocks), stream, a);
     return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
 }
