@@ -582,71 +582,30 @@ def wino_probe_conv_kernels(plan, x, n, h, w, layout=NCHW):
     return dict(d, xform=PROBE_XFORMS[d["xform"]], gemm=PROBE_GEMMS[d["gemm"]])
 
 
-# ---- Decoder operators in 4 bits: tensors carry the sizes and the type.
+# ---- Decoder operators in 4 bits: tensors carry the sizes and the type, and
+# are checked in _marshal.so (csrc/marshal.cpp).
 
 class _KV4Cache(ctypes.Structure):
+    """kv4_cache, for callers of the C functions."""
     _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
                 ("v_scales", ctypes.c_void_p), ("pages", ctypes.c_int64), ("kv_heads", ctypes.c_int32),
                 ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
-_FLOAT_TYPES = None
+_MARSHAL = None
 
 
-def _float_type(t, what):
-    """WINO_BF16 or WINO_FP16 of a 16-bit GPU tensor."""
-    global _FLOAT_TYPES
-    if _FLOAT_TYPES is None:
-        import torch
-        _FLOAT_TYPES = {torch.bfloat16: 0, torch.float16: 1}
-    code = _FLOAT_TYPES.get(getattr(t, "dtype", None))
-    if code is None:
-        raise ValueError(f"{what}: expected a bf16 or fp16 tensor on the GPU")
-    return code
-
-
-def _rows(t, dtype, shape, what):
-    """(address, row stride) of a GPU tensor of `shape` whose rows (all
-    dimensions but the first) are dense; the rows may lie apart."""
-    if not (t.shape == shape and t.dtype is dtype and t.is_cuda):
-        raise ValueError(f"{what}: expected {dtype} {tuple(shape)} on the GPU, got {t.dtype} {tuple(t.shape)} on "
-                         f"{t.device}")
-    st = t.stride()
-    if t.is_contiguous():
-        return t.data_ptr(), st[0]
-    want = 1
-    for n, s in zip(reversed(shape[1:]), reversed(st[1:])):
-        if n > 1 and s != want:
-            raise ValueError(f"{what}: only the first dimension may be strided")
-        want *= n
-    return t.data_ptr(), (st[0] if shape[0] > 1 else want)
-
-
-def _dense(t, dtype, shape, what):
-    """Address of a dense GPU tensor of `shape`."""
-    if t.shape == shape and t.dtype is dtype and t.is_cuda and t.is_contiguous():
-        return t.data_ptr()
-    raise ValueError(f"{what}: expected dense {dtype} {tuple(shape)} on the GPU, got {t.dtype} {tuple(t.shape)} on "
-                     f"{t.device}")
-
-
-def _scratch(t):
-    """(address, bytes) of a workspace: any dense GPU tensor, or None."""
-    if t is None:
-        return None, 0
-    return _dptr(t, None, 0, "workspace"), t.numel() * t.element_size()
-
-
-def _cache_struct(cache):
-    import torch
-    kc, ks, vc, vs = cache
-    if kc.dim() != 4:
-        raise ValueError("cache: expected (k_codes, k_scales, v_codes, v_scales), each [pages, kv_heads, page, width]")
-    pages, heads, page, half = kc.shape
-    codes, scales = (pages, heads, page, half), (pages, heads, page, half // 16)
-    u8 = torch.uint8
-    return _KV4Cache(_dense(kc, u8, codes, "k_codes"), _dense(ks, u8, scales, "k_scales"),
-                     _dense(vc, u8, codes, "v_codes"), _dense(vs, u8, scales, "v_scales"), pages, heads, page, 2 * half)
+def _marshal():
+    """The marshalling module; loaded after torch and the library, whose symbols it uses."""
+    global _MARSHAL
+    if _MARSHAL is None:
+        load_library()
+        try:
+            from . import _marshal as module
+        except ImportError as e:
+            raise LibraryNotBuilt(f"_marshal.so: {e}; run __graft_entry__.build()") from e
+        _MARSHAL = module
+    return _MARSHAL
 
 
 def w4_quantize_weights(w):
@@ -667,17 +626,7 @@ def w4_matvec_workspace_bytes(m, n, k):
 
 def w4_matvec(x, codes, scales, y, bias=None, workspace=None, stream=None):
     """y [m, n] = x [m, k] times the 4-bit weights [n, k] transposed, + bias."""
-    import torch
-    lib = load_library()
-    kind = _float_type(x, "x")
-    m, k = x.shape
-    n = codes.shape[0]
-    xp, xs = _rows(x, x.dtype, (m, k), "x")
-    yp, ys = _rows(y, x.dtype, (m, n), "y")
-    st = lib.w4_matvec(xp, xs, _dense(codes, torch.uint8, (n, k // 2), "codes"),
-                       _dense(scales, torch.uint8, (n, k // 32), "scales"),
-                       None if bias is None else _dense(bias, x.dtype, (n,), "bias"), yp, ys, m, n, k, kind,
-                       *_scratch(workspace), _stream(stream))
+    st = (_MARSHAL or _marshal()).w4_matvec(x, codes, scales, y, bias, workspace, _stream(stream))
     if st:
         _check(st, "w4_matvec")
 
@@ -686,31 +635,10 @@ def kv4_append(q, k, v, cos_sin, positions, slots, cache, q_out=None, k_out=None
                values=KV4_ROTATED, stream=None):
     """Turns q [tokens, heads, d] (or None) and k [tokens, kv_heads, d], puts k
     and v into `cache` (k_codes, k_scales, v_codes, v_scales) at `slots`."""
-    import torch
-    lib = load_library()
-    kind = _float_type(k, "k")
-    dt = k.dtype
-    c = _cache_struct(cache)
-    n, hkv, d = k.shape
-    if (hkv, d) != (c.kv_heads, c.head_dim):
-        raise ValueError(f"k: {hkv} heads of {d}, the cache has {c.kv_heads} of {c.head_dim}")
-    kp, ks = _rows(k, dt, (n, hkv, d), "k")
-    vp, vs = _rows(v, dt, (n, hkv, d), "v")
-    hq, qp, qs = 0, None, 0
-    if q is not None:
-        hq = q.shape[1]
-        qp, qs = _rows(q, dt, (n, hq, d), "q")
-    if (q is None) != (q_out is None):
-        raise ValueError("q and q_out go together")
-    rows, rot = cos_sin.shape
-    st = lib.kv4_append(qp, qs, kp, ks, vp, vs, n, hq, _dense(cos_sin, torch.float32, (rows, rot), "cos_sin"), rows,
-                        rot, _dense(positions, torch.int32, (n,), "positions"),
-                        _dense(slots, torch.int64, (n,), "slots"), ctypes.byref(c),
-                        None if q_out is None else _dense(q_out, dt, (n, hq, d), "q_out"),
-                        None if k_out is None else _dense(k_out, dt, (n, hkv, d), "k_out"),
-                        None if v_out is None else _dense(v_out, dt, (n, hkv, d), "v_out"), rotary, values, kind,
-                        _stream(stream))
-    _check(st, "kv4_append")
+    st = (_MARSHAL or _marshal()).kv4_append(q, k, v, cos_sin, positions, slots, cache, q_out, k_out, v_out, rotary,
+                                             values, _stream(stream))
+    if st:
+        _check(st, "kv4_append")
 
 
 def kv4_attention_workspace_bytes(batch, q_len, heads, kv_heads, head_dim, max_pages, page_size):
@@ -721,19 +649,7 @@ def kv4_attention_workspace_bytes(batch, q_len, heads, kv_heads, head_dim, max_p
 def kv4_attention(q, cache, block_table, lens, out, scale, workspace=None, stream=None):
     """out = attention of q [batch * q_len, heads, d] over the cached tokens of
     each sequence; block_table int32 [batch, max_pages], lens int32 [batch]."""
-    import torch
-    lib = load_library()
-    kind = _float_type(q, "q")
-    c = _cache_struct(cache)
-    rows, hq, d = q.shape
-    batch, max_pages = block_table.shape
-    if d != c.head_dim or (rows % batch if batch else rows):
-        raise ValueError(f"q: {rows} rows of {d} for {batch} sequences and heads of {c.head_dim}")
-    qp, qs = _rows(q, q.dtype, (rows, hq, d), "q")
-    st = lib.kv4_attention(qp, qs, ctypes.byref(c), _dense(block_table, torch.int32, (batch, max_pages), "block_table"),
-                           max_pages, _dense(lens, torch.int32, (batch,), "lens"),
-                           _dense(out, q.dtype, (rows, hq, d), "out"), batch, rows // batch if batch else 0, hq, scale,
-                           kind, *_scratch(workspace), _stream(stream))
+    st = (_MARSHAL or _marshal()).kv4_attention(q, cache, block_table, lens, out, scale, workspace, _stream(stream))
     if st:
         _check(st, "kv4_attention")
 
@@ -741,17 +657,6 @@ def kv4_attention(q, cache, block_table, lens, out, scale, workspace=None, strea
 def prompt_attention(q, k, v, cu_q, cu_k, max_q, out, scale, causal=True, stream=None):
     """out = attention of the packed queries q [total_q, heads, d] over k, v
     [total_k, kv_heads, d]; cu_q, cu_k int32 [seqs + 1]."""
-    import torch
-    lib = load_library()
-    kind = _float_type(q, "q")
-    dt = q.dtype
-    nq, hq, d = q.shape
-    nk, hkv, _ = k.shape
-    seqs = max(cu_q.numel() - 1, 0)
-    qp, qs = _rows(q, dt, (nq, hq, d), "q")
-    kp, ks = _rows(k, dt, (nk, hkv, d), "k")
-    vp, vs = _rows(v, dt, (nk, hkv, d), "v")
-    st = lib.prompt_attention(qp, qs, kp, ks, vp, vs, _dense(cu_q, torch.int32, (cu_q.numel(),), "cu_q"),
-                              _dense(cu_k, torch.int32, (cu_q.numel(),), "cu_k"), seqs, nq, nk, max_q, hq, hkv, d,
-                              scale, int(bool(causal)), _dense(out, dt, (nq, hq, d), "out"), kind, _stream(stream))
-    _check(st, "prompt_attention")
+    st = (_MARSHAL or _marshal()).prompt_attention(q, k, v, cu_q, cu_k, max_q, out, scale, causal, _stream(stream))
+    if st:
+        _check(st, "prompt_attention")

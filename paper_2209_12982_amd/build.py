@@ -1,17 +1,21 @@
-"""Builds libwinof4.so (host plan + gfx950 HIP kernels) in-tree with hipcc.
+"""Builds libwinof4.so (host plan + gfx950 HIP kernels) in-tree with hipcc, and
+the binding's _marshal.so with the host compiler.
 
-The library is a plain C ABI (include/winof4.h); nothing here links against
-torch.  ``build()`` always recompiles.
+The library is a plain C ABI (include/winof4.h) that links nothing of torch;
+_marshal.so checks torch tensors for the binding and links both.  ``build()``
+always recompiles.
 """
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libwinof4.so")
+MARSHAL = os.path.join(PKG, "_marshal.so")
 SOURCES = ["plan.cpp", "plan_device.hip", "wino_kernels.hip", "wino_fused.hip", "direct_conv.hip", "wino_float.hip", "probe.hip",
            "w4_quantize.cpp", "w4_matvec.hip", "kv4_append.hip", "kv4_attention.hip", "prompt_attention.hip"]
 ARCH = "gfx950"
@@ -29,6 +33,23 @@ def hipcc():
     raise RuntimeError("hipcc not found")
 
 
+def marshal_commands(out):
+    """Compile and link commands of _marshal.so; the library has to be there for the second."""
+    import torch
+    from torch.utils.cpp_extension import include_paths, library_paths
+    rocm = os.path.dirname(os.path.dirname(os.path.realpath(hipcc())))
+    obj = os.path.join(PKG, "_build", "marshal.cpp.o")
+    compile_ = ["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__",
+                f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"]]
+    for p in include_paths() + [os.path.join(rocm, "include")]:
+        compile_ += ["-isystem", p]
+    link = ["g++", "-shared", "-o", out, obj, "-L", PKG, "-l:libwinof4.so", "-Wl,-rpath,$ORIGIN"]
+    for p in library_paths()[:1]:
+        link += ["-L", p]
+    return compile_ + ["-c", os.path.join(CSRC, "marshal.cpp"), "-o", obj], link + ["-ltorch_python", "-ltorch_cpu", "-lc10"]
+
+
 def build(verbose=False, jobs=None):
     cc = hipcc()
     objdir = os.path.join(PKG, "_build")
@@ -44,6 +65,9 @@ def build(verbose=False, jobs=None):
             print(" ".join(cmd), flush=True)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
         objs.append(obj)
+    compile_marshal, link_marshal = marshal_commands(MARSHAL + ".tmp")
+    procs.append(("marshal.cpp", subprocess.Popen(compile_marshal, stdout=subprocess.PIPE, stderr=subprocess.STDOUT,
+                                                  text=True)))
     failed = []
     for src, p in procs:
         out, _ = p.communicate()
@@ -54,7 +78,7 @@ def build(verbose=False, jobs=None):
         elif verbose and msgs:
             print("\n".join(msgs))
     if failed:
-        raise RuntimeError("hipcc failed for " + ", ".join(failed))
+        raise RuntimeError("compilation failed for " + ", ".join(failed))
     tmp = LIB + ".tmp"
     cmd = [cc, "-shared", f"--offload-arch={ARCH}", "-o", tmp] + objs
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
@@ -62,6 +86,11 @@ def build(verbose=False, jobs=None):
         sys.stderr.write(r.stdout)
         raise RuntimeError("link failed")
     os.replace(tmp, LIB)
+    r = subprocess.run(link_marshal, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if r.returncode != 0:
+        sys.stderr.write(r.stdout)
+        raise RuntimeError("link failed")
+    os.replace(MARSHAL + ".tmp", MARSHAL)
     return LIB
 
 
