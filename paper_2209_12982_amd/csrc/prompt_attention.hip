@@ -25,7 +25,6 @@ namespace {
 using namespace mx4;
 
 constexpr float kNever = -__builtin_inff();
-constexpr int kFew = 512;       // tiles of 128 rows that fill the device
 
 struct PromptArgs {
     const void *q, *k, *v;
@@ -404,11 +403,20 @@ template <int TYPE, int DIM, int ROWS, int TEAMS, int KEYS> wino_status launch(c
                        dim3(64 * Shape<DIM, ROWS, TEAMS, KEYS>::kWaves), 0, stream, a);
     return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
 }
+// Tiles of 128 rows by one team once they fill the device twice over (once for wide heads, whose workgroups take a whole
+// compute unit); before that 64 rows by two teams, and by four where the keys are many and the tiles very few.  Heads of
+// 128, causal, us for one team of 128 / two of 64 / four of 64:
+//   1 x 256, 16 heads (32 tiles) 11.8 / 9.8 / 11.2      1 x 512 on 4096 keys, 8 heads (32) 80 / 53 / 44
+//   1 x 1024, 16 heads (128) 26.0 / 19.4 / 19.0         1 x 2048, 16 heads (256) 45 / 35 / 38
+//   4 x 512, 32 heads (512) 25.6 / 27.3 / 42.9          8 x 512, 32 heads (1024) 41 / 49 / 84
+// and of 256 for one / two: 1 x 2048, 16 heads (256) 85 / 72, 1 x 3000 (376) 127 / 148.
 template <int TYPE, int DIM> wino_status pick(const PromptArgs& a, int max_q, hipStream_t stream) {
     // tiles of 128 rows that have something to do, by the longest sequence's length
     const int64_t busy = std::min(tiles(a, 128), (((int64_t)max_q * a.group + 127) / 128) * a.seqs * a.kv_heads);
-    if (busy >= kFew) return launch<TYPE, DIM, 128, 1, 64>(a, stream);
-    return launch<TYPE, DIM, 64, (DIM > 128 ? 2 : 4), 32>(a, stream);
+    if (busy >= (DIM > 128 ? 320 : 512)) return launch<TYPE, DIM, 128, 1, 64>(a, stream);
+    if constexpr (DIM <= 128)
+        if (busy <= 128 && a.total_k / a.seqs >= 1024) return launch<TYPE, DIM, 64, 4, 32>(a, stream);
+    return launch<TYPE, DIM, 64, 2, 32>(a, stream);
 }
 template <int TYPE> wino_status launch_dim(int dim, const PromptArgs& a, int max_q, hipStream_t stream) {
     switch (dim) {
