@@ -600,7 +600,7 @@ extern "C" wino_status kv4_attention(const void* q, int64_t q_stride, const kv4_
         return WINO_EUNSUPPORTED;
     const int64_t rows = (int64_t)batch * q_len * heads;
     if (rows > 0x7fffffffll) return WINO_EUNSUPPORTED;
-    const int64_t room = std::min<int64_t>((int64_t)max_pages * c.page_size, 0x7fffffff - 4096);
+    const int64_t room = std::min<int64_t>((int64_t)max_pages * c.page_size, 0x7fffffff - 65536);
     const Cut k = cut(batch, q_len, heads, c.kv_heads, c.head_dim, room);
     if (batch * k.units > 0x7fffffffll) return WINO_EUNSUPPORTED;
     const bool split = k.split && workspace && workspace_bytes >= k.bytes;

@@ -92,10 +92,12 @@ template <int ROWS> __device__ inline bool find(const PromptArgs& a, int index, 
     const int lane = threadIdx.x & 63;
     for (int s0 = 0; s0 < a.seqs; s0 += 64) {
         const int s = s0 + lane;
-        int from = 0, n = 0;
+        int from = 0, n = 0, k0 = 0, k1 = 0;
         if (s < a.seqs) {
             from = max(a.cu_q[s], 0);
             n = max(min(a.cu_q[s + 1], a.total_q) - from, 0);
+            k0 = max(min(a.cu_k[s], a.total_k), 0);
+            k1 = min(a.cu_k[s + 1], a.total_k);
         }
         const int count = (int)(((int64_t)n * a.group + ROWS - 1) / ROWS);
         int before = count;                                 // tiles of this and the sequences before, in the 64
@@ -109,8 +111,8 @@ template <int ROWS> __device__ inline bool find(const PromptArgs& a, int index, 
             w.q0 = __shfl(from, l);
             w.nq = __shfl(n, l);
             w.tile = index - __shfl(before - count, l);
-            w.k0 = max(min(a.cu_k[s0 + l], a.total_k), 0);
-            w.nk = max(min(a.cu_k[s0 + l + 1], a.total_k) - w.k0, 0);
+            w.k0 = __shfl(k0, l);
+            w.nk = max(__shfl(k1, l) - w.k0, 0);
             return true;
         }
         index -= all;

@@ -175,29 +175,37 @@ __global__ __launch_bounds__(64 * V) void w4_matvec_kernel(MatvecArgs a) {
             }
         }
     };
+    // The wave's steps, each workgroup beginning somewhere else: all of them read the same x, and would otherwise ask the
+    // same part of the L2 for it at the same time.
+    const int mine = max(0, (end - begin - wave * 4 + 4 * V - 1) / (4 * V)), turn = mine > 0 ? (int)(blockIdx.x % mine) : 0;
+    auto at = [&](int i) {
+        i += turn;
+        return begin + (wave + V * (i >= mine ? i - mine : i)) * 4;
+    };
     auto sweep = [&](Step (&t)[D], auto split) {
 #pragma unroll
         for (int i = 0; i < R; ++i)
 #pragma unroll
             for (int j = 0; j < N; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int k0 = begin + wave * 4; k0 < end;) {
+        for (int i = 0; i < mine; i += D) {
 #pragma unroll
             for (int d = 0; d < D; ++d) {
-                if (k0 < end) {
-                    compute(k0, t[d], split);
-                    load(k0 + 4 * V * D, t[d]);
+                if (i + d < mine) {
+                    compute(at(i + d), t[d], split);
+                    if (i + d + D < mine) load(at(i + d + D), t[d]);
                 }
-                k0 += 4 * V;
             }
         }
     };
     Step t[D];
 #pragma unroll
-    for (int d = 0; d < D; ++d) load(begin + (wave + d * V) * 4, t[d]);
+    for (int d = 0; d < D; ++d)
+        if (d < mine) load(at(d), t[d]);
     if constexpr (X) {
         const int pieces = (end - begin) * 4, rows = min(16 * N, a.m - tok0);
+        const int skip = pieces > 0 ? (int)(blockIdx.x * 64u % pieces) : 0;
         for (int i = threadIdx.x; i < pieces * rows; i += 64 * V) {
-            const int tok = i / pieces, p = i - tok * pieces;
+            const int tok = i / pieces, q = i - tok * pieces + skip, p = q >= pieces ? q - pieces : q;
             *(T8*)(x_lds + tok * x_row + p * 16) =
                 *(const T8*)((const T*)a.x + (int64_t)(tok0 + tok) * a.x_stride + begin * kGroup + p * 8);
         }
@@ -208,7 +216,8 @@ __global__ __launch_bounds__(64 * V) void w4_matvec_kernel(MatvecArgs a) {
         const uint32_t hi = max(most & 0xffffu, most >> 16), lo = min(least & 0xffffu, least >> 16);
         if (__any(hi > 140u || lo < 104u)) {
 #pragma unroll
-            for (int d = 0; d < D; ++d) load(begin + (wave + d * V) * 4, t[d]);
+            for (int d = 0; d < D; ++d)
+        if (d < mine) load(at(d), t[d]);
             sweep(t, std::true_type{});
         }
     }
@@ -262,28 +271,57 @@ template <int TYPE, int R, int N, int V, int D, bool X> void launch(MatvecArgs a
 }
 
 #ifndef W4_MATVEC_KERNEL_ONLY
-// Parts of k for kernels that take 64 rows of W a workgroup: as many as it takes to have a workgroup for each compute
-// unit, while each part keeps 1024 of k.
-int parts(int32_t n, int32_t k) {
-    const int64_t rows = (n + 63) / 64;
-    return (int)std::max<int64_t>(1, std::min<int64_t>((256 + rows - 1) / rows, k / 1024));
+// How a call is cut: 16 rows of W a workgroup (times `r`), k in `splits` parts, x in LDS or beside the codes.
+struct Cut {
+    int r, splits;
+    bool x;
+    int waves = 8;
+};
+
+// Few workgroups read x few times, many keep the device busy; a second launch, for the join, costs 3 us.  Measured (us,
+// bf16, rows of x / n / k; r and parts):
+//   x in LDS                    1/4096/4096: r1 4.7 (8 waves 5.1)   4/16384/4096: r2 13.0, r1 14.4   1/16384/4096: r2 11.3
+//   x beside the codes          8/4096/4096: r1 6.5, r4 in 4 8.0    8/8192/8192: r2 15.3, r4 in 2 16.5
+//                               16/16384/4096: r4 14.8, r2 17.6     16/2048/8192: r2 in 4 9.2, r4 in 8 9.9
+//                               16/4096/16384: r4 in 4 18.4, r2 in 2 19.9, r1 24   1/1024/16384: r2 in 8 7.9, r1 10.9
+//   more than 16 rows           32/4096/1024: r2 5.2, r4 6.4        32/2048/4096: r2 in 4 8.6, r4 in 4 9.8
+//                               32/8192/8192: r4 in 2 22.2, r2 25.4 64/16384/4096: r4 28, r2 42
+Cut cut(int64_t m, int64_t n, int64_t k) {
+    // as many parts as make a workgroup for each of 256 compute units, no more, with 1024 of k in each at least
+    auto parts = [&](int r) {
+        const int64_t groups = (n + 16 * r - 1) / (16 * r);
+        return (int)std::max<int64_t>(1, std::min<int64_t>(256 / groups, k / 1024));
+    };
+    if (m > 16) {
+        const int r = n <= 2048 || (k < 2048 && n <= 8192) ? 2 : 4;
+        return Cut{r, parts(r), false};
+    }
+    const bool fits = m * (2 * k + 16) <= 40960;
+    if (n <= 2048 && k >= 12288) return Cut{2, parts(2), false};
+    if (fits) return Cut{n <= 8192 ? 1 : 2, 1, true, n <= 4096 ? 16 : 8};
+    if (n <= 4096 && k >= 8192) {
+        const int r = m > 8 && n > 2048 ? 4 : 2;
+        return Cut{r, parts(r), false};
+    }
+    return Cut{n <= 4096 ? 1 : (n <= 8192 ? 2 : 4), 1, false};
 }
 
-// x in LDS where it fits in 40 KB: the workgroup then takes 16 rows of W and nothing but their codes comes from memory
-// in the loop (1 x 4096, n = 16384: 11.6 us, 14.1 with x fetched beside the codes).  More of x is fetched by each
-// workgroup, for 64 rows of W (16 x 16384, n = 4096: 18.6 us in four parts, 24 with 16 rows in one).
-bool x_fits(int32_t m, int32_t k) { return m <= 16 && (int64_t)m * (2 * k + 16) <= 40960; }
-
-template <int TYPE> void pick(const MatvecArgs& a, bool split, hipStream_t stream) {
-    const int splits = split ? parts(a.n, a.k) : 1;
-    if (x_fits(a.m, a.k))
-        launch<TYPE, 1, 1, 8, 2, true>(a, 1, stream);
-    else if (a.m <= 16)
-        launch<TYPE, 4, 1, 8, 2, false>(a, splits, stream);
-    else if (a.m <= 32)
-        launch<TYPE, 4, 2, 8, 2, false>(a, splits, stream);
+template <int TYPE> void pick(const MatvecArgs& a, bool room, hipStream_t stream) {
+    const Cut c = cut(a.m, a.n, a.k);
+    const int s = room ? c.splits : 1;
+    if (a.m > 32)
+        c.r == 2 ? launch<TYPE, 2, 4, 8, 1, false>(a, s, stream) : launch<TYPE, 4, 4, 8, 1, false>(a, s, stream);
+    else if (a.m > 16)
+        c.r == 2 ? launch<TYPE, 2, 2, 8, 2, false>(a, s, stream) : launch<TYPE, 4, 2, 8, 2, false>(a, s, stream);
+    else if (c.x)
+        c.waves == 16 ? launch<TYPE, 1, 1, 16, 2, true>(a, 1, stream)
+                      : (c.r == 1 ? launch<TYPE, 1, 1, 8, 2, true>(a, 1, stream) : launch<TYPE, 2, 1, 8, 2, true>(a, 1, stream));
+    else if (c.r == 1)
+        launch<TYPE, 1, 1, 8, 2, false>(a, s, stream);
+    else if (c.r == 2)
+        launch<TYPE, 2, 1, 8, 2, false>(a, s, stream);
     else
-        launch<TYPE, 4, 4, 4, 1, false>(a, splits, stream);
+        launch<TYPE, 4, 1, 8, 2, false>(a, s, stream);
 }
 #endif
 
@@ -291,8 +329,9 @@ template <int TYPE> void pick(const MatvecArgs& a, bool split, hipStream_t strea
 
 #ifndef W4_MATVEC_KERNEL_ONLY
 extern "C" size_t w4_matvec_workspace_bytes(int32_t m, int32_t n, int32_t k) {
-    if (m < 1 || n < 1 || k < 1 || x_fits(m, k) || parts(n, k) < 2) return 0;
-    return (size_t)parts(n, k) * m * n * sizeof(float);
+    if (m < 1 || n < 1 || k < 1) return 0;
+    const int splits = cut(m, n, k).splits;
+    return splits > 1 ? (size_t)splits * m * n * sizeof(float) : 0;
 }
 
 extern "C" wino_status w4_matvec(const void* x, int64_t x_stride, const uint8_t* codes, const uint8_t* scales,
@@ -306,11 +345,11 @@ extern "C" wino_status w4_matvec(const void* x, int64_t x_stride, const uint8_t*
     if (m > 65535 || n > (1 << 24) || k > (1 << 20)) return WINO_EUNSUPPORTED;
     if (!aligned16(x) || !aligned16(codes) || !aligned16(workspace) || (k > 0 && m > 1 && (x_stride & 7))) return WINO_EUNSUPPORTED;
     MatvecArgs a = {x, codes, scales, bias, y, x_stride, y_stride, m, n, k, 0, (float*)workspace};
-    const bool split = workspace && workspace_bytes >= w4_matvec_workspace_bytes(m, n, k);
+    const bool room = workspace && workspace_bytes >= w4_matvec_workspace_bytes(m, n, k);
     if (type == WINO_BF16)
-        pick<WINO_BF16>(a, split, stream);
+        pick<WINO_BF16>(a, room, stream);
     else
-        pick<WINO_FP16>(a, split, stream);
+        pick<WINO_FP16>(a, room, stream);
     return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
 }
 #endif
