@@ -175,12 +175,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
 
-    int b, unit, blk, left, share = 0;                      // left: blocks of the share still to do
+    int b, unit, blk, len, left, share = 0;                 // left: blocks of the share still to do
     if (a.part) {
         const Place p = find(a, blockIdx.x);
         if (p.b >= a.batch) return;
         b = p.b;
-        const int n = __builtin_amdgcn_readfirstlane(blocks(length(a, b)));
+        len = __builtin_amdgcn_readfirstlane(length(a, b));
+        const int n = blocks(len);
         const int64_t in = p.share * blockIdx.x - p.before * a.units;
         unit = __builtin_amdgcn_readfirstlane((int)(in / n));
         blk = __builtin_amdgcn_readfirstlane((int)(in - (int64_t)unit * n));
@@ -189,11 +190,12 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
         b = blockIdx.x / a.units;
         unit = blockIdx.x % a.units;
         blk = 0;
-        left = __builtin_amdgcn_readfirstlane(blocks(length(a, b)));
+        len = __builtin_amdgcn_readfirstlane(length(a, b));
+        left = blocks(len);
     }
     bool opening = true;                                    // the first unit of the share
     for (;;) {
-    const int len = __builtin_amdgcn_readfirstlane(length(a, b)), n_blocks = blocks(len);
+    const int n_blocks = blocks(len);
     const int take = min(left, n_blocks - blk);
     const bool is_part = take < n_blocks;
     if (a.part && blk == 0 && threadIdx.x == 0)
@@ -451,6 +453,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
     if (++unit == a.units) {
         unit = 0;
         if (++b == a.batch) return;
+        len = __builtin_amdgcn_readfirstlane(length(a, b));
     }
     __syncthreads();
     }
