@@ -48,7 +48,8 @@ struct DecodeArgs {
     int32_t groups;         // workgroups
     int32_t room;           // tokens that a table has room for
     FastDiv by_page;
-    float scale_log2;       // scale * log2(e): probabilities are powers of two
+    float scale_log2;       // |scale| * log2(e), 1 for a scale of 0: probabilities are powers of two
+    uint32_t q_and, q_xor;  // the scale's sign, or its being 0, put into pairs of query elements
 };
 
 __device__ inline int fast_div(int n, FastDiv f) {
@@ -218,7 +219,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
                      g * (DIM / 4);
 #pragma unroll
         for (int j = 0; j < S::kSteps; ++j) {
-            const T8 x = *(const T8*)(p + 8 * j);
+            const T8 x = __builtin_bit_cast(T8, (*(const u32x4*)(p + 8 * j) & a.q_and) ^ a.q_xor);
             if constexpr (TYPE == WINO_BF16) {
                 q[0][j] = x;
             } else {
@@ -291,7 +292,6 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
                 for (int p = 0; p < kParts; ++p)
                     z[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[p][j], z[n], 0, 0, 0);
             }
-            z[n] *= a.scale_log2;
         }
         // the next step's codes are on their way as soon as the registers of this one's are free
         int64_t at[S::kTiles];
@@ -335,9 +335,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
         }
         float top = kNever;
 #pragma unroll
-        for (int n = 0; n < S::kTiles; ++n)
-            top = __builtin_fmaxf(__builtin_fmaxf(top, __builtin_fmaxf(z[n][0], z[n][1])), __builtin_fmaxf(z[n][2], z[n][3]));
-        top = max_rows(top);
+        for (int n = 0; n < S::kTiles; ++n) top = max3(max3(z[n][0], z[n][1], z[n][2]), z[n][3], top);
+        top = max_rows(top) * a.scale_log2;
         // o and sum move to a new reference only where the maximum has outgrown the old one by 2^8
         if (__any(top > ref + 8.f)) {
             const float to = __builtin_fmaxf(ref, top);
@@ -347,13 +346,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
 #pragma unroll
             for (int n = 0; n < DIM / 16; ++n) o[n] *= alpha;
         }
-        const float base = ref == kNever ? 0.f : ref;
+        const float base = ref == kNever ? 0.f : -ref;
         uint32_t hi[S::kTiles][2], lo[S::kTiles][2];
 #pragma unroll
         for (int n = 0; n < S::kTiles; ++n)
 #pragma unroll
             for (int e = 0; e < 4; e += 2) {
-                const float p0 = __builtin_amdgcn_exp2f(z[n][e] - base), p1 = __builtin_amdgcn_exp2f(z[n][e + 1] - base);
+                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[n][e], a.scale_log2, base));
+                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[n][e + 1], a.scale_log2, base));
                 sum += p0 + p1;
                 const bf16x2 x = {(__bf16)p0, (__bf16)p1};
                 const bf16x2 y = {(__bf16)(p0 - (float)x[0]), (__bf16)(p1 - (float)x[1])};
@@ -611,7 +611,10 @@ extern "C" wino_status kv4_attention(const void* q, int64_t q_stride, const kv4_
                     split ? (float*)workspace : nullptr, q_stride, c.pages, q_len, heads, c.kv_heads,
                     heads / c.kv_heads, c.page_size, max_pages, (int32_t)k.tiles, batch, (int32_t)k.units,
                     (int32_t)(split ? k.groups : batch * k.units), (int32_t)room,
-                    winof4::make_fastdiv((uint32_t)c.page_size), scale * 1.44269504088896340736f};
+                    winof4::make_fastdiv((uint32_t)c.page_size),
+                    scale == 0.f ? 1.f : __builtin_fabsf(scale) * 1.44269504088896340736f, scale == 0.f ? 0u : 0xffffffffu,
+                    scale < 0.f ? 0x80008000u : 0u};
+    if (a.scale_log2 - a.scale_log2 != 0.f) return WINO_EUNSUPPORTED;       // past fp32's range
     return type == WINO_BF16 ? launch_dim<WINO_BF16>(c.head_dim, a, rows, stream)
                              : launch_dim<WINO_FP16>(c.head_dim, a, rows, stream);
 }

@@ -102,8 +102,8 @@ __device__ inline float max3(float a, float b, float c) {
 // Maximum and sum over the four 16-lane rows of a wave, lane by lane.
 __device__ inline float max_rows(float x) {
     const f32x2 a = swap_rows<2>(x);
-    const f32x2 b = swap_rows<1>(__builtin_fmaxf(a[0], a[1]));
-    return __builtin_fmaxf(b[0], b[1]);
+    const f32x2 b = swap_rows<1>(max3(a[0], a[1], a[1]));
+    return max3(b[0], b[1], b[1]);
 }
 __device__ inline float sum_rows(float x) {
     const f32x2 a = swap_rows<2>(x);
