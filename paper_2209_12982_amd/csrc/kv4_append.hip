@@ -23,7 +23,6 @@ struct AppendArgs {
     uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
     int64_t q_stride, k_stride, v_stride, slot_end, threads;
     int32_t heads, kv_heads, dim, rot, table_rows, page, values;
-    int32_t large;          // outputs that no L2 holds until somebody reads them: they do not go through it
 };
 
 // The bytes bound it: every value is read once and written once in 16 bits,
@@ -32,7 +31,8 @@ struct AppendArgs {
 // wave.  With halves rotated it reads the 8 partners too (from the cache:
 // another thread reads them as its own), which needs neither LDS nor a barrier.
 // 8200 tokens of 32 + 2 x 8 heads of 128: 50.7 us, 4.2 TB/s.
-template <int TYPE, int ROTARY>
+// LARGE: outputs that no L2 holds until somebody reads them do not go through it (53.3 us otherwise).
+template <int TYPE, int ROTARY, bool LARGE>
 __global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
 #pragma clang fp contract(off)
     typedef typename Half<TYPE>::type T;
@@ -116,11 +116,19 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
         T8 t;
         for (int i = 0; i < 8; ++i) t[i] = (T)x[i];
         T8* at = (T8*)(out + (tok * (kind == 0 ? a.heads : a.kv_heads) + h) * a.dim + d0);
-        if (a.large)
+        if constexpr (LARGE)
             __builtin_nontemporal_store(t, at);
         else
             *at = t;
     }
+}
+
+template <int TYPE, int ROTARY> void launch(const AppendArgs& a, bool large, hipStream_t stream) {
+    const dim3 grid((unsigned)((a.threads + 255) / 256)), block(256);
+    if (large)
+        hipLaunchKernelGGL((kv4_append_kernel<TYPE, ROTARY, true>), grid, block, 0, stream, a);
+    else
+        hipLaunchKernelGGL((kv4_append_kernel<TYPE, ROTARY, false>), grid, block, 0, stream, a);
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
@@ -155,21 +163,14 @@ extern "C" wino_status kv4_append(const void* q, int64_t q_stride, const void* k
     AppendArgs a = {q, k, v, q_out, k_out, v_out, cos_sin, positions, slots,
                     c.k_codes, c.k_scales, c.v_codes, c.v_scales, q_stride, k_stride, v_stride,
                     c.pages * c.page_size, (int64_t)tokens * (heads + 2 * c.kv_heads) * (dim / 8),
-                    heads, c.kv_heads, c.head_dim, rot, table_rows, c.page_size, values, 0};
-    a.large = a.threads * 16 > 32 << 20;        // 8200 tokens of 32 + 2 x 8 heads of 128: 50.7 us, 53.3 through the L2
-    const int64_t blocks = (a.threads + 255) / 256;
-    if (blocks > 0x7fffffffll) return WINO_EUNSUPPORTED;
-    const dim3 grid((unsigned)blocks), block(256);
-    if (type == WINO_BF16) {
-        if (rotary == WINO_ROTARY_HALVES)
-            hipLaunchKernelGGL((kv4_append_kernel<WINO_BF16, WINO_ROTARY_HALVES>), grid, block, 0, stream, a);
-        else
-            hipLaunchKernelGGL((kv4_append_kernel<WINO_BF16, WINO_ROTARY_PAIRS>), grid, block, 0, stream, a);
-    } else {
-        if (rotary == WINO_ROTARY_HALVES)
-            hipLaunchKernelGGL((kv4_append_kernel<WINO_FP16, WINO_ROTARY_HALVES>), grid, block, 0, stream, a);
-        else
-            hipLaunchKernelGGL((kv4_append_kernel<WINO_FP16, WINO_ROTARY_PAIRS>), grid, block, 0, stream, a);
-    }
+                    heads, c.kv_heads, c.head_dim, rot, table_rows, c.page_size, values};
+    if ((a.threads + 255) / 256 > 0x7fffffffll) return WINO_EUNSUPPORTED;
+    const bool large = a.threads * 16 > 32 << 20;
+    if (type == WINO_BF16)
+        rotary == WINO_ROTARY_HALVES ? launch<WINO_BF16, WINO_ROTARY_HALVES>(a, large, stream)
+                                     : launch<WINO_BF16, WINO_ROTARY_PAIRS>(a, large, stream);
+    else
+        rotary == WINO_ROTARY_HALVES ? launch<WINO_FP16, WINO_ROTARY_HALVES>(a, large, stream)
+                                     : launch<WINO_FP16, WINO_ROTARY_PAIRS>(a, large, stream);
     return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
 }
