@@ -83,8 +83,9 @@ template <> struct Mfma<WINO_FP16> {
     static __device__ f32x16 mul(T8 a, T8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
-// The sequence and the tile of its rows that workgroup `index` takes, or false past the last.  Offsets are cut to the
-// tensor.
+// The sequence and the tile of its rows that workgroup `index` takes, or false past the last.  Those that see the most
+// keys come first, so that the device is full to the end: among each 64 sequences the longest one's tiles, from its end
+// to its beginning, then the next one's.  Offsets are cut to the tensor.
 struct Work {
     int q0, nq, k0, nk, tile;
 };
@@ -100,19 +101,21 @@ template <int ROWS> __device__ inline bool find(const PromptArgs& a, int index, 
             k1 = min(a.cu_k[s + 1], a.total_k);
         }
         const int count = (int)(((int64_t)n * a.group + ROWS - 1) / ROWS);
-        int before = count;                                 // tiles of this and the sequences before, in the 64
-        for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(before, o);
-            if (lane >= o) before += x;
+        // the 64 sequences by their keys, the longest first: tiles before this lane's, and all of them
+        const int keys = k1 - k0;
+        int before = 0, all = 0;
+        for (int j = 0; j < min(64, a.seqs - s0); ++j) {
+            const int other = __builtin_amdgcn_readlane(keys, j), tiles = __builtin_amdgcn_readlane(count, j);
+            before += other > keys || (other == keys && j < lane) ? tiles : 0;
+            all += tiles;
         }
-        const int all = __shfl(before, 63);
         if (index < all) {
-            const int l = __builtin_ctzll(__ballot(index < before));
+            const int l = __builtin_ctzll(__ballot(index >= before && index < before + count));
             w.q0 = __shfl(from, l);
             w.nq = __shfl(n, l);
-            w.tile = index - __shfl(before - count, l);
+            w.tile = __shfl(before + count, l) - 1 - index;
             w.k0 = __shfl(k0, l);
-            w.nk = max(__shfl(k1, l) - w.k0, 0);
+            w.nk = max(__shfl(keys, l), 0);
             return true;
         }
         index -= all;
@@ -137,11 +140,10 @@ __global__ __launch_bounds__((64 * Shape<DIM, ROWS, TEAMS, KEYS>::kWaves), 2) vo
     const int c = lane & 31, half = lane >> 5;
     const int team = wave / S::kTeam, mate = wave % S::kTeam, d0 = mate / S::kBlocks * (S::kOut * 32);   // d0: first dimension
 
-    // Workgroups that follow each other run on different XCDs: a K and V stays with one or two of them.  Late tiles,
-    // which see the most keys, come first.
-    const int kvh = blockIdx.x % a.kv_heads, tiles = gridDim.x / a.kv_heads;
+    // Workgroups that follow each other run on different XCDs: a K and V stays with one or two of them.
+    const int kvh = blockIdx.x % a.kv_heads;
     Work w;
-    if (!find<ROWS>(a, tiles - 1 - (int)(blockIdx.x / a.kv_heads), w)) return;
+    if (!find<ROWS>(a, blockIdx.x / a.kv_heads, w)) return;
     w.q0 = __builtin_amdgcn_readfirstlane(w.q0), w.nq = __builtin_amdgcn_readfirstlane(w.nq);
     w.k0 = __builtin_amdgcn_readfirstlane(w.k0), w.nk = __builtin_amdgcn_readfirstlane(w.nk);
     w.tile = __builtin_amdgcn_readfirstlane(w.tile);
