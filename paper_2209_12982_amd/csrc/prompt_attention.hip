@@ -32,6 +32,7 @@ struct PromptArgs {
     const int32_t *cu_q, *cu_k;
     int64_t q_stride, k_stride, v_stride;
     int32_t seqs, total_q, total_k, heads, kv_heads, group, causal;
+    winof4::FastDiv by_group;
     float scale_log2;       // |scale| * log2(e), 1 for a scale of 0: probabilities are powers of two
     uint32_t q_and, q_xor;  // the scale's sign, or its being 0, put into pairs of query elements
 };
@@ -100,7 +101,7 @@ template <int ROWS> __device__ inline bool find(const PromptArgs& a, int index, 
             k0 = max(min(a.cu_k[s], a.total_k), 0);
             k1 = min(a.cu_k[s + 1], a.total_k);
         }
-        const int count = (int)(((int64_t)n * a.group + ROWS - 1) / ROWS);
+        const int count = (n * a.group + ROWS - 1) / ROWS;
         // the 64 sequences by their keys, the longest first: tiles before this lane's, and all of them
         const int keys = k1 - k0;
         int before = 0, all = 0;
@@ -149,18 +150,18 @@ __global__ __launch_bounds__((64 * Shape<DIM, ROWS, TEAMS, KEYS>::kWaves), 2) vo
     w.tile = __builtin_amdgcn_readfirstlane(w.tile);
 
     // row r is query r / group, head r % group of the heads at kvh
-    const int64_t rows = (int64_t)w.nq * a.group, r0 = (int64_t)w.tile * ROWS, rw = r0 + 32 * (mate % S::kBlocks);
+    const int rows = w.nq * a.group, r0 = w.tile * ROWS, rw = r0 + 32 * (mate % S::kBlocks);
     const int shift = a.causal ? w.nk - w.nq + 1 : w.nk;    // query i sees shift + i keys (all, where not causal)
-    auto sees = [&](int64_t row) {
-        const int i = (int)(row / a.group);
+    auto sees = [&](int row) {
+        const int i = (int)winof4::fast_div((uint32_t)row, a.by_group);
         return max(0, a.causal ? min(shift + i, w.nk) : w.nk);
     };
     const int every = sees(r0);                             // keys that all rows of the workgroup see
     const int end = sees(min(r0 + ROWS, rows) - 1);         // keys that some row sees
     const int wave_every = sees(rw), wave_end = rw < rows ? sees(min(rw + 32, rows) - 1) : 0;
     const bool real = rw + c < rows;
-    const int64_t row = real ? rw + c : rows - 1;           // this lane's row
-    const int i = (int)(row / a.group), h = kvh * a.group + (int)(row - (int64_t)i * a.group);
+    const int row = real ? rw + c : rows - 1;               // this lane's row
+    const int i = (int)winof4::fast_div((uint32_t)row, a.by_group), h = kvh * a.group + row - i * a.group;
     const int row_end = real ? sees(row) : 0;
 
     T8 q[DIM / 16];
@@ -445,6 +446,7 @@ extern "C" wino_status prompt_attention(const void* q, int64_t q_stride, const v
     if (head_dim != 64 && head_dim != 96 && head_dim != 128 && head_dim != 192 && head_dim != 256)
         return WINO_EUNSUPPORTED;
     if (seqs > 65536 || heads > 65536 || total_q > 0x7fffffff - 4096 || total_k > 0x7fffffff - 4096) return WINO_EUNSUPPORTED;
+    if ((int64_t)total_q * (heads / kv_heads) > 0x7fffffff - 4096) return WINO_EUNSUPPORTED;     // rows are counted in 32 bits
     if (total_q == 0 || seqs == 0) return WINO_OK;
     if (!q || !out || (total_k > 0 && (!k || !v)) || !cu_q || !cu_k) return WINO_EINVAL;
     const int64_t dim = head_dim;
@@ -455,7 +457,8 @@ extern "C" wino_status prompt_attention(const void* q, int64_t q_stride, const v
         !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
         return WINO_EUNSUPPORTED;
     PromptArgs a = {q, k, v, out, cu_q, cu_k, q_stride, k_stride, v_stride, seqs, total_q, total_k,
-                    heads, kv_heads, heads / kv_heads, causal, 0.f, scale == 0.f ? 0u : 0xffffffffu, scale < 0.f ? 0x80008000u : 0u};
+                    heads, kv_heads, heads / kv_heads, causal, winof4::make_fastdiv((uint32_t)(heads / kv_heads)), 0.f,
+                    scale == 0.f ? 0u : 0xffffffffu, scale < 0.f ? 0x80008000u : 0u};
     a.scale_log2 = scale == 0.f ? 1.f : __builtin_fabsf(scale) * 1.44269504088896340736f;
     if (a.scale_log2 - a.scale_log2 != 0.f) return WINO_EUNSUPPORTED;       // past fp32's range
     return type == WINO_BF16 ? launch_dim<WINO_BF16>(head_dim, a, max_q, stream)
