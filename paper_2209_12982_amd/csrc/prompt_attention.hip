@@ -383,16 +383,24 @@ __global__ __launch_bounds__((64 * Shape<DIM, ROWS, TEAMS, KEYS>::kWaves), 2) vo
         const f32x2 x = swap_rows<2>(sum);
         sum = x[0] + x[1];
     }
-    if (real && team == 0) {
-        typedef T T4 __attribute__((ext_vector_type(4)));
+    if (team == 0) {
+        // the halves of the wave exchange four dimensions of sixteen, so that a lane stores eight neighbours
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        T* out = (T*)a.out + ((int64_t)(w.q0 + i) * a.heads + h) * DIM + d0 + 4 * half;
+        T* out = (T*)a.out + ((int64_t)(w.q0 + i) * a.heads + h) * DIM + d0 + 8 * half;
 #pragma unroll
         for (int n = 0; n < S::kOut; ++n)
 #pragma unroll
-            for (int e = 0; e < 16; e += 4)
-                *(T4*)(out + 32 * n + 2 * e) =
-                    sum == 0.f ? T4{} : T4{(T)(o[n][e] * inv), (T)(o[n][e + 1] * inv), (T)(o[n][e + 2] * inv), (T)(o[n][e + 3] * inv)};
+            for (int e = 0; e < 16; e += 8) {
+                uint32_t y[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const T2 x = {(T)(o[n][e + 2 * k] * inv), (T)(o[n][e + 2 * k + 1] * inv)};
+                    y[k] = sum == 0.f ? 0u : __builtin_bit_cast(uint32_t, x);
+                }
+                const auto s02 = __builtin_amdgcn_permlane32_swap(y[0], y[2], false, false);
+                const auto s13 = __builtin_amdgcn_permlane32_swap(y[1], y[3], false, false);
+                if (real) *(u32x4*)(out + 32 * n + 2 * e) = u32x4{s02[0], s13[0], s02[1], s13[1]};
+            }
     }
 }
 
