@@ -8,7 +8,10 @@
 // the compiler groups them, and a key always gets the same code.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "mx4.h"
+#include "wino_device.h"
 #include "winof4.h"
 
 namespace {
@@ -21,8 +24,10 @@ struct AppendArgs {
     const int32_t* positions;
     const int64_t* slots;
     uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
-    int64_t q_stride, k_stride, v_stride, slot_end, threads;
+    int64_t q_stride, k_stride, v_stride, slot_end;
+    int32_t first, threads;     // of a launch: its first token, and its threads (a multiple of 4)
     int32_t heads, kv_heads, dim, rot, table_rows, page, values;
+    winof4::FastDiv by_eights, by_heads, by_page;       // by dim / 8, by the heads of q, k and v together, by page
 };
 
 // The bytes bound it: every value is read once and written once in 16 bits,
@@ -30,21 +35,21 @@ struct AppendArgs {
 // one head of one token; the four threads of a 32-group are neighbours in a
 // wave.  With halves rotated it reads the 8 partners too (from the cache:
 // another thread reads them as its own), which needs neither LDS nor a barrier.
-// 8200 tokens of 32 + 2 x 8 heads of 128: 50.7 us, 4.2 TB/s.
-// LARGE: outputs that no L2 holds until somebody reads them do not go through it (53.3 us otherwise).
+// Its indices are 32 bits wide, divided by multiplying: with 64-bit divisions it
+// took 50.0 us for 8200 tokens of 32 + 2 x 8 heads of 128, now 46.2, 4.6 TB/s
+// (a large copy: 4.9).
+// LARGE: outputs that no L2 holds until somebody reads them do not go through it, 2.6 us of those 50.
 template <int TYPE, int ROTARY, bool LARGE>
 __global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
 #pragma clang fp contract(off)
     typedef typename Half<TYPE>::type T;
     typedef T T8 __attribute__((ext_vector_type(8)));
-    const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (gid >= a.threads) return;                     // whole groups of four: threads is a multiple of 4
-    const int chunks = a.dim / 8;
-    const int all = a.heads + 2 * a.kv_heads;
-    const int64_t th = gid / chunks;
-    const int d0 = (int)(gid - th * chunks) * 8;
-    const int64_t tok = th / all;
-    int h = (int)(th - tok * all);
+    const uint32_t gid = blockIdx.x * 256 + threadIdx.x;
+    if (gid >= (uint32_t)a.threads) return;           // whole groups of four
+    const uint32_t th = winof4::fast_div(gid, a.by_eights), t = winof4::fast_div(th, a.by_heads);
+    const int d0 = (int)(gid - th * a.by_eights.d) * 8;
+    const int64_t tok = a.first + (int)t;
+    int h = (int)(th - t * a.by_heads.d);
     const int kind = h < a.heads ? 0 : (h < a.heads + a.kv_heads ? 1 : 2);
     h -= kind == 0 ? 0 : (kind == 1 ? a.heads : a.heads + a.kv_heads);
     const T* src = kind == 0 ? (const T*)a.q + tok * a.q_stride
@@ -102,7 +107,7 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
         for (int i = 0; i < 8; ++i) word |= (s == 255u ? 0u : encode(x[i], inv)) << (4 * i);
         const int64_t slot = a.slots[tok];
         if (placed && slot >= 0 && slot < a.slot_end) {
-            const int64_t pg = slot / a.page;
+            const int64_t pg = slot >> 31 ? slot / a.page : winof4::fast_div((uint32_t)slot, a.by_page);
             const int64_t at = (pg * a.kv_heads + h) * a.page + (slot - pg * a.page);
             *(uint32_t*)((kind == 1 ? a.k_codes : a.v_codes) + at * (a.dim / 2) + d0 / 2) = word;
             if (d0 % kGroup == 0) (kind == 1 ? a.k_scales : a.v_scales)[at * (a.dim / kGroup) + d0 / kGroup] = (uint8_t)s;
@@ -162,15 +167,22 @@ extern "C" wino_status kv4_append(const void* q, int64_t q_stride, const void* k
         return WINO_EUNSUPPORTED;
     AppendArgs a = {q, k, v, q_out, k_out, v_out, cos_sin, positions, slots,
                     c.k_codes, c.k_scales, c.v_codes, c.v_scales, q_stride, k_stride, v_stride,
-                    c.pages * c.page_size, (int64_t)tokens * (heads + 2 * c.kv_heads) * (dim / 8),
-                    heads, c.kv_heads, c.head_dim, rot, table_rows, c.page_size, values};
-    if ((a.threads + 255) / 256 > 0x7fffffffll) return WINO_EUNSUPPORTED;
-    const bool large = a.threads * 16 > 32 << 20;
-    if (type == WINO_BF16)
-        rotary == WINO_ROTARY_HALVES ? launch<WINO_BF16, WINO_ROTARY_HALVES>(a, large, stream)
-                                     : launch<WINO_BF16, WINO_ROTARY_PAIRS>(a, large, stream);
-    else
-        rotary == WINO_ROTARY_HALVES ? launch<WINO_FP16, WINO_ROTARY_HALVES>(a, large, stream)
-                                     : launch<WINO_FP16, WINO_ROTARY_PAIRS>(a, large, stream);
-    return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
+                    c.pages * c.page_size, 0, 0, heads, c.kv_heads, c.head_dim, rot, table_rows, c.page_size, values,
+                    winof4::make_fastdiv((uint32_t)(dim / 8)), winof4::make_fastdiv((uint32_t)(heads + 2 * c.kv_heads)),
+                    winof4::make_fastdiv((uint32_t)c.page_size)};
+    // threads of a token; as many tokens a launch as 32 bits count the threads of
+    const int64_t each = (int64_t)(heads + 2 * c.kv_heads) * (dim / 8), most = (1 << 30) / each;
+    const bool large = tokens * each * 16 > 32 << 20;
+    for (int64_t t0 = 0; t0 < tokens; t0 += most) {
+        a.first = (int32_t)t0;
+        a.threads = (int32_t)(std::min<int64_t>(most, tokens - t0) * each);
+        if (type == WINO_BF16)
+            rotary == WINO_ROTARY_HALVES ? launch<WINO_BF16, WINO_ROTARY_HALVES>(a, large, stream)
+                                         : launch<WINO_BF16, WINO_ROTARY_PAIRS>(a, large, stream);
+        else
+            rotary == WINO_ROTARY_HALVES ? launch<WINO_FP16, WINO_ROTARY_HALVES>(a, large, stream)
+                                         : launch<WINO_FP16, WINO_ROTARY_PAIRS>(a, large, stream);
+        if (hipGetLastError() != hipSuccess) return WINO_EHIP;
+    }
+    return WINO_OK;
 }
