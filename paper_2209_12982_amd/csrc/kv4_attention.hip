@@ -22,8 +22,8 @@
 #include <algorithm>
 
 #include "mx4.h"
+#include "wino_device.h"
 #include "winof4.h"
-#include "winof4_internal.h"
 
 namespace {
 using namespace mx4;
@@ -47,14 +47,14 @@ struct DecodeArgs {
     int32_t units;          // of a sequence: kv_heads * tiles
     int32_t groups;         // workgroups
     int32_t room;           // tokens that a table has room for
-    FastDiv by_page;
+    FastDiv by_page, by_group, by_tiles, by_units, by_heads, by_q;
     float scale_log2;       // |scale| * log2(e), 1 for a scale of 0: probabilities are powers of two
     uint32_t q_and, q_xor;  // the scale's sign, or its being 0, put into pairs of query elements
 };
 
-__device__ inline int fast_div(int n, FastDiv f) {
-    return f.d == 1 ? n : (int)((uint32_t)(((uint64_t)(uint32_t)n * f.mul) >> 32) >> f.shr);
-}
+__device__ inline int divide(int n, FastDiv f) { return (int)winof4::fast_div((uint32_t)n, f); }
+// For what hardly ever passes 32 bits (n is not negative).
+__device__ inline int64_t divide(int64_t n, int d) { return n >> 31 ? n / d : (int64_t)((uint32_t)n / (uint32_t)d); }
 
 template <int DIM, int WAVES = 4> struct Shape {
     static constexpr int kSteps = DIM / 32;                 // products of 32 dimensions
@@ -139,7 +139,7 @@ __device__ inline Place find(const DecodeArgs& a, int w) {
     int64_t total = 0;
     for (int b0 = 0; b0 < a.batch; b0 += 64) total += scan(b0);
     Place p;
-    p.share = (total * a.units + a.groups - 1) / a.groups;
+    p.share = divide(total * a.units + a.groups - 1, a.groups);
     p.b = a.batch;
     p.before = 0;
     const int64_t first = p.share * w;
@@ -184,12 +184,12 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
         len = __builtin_amdgcn_readfirstlane(length(a, b));
         const int n = blocks(len);
         const int64_t in = p.share * blockIdx.x - p.before * a.units;
-        unit = __builtin_amdgcn_readfirstlane((int)(in / n));
+        unit = __builtin_amdgcn_readfirstlane((int)divide(in, n));
         blk = __builtin_amdgcn_readfirstlane((int)(in - (int64_t)unit * n));
         share = left = __builtin_amdgcn_readfirstlane((int)p.share);
     } else {
-        b = blockIdx.x / a.units;
-        unit = blockIdx.x % a.units;
+        b = divide((int)blockIdx.x, a.by_units);
+        unit = (int)blockIdx.x - b * a.units;
         blk = 0;
         len = __builtin_amdgcn_readfirstlane(length(a, b));
         left = blocks(len);
@@ -202,14 +202,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
     if (a.part && blk == 0 && threadIdx.x == 0)
         unit_parts(a, DIM)[(int64_t)b * a.units + unit] =
             Parts{(int)blockIdx.x, (int)blockIdx.x + (n_blocks - take + share - 1) / share, opening ? 0 : 1, 0};
-    const int tile = unit % a.tiles, kvh = unit / a.tiles;
+    const int kvh = divide(unit, a.by_tiles), tile = unit - kvh * a.tiles;
     const int first_end = len - a.q_len + 1;                // tokens that query 0 sees; every row sees those
     const int begin = max(blk - 1, 0) * kBlock;
     const int end = a.pages == 0 ? begin : min((int64_t)len, (int64_t)(blk + take - 1) * kBlock);
 
     // this lane's row: query i, head h
     const int row = tile * 16 + r;
-    const int i = row / a.group, h = kvh * a.group + row % a.group;
+    const int i = divide(row, a.by_group), h = kvh * a.group + row - i * a.group;
     const bool real = i < a.q_len;
     const int row_end = real ? (first_end + i < len ? first_end + i : len) : 0;
 
@@ -250,7 +250,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
         int64_t id = -1;
         int pg = 0;
         if (t < end) {
-            pg = fast_div(t, a.by_page);
+            pg = divide(t, a.by_page);
             id = pages[pg];
         }
         const bool ok = id >= 0 && id < a.pages;
@@ -441,9 +441,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
             }
         } else {
             typedef T T4 __attribute__((ext_vector_type(4)));
-            const int ro = tile * 16 + rr;
+            const int ro = tile * 16 + rr, io = divide(ro, a.by_group);
             const T4 y = total == 0.f ? T4{} : T4{(T)(acc[0] / total), (T)(acc[1] / total), (T)(acc[2] / total), (T)(acc[3] / total)};
-            *(T4*)((T*)a.out + (((int64_t)b * a.q_len + ro / a.group) * a.heads + kvh * a.group + ro % a.group) * DIM + d) = y;
+            *(T4*)((T*)a.out + (((int64_t)b * a.q_len + io) * a.heads + kvh * a.group + ro - io * a.group) * DIM + d) = y;
         }
     }
     left -= take;
@@ -467,11 +467,10 @@ template <int TYPE, int DIM> __global__ __launch_bounds__(256) void kv4_join_ker
     constexpr int kCols = DIM / 4, kTeams = 256 / kCols;
     __shared__ f32x4 acc_s[kTeams][kCols];
     __shared__ float m_s[kTeams], total_s[kTeams];
-    const int h = blockIdx.x % a.heads;
-    const int64_t token = blockIdx.x / a.heads;
-    const int b = (int)(token / a.q_len), i = (int)(token % a.q_len);
-    const int row = i * a.group + h % a.group;
-    const int unit = h / a.group * a.tiles + row / 16;
+    const int token = divide((int)blockIdx.x, a.by_heads), h = (int)blockIdx.x - token * a.heads;
+    const int b = divide(token, a.by_q), i = token - b * a.q_len, kvh = divide(h, a.by_group);
+    const int row = i * a.group + h - kvh * a.group;
+    const int unit = kvh * a.tiles + row / 16;
     const Parts p = unit_parts(a, DIM)[(int64_t)b * a.units + unit];
     const int w0 = p.first, w1 = p.last;
     if (w0 == w1) return;                                   // whole, and in the output already
@@ -524,7 +523,7 @@ template <int TYPE, int DIM> __global__ __launch_bounds__(256) void kv4_join_ker
         acc += f * acc_s[t][threadIdx.x];
     }
     const T4 y = total == 0.f ? T4{} : T4{(T)(acc[0] / total), (T)(acc[1] / total), (T)(acc[2] / total), (T)(acc[3] / total)};
-    *(T4*)((T*)a.out + (token * a.heads + h) * DIM + 4 * threadIdx.x) = y;
+    *(T4*)((T*)a.out + ((int64_t)token * a.heads + h) * DIM + 4 * threadIdx.x) = y;
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
@@ -611,7 +610,9 @@ extern "C" wino_status kv4_attention(const void* q, int64_t q_stride, const kv4_
                     split ? (float*)workspace : nullptr, q_stride, c.pages, q_len, heads, c.kv_heads,
                     heads / c.kv_heads, c.page_size, max_pages, (int32_t)k.tiles, batch, (int32_t)k.units,
                     (int32_t)(split ? k.groups : batch * k.units), (int32_t)room,
-                    winof4::make_fastdiv((uint32_t)c.page_size),
+                    winof4::make_fastdiv((uint32_t)c.page_size), winof4::make_fastdiv((uint32_t)(heads / c.kv_heads)),
+                    winof4::make_fastdiv((uint32_t)k.tiles), winof4::make_fastdiv((uint32_t)k.units),
+                    winof4::make_fastdiv((uint32_t)heads), winof4::make_fastdiv((uint32_t)q_len),
                     scale == 0.f ? 1.f : __builtin_fabsf(scale) * 1.44269504088896340736f, scale == 0.f ? 0u : 0xffffffffu,
                     scale < 0.f ? 0x80008000u : 0u};
     if (a.scale_log2 - a.scale_log2 != 0.f) return WINO_EUNSUPPORTED;       // past fp32's range
