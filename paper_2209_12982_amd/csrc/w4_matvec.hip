@@ -39,60 +39,33 @@ struct MatvecArgs {
     float* part;            // [parts][m][n], or null
 };
 
-// R tiles of 16 rows of W, N tiles of 16 rows of x, V waves that share out k, D
-// steps of codes on their way.  X: x lies in LDS; else its pieces come with the
-// codes.  blockIdx.z takes `steps` steps of k; where there are several, their
-// sums go to a.part and w4_matvec_join adds them up.
-template <int TYPE, int R, int N, int V, int D, bool X>
-__global__ __launch_bounds__(64 * V) void w4_matvec_kernel(MatvecArgs a) {
-    typedef typename Half<TYPE>::type T;
-    typedef T T8 __attribute__((ext_vector_type(8)));
-    __shared__ float join[V][R * 16][N * 16 + 1];
-    extern __shared__ __attribute__((aligned(16))) uint8_t x_lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r = lane & 15, g = lane >> 4;
-    const int row0 = blockIdx.x * (16 * R), tok0 = blockIdx.y * (16 * N);
-    const int groups = a.k / kGroup;
-    const int begin = blockIdx.z * a.steps * 4, end = min(groups, begin + a.steps * 4);
+// One step (128 of k, four groups) of R tiles of 16 rows of W: lane (r, g) holds group g of row r, so that a row's four
+// lanes read one piece of memory.
+template <int R> struct Step {
+    u32x4 w[R];
+    uint32_t s[R];          // the four scales of the row
+};
 
+template <int R> struct Rows {
     const uint8_t* codes[R];
     const uint8_t* scales[R];
+    // rows past the end are computed and not stored
+    __device__ Rows(const MatvecArgs& a, int row0, int r, int g) {
+        const int groups = a.k / kGroup;
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-        const int64_t row = min(row0 + 16 * i + r, a.n - 1);    // rows past the end are computed and not stored
-        codes[i] = a.codes + (row * groups + g) * 16;
-        scales[i] = a.scales + row * groups;
+        for (int i = 0; i < R; ++i) {
+            const int64_t row = min(row0 + 16 * i + r, a.n - 1);
+            codes[i] = a.codes + (row * groups + g) * 16;
+            scales[i] = a.scales + row * groups;
+        }
     }
-    // x of this lane: row r of each tile (the last one again past the end), eighth g of a group
-    const T* x[N];
-    const uint8_t* xl[N];
-    const int x_row = (end - begin) * kGroup * 2 + 16;          // bytes of a row in LDS: 16 rows in 16 columns of the banks
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-        const int tok = min(16 * j + r, a.m - 1 - tok0);
-        x[j] = (const T*)a.x + (int64_t)(tok0 + tok) * a.x_stride + 8 * g;
-        xl[j] = x_lds + tok * x_row - begin * kGroup * 2 + 16 * g;
-    }
-
-    // A step's four groups.  Codes arrive with group g in quarter g of the wave, which reads whole cache lines; the
-    // products take group e with its eighths spread over the quarters, which reads x in whole lines too.
-    struct Step {
-        u32x4 w[R];
-        uint32_t s[R];
-        T8 x[X ? 1 : N][4];
-    };
-    auto load = [&](int first, Step& t) {
+    // groups first .. first + 3; zeros past the end
+    __device__ void load(int first, int end, int g, Step<R>& t) const {
         if (first + 4 <= end) {
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 t.w[i] = *(const u32x4*)(codes[i] + (int64_t)first * 16);
                 __builtin_memcpy(&t.s[i], scales[i] + first, 4);
-            }
-            if constexpr (!X) {
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) t.x[j][e] = *(const T8*)(x[j] + (first + e) * kGroup);
             }
         } else if (first < end) {
 #pragma unroll
@@ -102,95 +75,168 @@ __global__ __launch_bounds__(64 * V) void w4_matvec_kernel(MatvecArgs a) {
                 for (int e = 0; e < 3; ++e)
                     if (first + e < end) t.s[i] = (t.s[i] & ~(255u << (8 * e))) | (uint32_t)scales[i][first + e] << (8 * e);
             }
-            if constexpr (!X) {
+        }
+    }
+};
+
+// The same without a branch, for k of a step at least: what lies past the end is read from before it, and not used.
+template <int R> __device__ inline void load_within(const Rows<R>& rows, int first, int groups, int g, Step<R>& t) {
+    const int from = min(first, groups - 4), shift = 8 * min(first - from, 3), back = min(first + g, groups - 1) - g;
 #pragma unroll
-                for (int j = 0; j < N; ++j)
+    for (int i = 0; i < R; ++i) {
+        t.w[i] = *(const u32x4*)(rows.codes[i] + (int64_t)back * 16);
+        __builtin_memcpy(&t.s[i], rows.scales[i] + from, 4);
+        t.s[i] = t.s[i] >> shift | (~(0xffffffffu >> shift) & 0x7f7f7f7fu);
+    }
+}
+
+// The products take group e of a step with its eighths spread over the quarters of the wave: a 4 x 4 exchange.
+__device__ inline void turn(const u32x4& w, uint32_t (&out)[4]) {
+    const auto s02 = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+    const auto s13 = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+    const auto s01 = __builtin_amdgcn_permlane16_swap(s02[0], s13[0], false, false);
+    const auto s23 = __builtin_amdgcn_permlane16_swap(s02[1], s13[1], false, false);
+    out[0] = s01[0], out[1] = s01[1], out[2] = s23[0], out[3] = s23[1];
+}
+
+// Smallest and largest scale byte, two at a time.
+struct Range {
+    uint32_t most = 0x007f007f, least = 0x007f007f;
+    __device__ void add(uint32_t s) {
+        typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+        const u16x2 even = __builtin_bit_cast(u16x2, s & 0x00ff00ffu), odd = __builtin_bit_cast(u16x2, (s >> 8) & 0x00ff00ffu);
+        most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, most),
+                                                                      __builtin_elementwise_max(even, odd)));
+        least = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, least),
+                                                                       __builtin_elementwise_min(even, odd)));
+    }
+    // scales from 2^-23 to 2^13: fp16 holds the weights exactly
+    __device__ bool fits_fp16() const {
+        return max(most & 0xffffu, most >> 16) <= 140u && min(least & 0xffffu, least >> 16) >= 104u;
+    }
+};
+
+// acc += W x for one group: word w[i] and scale s[i] of R rows, v of N tiles of x.  SPLIT: x in fp16 as two bf16
+// numbers (8 + 3 bits, exact); else the products of fp16 are fp16 ones.
+template <int TYPE, bool SPLIT, int R, int N, typename T8>
+__device__ inline void multiply(const uint32_t (&w)[R], const float (&s)[R], const T8 (&v)[N], f32x4 (&acc)[R][N]) {
+    if constexpr (TYPE == WINO_FP16 && !SPLIT) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        t.x[j][e] = first + e < end ? *(const T8*)(x[j] + (first + e) * kGroup) : T8{};
+        for (int i = 0; i < R; ++i) {
+            const f16x8 u = decode8_f16(w[i], s[i]);
+#pragma unroll
+            for (int j = 0; j < N; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(u, v[j], acc[i][j], 0, 0, 0);
+        }
+    } else {
+        constexpr int kParts = SPLIT ? 2 : 1;
+        bf16x8 b[kParts][N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if constexpr (!SPLIT) {
+                b[0][j] = v[j];
+            } else {
+#pragma unroll
+                for (int d = 0; d < 8; ++d) {
+                    const float f = (float)v[j][d];
+                    const __bf16 hi = (__bf16)f;
+                    b[0][j][d] = hi;
+                    b[1][j][d] = (__bf16)(f - (float)hi);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const bf16x8 u = decode8(w[i], s[i]);
+#pragma unroll
+            for (int p = 0; p < kParts; ++p)
+#pragma unroll
+                for (int j = 0; j < N; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, b[p][j], acc[i][j], 0, 0, 0);
+        }
+    }
+}
+
+// A sum of row `row` of W and row `tok` of x: stored, or left for w4_matvec_join.
+template <typename T> __device__ inline void store(const MatvecArgs& a, int row, int tok, float sum) {
+    if (row >= a.n || tok >= a.m) return;
+    if (a.part) {
+        a.part[((int64_t)blockIdx.z * a.m + tok) * a.n + row] = sum;
+    } else {
+        if (a.bias) sum += (float)((const T*)a.bias)[row];
+        ((T*)a.y)[(int64_t)tok * a.y_stride + row] = (T)sum;
+    }
+}
+
+// 16 rows of x.  R tiles of 16 rows of W, V waves that share out k, two steps of codes on their way.  X: x lies in
+// LDS; else its pieces come with the codes.  blockIdx.z takes `steps` steps of k; where there are several, their sums
+// go to a.part and w4_matvec_join adds them up.
+template <int TYPE, int R, int V, bool X> __global__ __launch_bounds__(64 * V) void w4_matvec_kernel(MatvecArgs a) {
+    typedef typename Half<TYPE>::type T;
+    typedef T T8 __attribute__((ext_vector_type(8)));
+    constexpr int D = 2;
+    __shared__ float join[V][R * 16][17];
+    extern __shared__ __attribute__((aligned(16))) uint8_t x_lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int row0 = blockIdx.x * (16 * R), tok0 = blockIdx.y * 16, toks = min(16, a.m - tok0);
+    const int begin = blockIdx.z * a.steps * 4, end = min(a.k / kGroup, begin + a.steps * 4);
+    const Rows<R> rows(a, row0, r, g);
+    // x of this lane: row r (the last one again past the end), eighth g of a group
+    const int x_row = (end - begin) * kGroup * 2 + 16;          // bytes of a row in LDS: 16 rows in 16 columns of the banks
+    const int tok = min(r, toks - 1);
+    const T* x = (const T*)a.x + (int64_t)(tok0 + tok) * a.x_stride + 8 * g;
+    const uint8_t* xl = x_lds + tok * x_row - begin * kGroup * 2 + 16 * g;
+
+    struct Both {
+        Step<R> w;
+        T8 x[4];
+    };
+    auto load = [&](int first, Both& t) {
+        rows.load(first, end, g, t.w);
+        if constexpr (!X) {
+            if (first + 4 <= end) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t.x[e] = *(const T8*)(x + (first + e) * kGroup);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t.x[e] = first + e < end ? *(const T8*)(x + (first + e) * kGroup) : T8{};
             }
         }
     };
-
-    f32x4 acc[R][N];                                            // lane: rows 4 g + e of W, row r of x
-    uint32_t most = 0x007f007f, least = 0x007f007f;             // of the scales, two at a time
-    // `split`: x in fp16 as two bf16 numbers (8 + 3 bits, exact).  Else the products are fp16 ones, which hold W
-    // exactly as long as its scales lie between 2^-23 and 2^13.
-    auto compute = [&](int first, const Step& t, auto split) {
-        constexpr bool kSplit = decltype(split)::value, kF16 = TYPE == WINO_FP16 && !kSplit;
-        constexpr int kParts = kSplit ? 2 : 1;
+    f32x4 acc[R][1];                                            // lane: rows 4 g + e of W, row r of x
+    Range range;
+    auto compute = [&](int first, const Both& t, auto split) {
         uint32_t w[R][4];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const auto s02 = __builtin_amdgcn_permlane32_swap(t.w[i][0], t.w[i][2], false, false);
-            const auto s13 = __builtin_amdgcn_permlane32_swap(t.w[i][1], t.w[i][3], false, false);
-            const auto s01 = __builtin_amdgcn_permlane16_swap(s02[0], s13[0], false, false);
-            const auto s23 = __builtin_amdgcn_permlane16_swap(s02[1], s13[1], false, false);
-            w[i][0] = s01[0], w[i][1] = s01[1], w[i][2] = s23[0], w[i][3] = s23[1];
-            if constexpr (kF16) {
-                typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
-                const u16x2 even = __builtin_bit_cast(u16x2, t.s[i] & 0x00ff00ffu);
-                const u16x2 odd = __builtin_bit_cast(u16x2, (t.s[i] >> 8) & 0x00ff00ffu);
-                most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(
-                           __builtin_bit_cast(u16x2, most), __builtin_elementwise_max(even, odd)));
-                least = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(
-                            __builtin_bit_cast(u16x2, least), __builtin_elementwise_min(even, odd)));
-            }
+            turn(t.w.w[i], w[i]);
+            if constexpr (TYPE == WINO_FP16) range.add(t.w.s[i]);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            T8 v[N];
+            T8 v[1];
+            if constexpr (X)
+                v[0] = first + e < end ? *(const T8*)(xl + (first + e) * (kGroup * 2)) : T8{};
+            else
+                v[0] = t.x[e];
+            uint32_t we[R];
+            float s[R];
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                if constexpr (X)
-                    v[j] = first + e < end ? *(const T8*)(xl[j] + (first + e) * (kGroup * 2)) : T8{};
-                else
-                    v[j] = t.x[j][e];
-            }
-            bf16x8 b[kParts][N];
-            if constexpr (!kF16) {
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    if constexpr (TYPE == WINO_BF16) {
-                        b[0][j] = v[j];
-                    } else {
-#pragma unroll
-                        for (int d = 0; d < 8; ++d) {
-                            const float f = (float)v[j][d];
-                            const __bf16 hi = (__bf16)f;
-                            b[0][j][d] = hi;
-                            b[kParts - 1][j][d] = (__bf16)(f - (float)hi);
-                        }
-                    }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const float s = scale_bits((t.s[i] >> (8 * e)) & 255u);
-                if constexpr (kF16) {
-                    const f16x8 u = decode8_f16(w[i][e], s);
-#pragma unroll
-                    for (int j = 0; j < N; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(u, v[j], acc[i][j], 0, 0, 0);
-                } else {
-                    const bf16x8 u = decode8(w[i][e], s);
-#pragma unroll
-                    for (int p = 0; p < kParts; ++p)
-#pragma unroll
-                        for (int j = 0; j < N; ++j)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, b[p][j], acc[i][j], 0, 0, 0);
-                }
-            }
+            for (int i = 0; i < R; ++i) we[i] = w[i][e], s[i] = scale_bits((t.w.s[i] >> (8 * e)) & 255u);
+            multiply<TYPE, decltype(split)::value, R, 1>(we, s, v, acc);
         }
     };
     // the wave's steps: every V-th
     const int mine = max(0, (end - begin - wave * 4 + 4 * V - 1) / (4 * V));
     auto at = [&](int i) { return begin + (wave + V * i) * 4; };
-    auto sweep = [&](Step (&t)[D], auto split) {
+    Both t[D];
+    auto start = [&]() {
 #pragma unroll
-        for (int i = 0; i < R; ++i)
+        for (int d = 0; d < D; ++d)
+            if (d < mine) load(at(d), t[d]);
+    };
+    auto sweep = [&](auto split) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < R; ++i) acc[i][0] = f32x4{0.f, 0.f, 0.f, 0.f};
         for (int i = 0; i < mine; i += D) {
 #pragma unroll
             for (int d = 0; d < D; ++d) {
@@ -201,48 +247,143 @@ __global__ __launch_bounds__(64 * V) void w4_matvec_kernel(MatvecArgs a) {
             }
         }
     };
-    Step t[D];
-#pragma unroll
-    for (int d = 0; d < D; ++d)
-        if (d < mine) load(at(d), t[d]);
+    start();
     if constexpr (X) {
-        const int pieces = (end - begin) * 4, rows = min(16 * N, a.m - tok0);
-        for (int i = threadIdx.x; i < pieces * rows; i += 64 * V) {
+        const int pieces = (end - begin) * 4;
+        for (int i = threadIdx.x; i < pieces * toks; i += 64 * V) {
             const int tok = i / pieces, p = i - tok * pieces;
             *(T8*)(x_lds + tok * x_row + p * 16) =
                 *(const T8*)((const T*)a.x + (int64_t)(tok0 + tok) * a.x_stride + begin * kGroup + p * 8);
         }
         __syncthreads();
     }
-    sweep(t, std::false_type{});
+    sweep(std::false_type{});
     if constexpr (TYPE == WINO_FP16) {
-        const uint32_t hi = max(most & 0xffffu, most >> 16), lo = min(least & 0xffffu, least >> 16);
-        if (__any(hi > 140u || lo < 104u)) {
-#pragma unroll
-            for (int d = 0; d < D; ++d)
-                if (d < mine) load(at(d), t[d]);
-            sweep(t, std::true_type{});
+        if (__any(!range.fits_fp16())) {
+            start();
+            sweep(std::true_type{});
         }
     }
 #pragma unroll
     for (int i = 0; i < R; ++i)
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) join[wave][16 * i + 4 * g + e][16 * j + r] = acc[i][j][e];
+        for (int e = 0; e < 4; ++e) join[wave][16 * i + 4 * g + e][r] = acc[i][0][e];
     __syncthreads();
-    for (int o = threadIdx.x; o < R * N * 256; o += 64 * V) {
+    for (int o = threadIdx.x; o < R * 256; o += 64 * V) {
         const int row = o % (R * 16), tok = o / (R * 16);
-        if (row0 + row >= a.n || tok0 + tok >= a.m) continue;
         float sum = join[0][row][tok];
 #pragma unroll
         for (int w = 1; w < V; ++w) sum += join[w][row][tok];
-        if (a.part) {
-            a.part[((int64_t)blockIdx.z * a.m + tok0 + tok) * a.n + row0 + row] = sum;
-        } else {
-            if (a.bias) sum += (float)((const T*)a.bias)[row0 + row];
-            ((T*)a.y)[(int64_t)(tok0 + tok) * a.y_stride + row0 + row] = (T)sum;
+        store<T>(a, row0 + row, tok0 + tok, sum);
+    }
+}
+
+// More rows of x, or more of W, in tiles of N times 16 of x.  Eight waves: two with R tiles of 16 rows of W each, times
+// four that share out k.  x goes through LDS, 512 of k at a time, the next ones on their way while these are multiplied:
+// both halves of the waves read it there, which halves what the L2 has to deliver, and rows are copied a KiB at a time.
+// Two steps of codes are on their way.  64 rows by 16384 x 4096: 20.4 us, 1.7 TB/s of weights; a workgroup takes 1.6 us
+// for 512 of k, whose products and LDS reads take half of that and whose barrier keeps the waves in step.
+template <int TYPE, int R, int N> __global__ __launch_bounds__(512) void w4_matmul_kernel(MatvecArgs a) {
+    typedef typename Half<TYPE>::type T;
+    typedef T T8 __attribute__((ext_vector_type(8)));
+    constexpr int D = 2, kShare = 4, kRow = kShare * 256;       // steps of codes; waves along k; bytes of a row of x in LDS
+    constexpr int kBuf = 16 * N * kRow, kCopies = 2 * N;        // pieces of 16 bytes that a thread copies
+    constexpr int kJoin = kShare * 32 * R * (16 * N + 1) * 4;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kBuf > kJoin ? 2 * kBuf : kJoin];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4, share = wave % kShare, upper = wave / kShare;
+    const int row0 = blockIdx.x * (32 * R), tok0 = blockIdx.y * (16 * N);
+    const int groups = a.k / kGroup, begin = blockIdx.z * a.steps * 4, end = min(groups, begin + a.steps * 4);
+    const Rows<R> rows(a, row0 + 16 * R * upper, r, g);
+    const int chunks = (end - begin + 4 * kShare - 1) / (4 * kShare);
+    auto at = [&](int c) { return begin + (c * kShare + share) * 4; };
+
+    // A wave copies row `wave` + 8 x of the tile, a lane one piece of it.  Piece p of row t lies at p ^ (t % 16), so that
+    // reading one piece of 16 rows takes all banks once.  Past the ends it copies the last row and piece again.
+    T8 piece[kCopies];
+    auto fetch = [&](int c) {
+        const int first = begin + c * (4 * kShare);
+#pragma unroll
+        for (int x = 0; x < kCopies; ++x) {
+            const int t = wave + 8 * x, tok = min(tok0 + t, a.m - 1), p = min(lane ^ (t & 15), (end - first) * 4 - 1);
+            piece[x] = *(const T8*)((const T*)a.x + (int64_t)tok * a.x_stride + first * kGroup + p * 8);
         }
+    };
+    auto put = [&](int buf) {
+#pragma unroll
+        for (int x = 0; x < kCopies; ++x) *(T8*)(lds + buf * kBuf + (wave + 8 * x) * kRow + lane * 16) = piece[x];
+    };
+    f32x4 acc[R][N];
+    Range range;
+    auto compute = [&](int first, int buf, const Step<R>& t, auto split) {
+        uint32_t w[R][4];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            turn(t.w[i], w[i]);
+            if constexpr (TYPE == WINO_FP16) range.add(t.s[i]);
+        }
+        const uint8_t* x = lds + buf * kBuf + r * kRow;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (first + e >= end) break;
+            T8 v[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = *(const T8*)(x + 16 * j * kRow + ((share * 16 + e * 4 + g) ^ r) * 16);
+            uint32_t we[R];
+            float s[R];
+#pragma unroll
+            for (int i = 0; i < R; ++i) we[i] = w[i][e], s[i] = scale_bits((t.s[i] >> (8 * e)) & 255u);
+            multiply<TYPE, decltype(split)::value, R, N>(we, s, v, acc);
+        }
+    };
+    auto sweep = [&](auto split) {
+        Step<R> t[D];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int d = 0; d < D; ++d)
+            if (d < chunks) load_within(rows, at(d), groups, g, t[d]);
+        fetch(0);
+        put(0);
+        // chunk c, whose codes are in t[d], and what is asked for meanwhile
+        auto turn_to = [&](int c, int d, bool next, bool codes) {
+            __syncthreads();                                    // the chunk is there, and nobody reads the other one any more
+            if (next) fetch(c + 1);
+            compute(at(c), c & 1, t[d], split);
+            if (codes) load_within(rows, at(c + D), groups, g, t[d]);
+            if (next) put((c + 1) & 1);
+        };
+        // Loads behind conditions make the products wait for all that may have been asked for, so there are none but at
+        // the end.
+        int c = 0;
+        for (; c + 2 * D <= chunks; c += D) {
+#pragma unroll
+            for (int d = 0; d < D; ++d) turn_to(c + d, d, true, true);
+        }
+#pragma unroll
+        for (int d = 0; d < 2 * D - 1; ++d)
+            if (c + d < chunks) turn_to(c + d, d % D, c + d + 1 < chunks, d < D - 1 && c + d + D < chunks);
+        __syncthreads();
+    };
+    sweep(std::false_type{});
+    if constexpr (TYPE == WINO_FP16)
+        if (__syncthreads_or(!range.fits_fp16())) sweep(std::true_type{});
+    float(*join)[32 * R][16 * N + 1] = (float(*)[32 * R][16 * N + 1])lds;
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) join[share][16 * (R * upper + i) + 4 * g + e][16 * j + r] = acc[i][j][e];
+    __syncthreads();
+    for (int o = threadIdx.x; o < R * N * 512; o += 512) {
+        const int row = o % (32 * R), tok = o / (32 * R);
+        float sum = join[0][row][tok];
+#pragma unroll
+        for (int w = 1; w < kShare; ++w) sum += join[w][row][tok];
+        store<T>(a, row0 + row, tok0 + tok, sum);
     }
 }
 
@@ -260,70 +401,85 @@ template <int TYPE> __global__ __launch_bounds__(256) void w4_matvec_join(Matvec
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
-template <int TYPE, int R, int N, int V, int D, bool X> void launch(MatvecArgs a, int splits, hipStream_t stream) {
+// Parts of k in whole steps.
+int share_out(MatvecArgs& a, int splits) {
     const int steps = (a.k + 127) / 128;
     a.steps = (steps + splits - 1) / splits;
     splits = a.steps > 0 ? (steps + a.steps - 1) / a.steps : 1;
     if (splits <= 1) a.part = nullptr;
-    const dim3 grid((unsigned)((a.n + 16 * R - 1) / (16 * R)), (unsigned)((a.m + 16 * N - 1) / (16 * N)), (unsigned)splits);
-    const size_t lds = X ? (size_t)std::min(a.m, 16 * N) * (std::min(a.k, a.steps * 128) * 2 + 16) : 0;
-    hipLaunchKernelGGL((w4_matvec_kernel<TYPE, R, N, V, D, X>), grid, dim3(64 * V), lds, stream, a);
+    return splits;
+}
+template <int TYPE> void join(const MatvecArgs& a, int splits, hipStream_t stream) {
     if (splits > 1)
         hipLaunchKernelGGL((w4_matvec_join<TYPE>), dim3((unsigned)((a.n + 255) / 256), (unsigned)a.m), dim3(256), 0, stream,
                            a, splits);
 }
+template <int TYPE, int R, int V, bool X> void launch(MatvecArgs a, int splits, hipStream_t stream) {
+    splits = share_out(a, splits);
+    const size_t lds = X ? (size_t)std::min(a.m, 16) * (std::min(a.k, a.steps * 128) * 2 + 16) : 0;
+    const dim3 grid((unsigned)((a.n + 16 * R - 1) / (16 * R)), (unsigned)((a.m + 15) / 16), (unsigned)splits);
+    hipLaunchKernelGGL((w4_matvec_kernel<TYPE, R, V, X>), grid, dim3(64 * V), lds, stream, a);
+    join<TYPE>(a, splits, stream);
+}
+template <int TYPE, int R, int N> void launch_wide(MatvecArgs a, int splits, hipStream_t stream) {
+    splits = share_out(a, splits);
+    const dim3 grid((unsigned)((a.n + 32 * R - 1) / (32 * R)), (unsigned)((a.m + 16 * N - 1) / (16 * N)), (unsigned)splits);
+    hipLaunchKernelGGL((w4_matmul_kernel<TYPE, R, N>), grid, dim3(512), 0, stream, a);
+    join<TYPE>(a, splits, stream);
+}
 
-// How a call is cut: 16 rows of W a workgroup (times `r`), k in `splits` parts, x in LDS or beside the codes.
+// Which kernel takes a call and how it is cut: tiles of 16 rows of W (times two waves where `wide`), k in `splits` parts,
+// x in LDS or beside the codes.
 struct Cut {
+    bool wide;
     int r, splits;
-    bool x;
+    bool x = false;
     int waves = 8;
 };
 
 // Few workgroups read x few times, many keep the device busy; a second launch, for the join, costs 3 us.  Measured (us,
-// bf16, rows of x / n / k; r and parts):
-//   x in LDS                    1/4096/4096: r1 4.7 (8 waves 5.1)   4/16384/4096: r2 13.0, r1 14.4   1/16384/4096: r2 11.3
-//   x beside the codes          8/4096/4096: r1 6.5, r4 in 4 8.0    8/8192/8192: r2 15.3, r4 in 2 16.5
-//                               16/16384/4096: r4 14.8, r2 17.6     16/2048/8192: r2 in 4 9.2, r4 in 8 9.9
-//                               16/4096/16384: r4 in 4 18.4, r2 in 2 19.9, r1 24   1/1024/16384: r2 in 8 7.9, r1 10.9
-//   more than 16 rows           32/4096/1024: r2 5.2, r4 6.4        32/2048/4096: r2 in 4 8.6, r4 in 4 9.8
-//                               32/8192/8192: r4 in 2 22.2, r2 25.4 64/16384/4096: r4 28, r2 42
+// bf16, rows of x / n / k; r, parts):
+//   x in LDS             1/4096/4096: 16 waves 4.7, 8 waves 5.1      4/4096/4096: r1 5.9, r2 7.7
+//                        4/16384/4096: r2 12.2, r1 15.4, wide 13.8
+//   x beside the codes   8/4096/4096: r1 6.6, wide in 2 7.8          8/8192/8192: r2 14.9, wide in 2 15.8
+//                        1/1024/16384: r2 in 8 7.9, r1 10.9          4/4096/16384: r2 in 2 15.9, wide in 4 16.3
+//   wide, one tile of x  8/32768/2048: r2 12.6, x in LDS 14.1        16/32768/2048: r2 13.2, beside the codes 16.4
+//                        16/16384/4096: r1 14.4, r2 14.6, beside 15.1
+//                        16/1024/16384: r1 in 8 9.6, beside in 4 12.4   16/4096/16384: r2 in 4 18.0, beside 18.4
+//   two                  32/4096/4096: r1 in 2 9.4, r2 in 4 9.9      32/2048/4096: r1 in 4 8.0, r2 in 4 9.5
+//                        32/8192/8192: r2 in 2 19.3, r1 20.9         32/16384/4096: r2 16.5, r1 18.2
+//   four                 64/4096/1024: r1 5.8, r2 7.7                64/4096/16384: r2 in 4 24.2, r1 in 2 30.4
+//                        64/8192/8192: r2 in 2 23.8, r1 28.5         64/16384/4096: r2 20.4, r1 29.4
 Cut cut(int64_t m, int64_t n, int64_t k) {
     // as many parts as make a workgroup for each of 256 compute units, no more, with 1024 of k in each at least
-    auto parts = [&](int r) {
-        const int64_t groups = (n + 16 * r - 1) / (16 * r);
+    auto parts = [&](int rows) {
+        const int64_t groups = (n + rows - 1) / rows;
         return (int)std::max<int64_t>(1, std::min<int64_t>(256 / groups, k / 1024));
     };
-    if (m > 16) {
-        const int r = n <= 2048 || (k < 2048 && n <= 8192) ? 2 : 4;
-        return Cut{r, parts(r), false};
+    const bool fits = std::min<int64_t>(m, 16) * (2 * k + 16) <= 40960;
+    if (k >= 128 && (m > 16 || (n > 8192 && (m > 4 || !fits)) || (m > 8 && n <= 4096 && k >= 8192))) {
+        const int r = n > 8192 || (n >= 4096 && k >= 8192) ? 2 : 1;
+        return Cut{true, r, parts(32 * r)};
     }
-    const bool fits = m * (2 * k + 16) <= 40960;
-    if (n <= 2048 && k >= 12288) return Cut{2, parts(2), false};
-    if (fits) return Cut{n <= 8192 ? 1 : 2, 1, true, n <= 4096 ? 16 : 8};
-    if (n <= 4096 && k >= 8192) {
-        const int r = m > 8 && n > 2048 ? 4 : 2;
-        return Cut{r, parts(r), false};
-    }
-    return Cut{n <= 4096 ? 1 : (n <= 8192 ? 2 : 4), 1, false};
+    if (n <= 4096 && k >= 8192 && (!fits || (n <= 2048 && k >= 12288))) return Cut{false, 2, parts(32)};
+    if (fits) return Cut{false, n <= 8192 ? 1 : 2, 1, true, n <= 4096 ? 16 : 8};
+    return Cut{false, n <= 4096 ? 1 : 2, 1};
 }
 
 template <int TYPE> void pick(const MatvecArgs& a, bool room, hipStream_t stream) {
     const Cut c = cut(a.m, a.n, a.k);
     const int s = room ? c.splits : 1;
-    if (a.m > 32)
-        c.r == 2 ? launch<TYPE, 2, 4, 8, 1, false>(a, s, stream) : launch<TYPE, 4, 4, 8, 1, false>(a, s, stream);
-    else if (a.m > 16)
-        c.r == 2 ? launch<TYPE, 2, 2, 8, 2, false>(a, s, stream) : launch<TYPE, 4, 2, 8, 2, false>(a, s, stream);
+    if (c.wide && a.m > 32)
+        c.r == 1 ? launch_wide<TYPE, 1, 4>(a, s, stream) : launch_wide<TYPE, 2, 4>(a, s, stream);
+    else if (c.wide && a.m > 16)
+        c.r == 1 ? launch_wide<TYPE, 1, 2>(a, s, stream) : launch_wide<TYPE, 2, 2>(a, s, stream);
+    else if (c.wide)
+        c.r == 1 ? launch_wide<TYPE, 1, 1>(a, s, stream) : launch_wide<TYPE, 2, 1>(a, s, stream);
     else if (c.x)
-        c.waves == 16 ? launch<TYPE, 1, 1, 16, 2, true>(a, 1, stream)
-                      : (c.r == 1 ? launch<TYPE, 1, 1, 8, 2, true>(a, 1, stream) : launch<TYPE, 2, 1, 8, 2, true>(a, 1, stream));
-    else if (c.r == 1)
-        launch<TYPE, 1, 1, 8, 2, false>(a, s, stream);
-    else if (c.r == 2)
-        launch<TYPE, 2, 1, 8, 2, false>(a, s, stream);
+        c.waves == 16 ? launch<TYPE, 1, 16, true>(a, 1, stream)
+                      : (c.r == 1 ? launch<TYPE, 1, 8, true>(a, 1, stream) : launch<TYPE, 2, 8, true>(a, 1, stream));
     else
-        launch<TYPE, 4, 1, 8, 2, false>(a, s, stream);
+        c.r == 1 ? launch<TYPE, 1, 8, false>(a, s, stream) : launch<TYPE, 2, 8, false>(a, s, stream);
 }
 
 }  // namespace
