@@ -13,9 +13,8 @@
 // share out k and are joined in LDS, workgroups that share out k are joined
 // by a second kernel, both in a fixed order.
 //
-// Measured (bf16): 16384 x 4096, 35.7 MB: 10.2 us for one row of x (3.5 TB/s,
-// of 4.9 that a large copy reaches), 17.6 us for 16, where the reads of x from
-// the L2 count as much as those of W.
+// Measured: 16384 x 4096, 35.7 MB: 9.9 us for one row of x (3.6 TB/s, of 4.9
+// that a large copy reaches); 4096 x 16384 for 16 rows, in parts: 16.1 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -441,6 +440,7 @@ struct Cut {
 // bf16, rows of x / n / k; r, parts):
 //   x in LDS             1/4096/4096: 16 waves 4.7, 8 waves 5.1      4/4096/4096: r1 5.9, r2 7.7
 //                        4/16384/4096: r2 12.2, r1 15.4, wide 13.8
+//                        64/2048/1248: 16 waves 4.3, wide 6.8     64/4096/1248: 16 waves 7.0, wide 6.9
 //   x beside the codes   8/4096/4096: r1 6.6, wide in 2 7.8          8/8192/8192: r2 14.9, wide in 2 15.8
 //                        1/1024/16384: r2 in 8 7.9, r1 10.9          4/4096/16384: r2 in 2 15.9, wide in 4 16.3
 //   wide, one tile of x  8/32768/2048: r2 12.6, x in LDS 14.1        16/32768/2048: r2 13.2, beside the codes 16.4
@@ -457,7 +457,7 @@ Cut cut(int64_t m, int64_t n, int64_t k) {
         return (int)std::max<int64_t>(1, std::min<int64_t>(256 / groups, k / 1024));
     };
     const bool fits = std::min<int64_t>(m, 16) * (2 * k + 16) <= 40960;
-    if (k >= 128 && (m > 16 || (n > 8192 && (m > 4 || !fits)) || (m > 8 && n <= 4096 && k >= 8192))) {
+    if (k >= 128 && ((m > 16 && !(fits && n <= 4096)) || (n > 8192 && (m > 4 || !fits)) || (m > 8 && n <= 4096 && k >= 8192))) {
         const int r = n > 8192 || (n >= 4096 && k >= 8192) ? 2 : 1;
         return Cut{true, r, parts(32 * r)};
     }

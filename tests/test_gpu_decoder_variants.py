@@ -66,6 +66,34 @@ def test_matvec_cuts(m, n, k, lowest, highest, name):
         assert (got[0] == got[1]).all(), "the same call gives another result"
 
 
+@pytest.mark.parametrize("name", ["bf16", "fp16"])
+@pytest.mark.parametrize("m,n,k", [(12, 1000, 8224), (6, 8300, 1312), (5, 8200, 160), (20, 40, 1312), (18, 300, 4640),
+                                   (18, 9000, 160), (17, 8200, 2624), (40, 4200, 128), (35, 300, 5152), (50, 8250, 544),
+                                   (70, 33, 1600), (64, 4100, 1024)])
+def test_matmul_far_apart_rows_and_not_finite(m, n, k, name):
+    """Rows of x within a wider tensor, the last columns of two of them not
+    finite: their own outputs are not numbers or infinite, the others' ordinary,
+    whatever is read past the ends of k and m."""
+    torch = torch_dev()
+    rng = np.random.default_rng(m + n + k)
+    codes = rng.integers(0, 256, (n, k // 2), dtype=np.uint8)
+    scales = rng.integers(120, 130, (n, k // 32), dtype=np.uint8)
+    w = decoder.decode(codes, scales)
+    wide, wv = half(torch, rng.normal(0, 1, (m, k + 24)), name)
+    x, xv = wide[:, 8:8 + k], wv[:, 8:8 + k]
+    x[3, k - 1], x[m - 1, k - 1] = float("nan"), float("inf")
+    wide[:, :8] = wide[:, 8 + k:] = float("nan")
+    cd, sd = torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda()
+    zero = (codes[:, -1] >> 4 & 7) == 0
+    keep = [i for i in range(m) if i not in (3, m - 1)]
+    for ws in (torch.full((W.w4_matvec_workspace_bytes(m, n, k) + 16,), 255, dtype=torch.uint8, device="cuda"), None):
+        y = torch.full((m, n), 3.0, dtype=dtype(torch, name), device="cuda")
+        W.w4_matvec(x, cd, sd, y, workspace=ws)
+        got = host(y)
+        assert np.isnan(got[3]).all() and np.isnan(got[m - 1][zero]).all() and np.isinf(got[m - 1][~zero]).all()
+        _check_rounded(got[keep], xv[keep], w, None, name)
+
+
 def test_matvec_cuts_into_parts():
     """The sizes above do reach the parts."""
     assert W.w4_matvec_workspace_bytes(3, 100, 8192) > 0 and W.w4_matvec_workspace_bytes(9, 2100, 8224) > 0
