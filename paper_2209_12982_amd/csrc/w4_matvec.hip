@@ -139,7 +139,8 @@ __device__ inline void multiply(const uint32_t (&w)[R], const float (&s)[R], con
                     const float f = (float)v[j][d];
                     const __bf16 hi = (__bf16)f;
                     b[0][j][d] = hi;
-                    b[1][j][d] = (__bf16)(f - (float)hi);
+                    const float rest = f - (float)hi;           // infinity less itself: no rest
+                    b[1][j][d] = (__bf16)(rest == rest ? rest : 0.f);
                 }
             }
         }

@@ -94,6 +94,22 @@ def test_matmul_far_apart_rows_and_not_finite(m, n, k, name):
         _check_rounded(got[keep], xv[keep], w, None, name)
 
 
+@pytest.mark.parametrize("m,n,k", [(3, 70, 96), (20, 300, 1312)])
+def test_matvec_infinity_times_weights_past_fp16(m, n, k):
+    """An infinite x with weights that fp16 does not hold: infinite, not NaN."""
+    torch = torch_dev()
+    rng = np.random.default_rng(71)
+    codes = rng.integers(0, 256, (n, k // 2), dtype=np.uint8) | 0x22          # no weight is zero
+    scales = np.full((n, k // 32), 98, np.uint8)
+    x, xv = half(torch, rng.normal(0, 1, (m, k)), "fp16")
+    x[1, 40] = float("-inf")
+    y = torch.zeros((m, n), dtype=torch.float16, device="cuda")
+    W.w4_matvec(x, torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), y)
+    got, w = host(y), decoder.decode(codes, scales)
+    assert (got[1] == -np.sign(w[:, 40]) * np.inf).all()
+    _check(np.delete(got, 1, 0), np.delete(xv, 1, 0), w, None, "fp16")
+
+
 def test_matvec_cuts_into_parts():
     """The sizes above do reach the parts."""
     assert W.w4_matvec_workspace_bytes(3, 100, 8192) > 0 and W.w4_matvec_workspace_bytes(9, 2100, 8224) > 0
