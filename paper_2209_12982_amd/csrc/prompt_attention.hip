@@ -13,6 +13,16 @@
 //
 // Where there are too few tiles for the device, teams of waves share out the
 // keys of one tile and are joined in LDS at the end.
+//
+// Precision: probabilities are rounded to the type of q, k and v for the second
+// product (fp16 ones held 2^6 higher, clear of its smallest numbers), and their
+// sum is that of the rounded ones, so that the weights of a row add up to 1.
+//
+// One sequence of 16384 tokens, 16 heads of 128 on 4: 1012 to 1030 us, 1.08
+// PFLOP/s (a large library product of the same type: 1.25); the matrix cores work
+// 57% of the cycles, at the clock that this load leaves (1.6 to 1.8 GHz).  Twelve
+// packed ones of up to 2048, 32 heads on 8: 143 us, 0.78 PFLOP/s, 40%: their
+// workgroups walk over eight tiles on average, and begin and end in between.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -97,9 +107,9 @@ template <int ROWS> __device__ inline bool find(const PromptArgs& a, int index, 
         int from = 0, n = 0, k0 = 0, k1 = 0;
         if (s < a.seqs) {
             from = max(a.cu_q[s], 0);
-            n = max(min(a.cu_q[s + 1], a.total_q) - from, 0);
+            n = max(max(min(a.cu_q[s + 1], a.total_q), 0) - from, 0);
             k0 = max(min(a.cu_k[s], a.total_k), 0);
-            k1 = min(a.cu_k[s + 1], a.total_k);
+            k1 = max(min(a.cu_k[s + 1], a.total_k), 0);
         }
         const int count = (n * a.group + ROWS - 1) / ROWS;
         // the 64 sequences by their keys, the longest first: tiles before this lane's, and all of them

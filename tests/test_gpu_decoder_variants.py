@@ -206,6 +206,25 @@ def test_prompt_few_queries_on_many_keys(d, name):
         _hold(host(out), ref, bound)
 
 
+def test_prompt_offsets_that_fall():
+    """Offsets below 0 and falling ones, down to the type's lowest value: such
+    sequences are empty, the others are not touched by it."""
+    torch = torch_dev()
+    rng = np.random.default_rng(62)
+    n, hq, hkv, d = 60, 4, 2, 64
+    q, qv = half(torch, rng.normal(0, 1, (n, hq, d)), "bf16")
+    k, kv = half(torch, rng.normal(0, 1, (n, hkv, d)), "bf16")
+    v, vv = half(torch, rng.normal(0, 1, (n, hkv, d)), "bf16")
+    low = -2 ** 31
+    cu_q = torch.tensor([5, 25, low, -1, 0], dtype=torch.int32, device="cuda")
+    cu_k = torch.tensor([7, 47, low, 3, -9], dtype=torch.int32, device="cuda")
+    out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+    W.prompt_attention(q, k, v, cu_q, cu_k, 20, out, 0.1)
+    ref, bound = prompt_reference(qv[5:25], kv[7:47], vv[7:47], [20], [40], 0.1, True, "bf16")
+    _hold(host(out)[5:25], ref, bound)
+    assert (out[:5] == 7).all() and (out[25:] == 7).all()
+
+
 def test_prompt_rows_far_apart():
     """Keys and values whose offsets pass 32 bits, in elements as well."""
     torch = torch_dev()
