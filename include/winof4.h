@@ -516,6 +516,10 @@ wino_status wino_f4_conv_float(const int8_t* x, const float* w_oihw, float* y, i
  *     code.  This rounding is the format's own and the one place where the
  *     library does not round half up;
  *   - two codes a byte, the lower index in the low half.
+ * Kernels read weights and cache as 16-bit numbers.  Values past their range,
+ * which only the scale bytes 253 and 254 reach (2^126 and 2^127), count as
+ * infinite there; cached values under such a scale make the rows of
+ * kv4_attention that see them infinite or NaN.
  * Activations are bf16 or fp16 (wino_float_type, one type for a call); every
  * sum, maximum and softmax statistic is held in fp32 and each result is
  * rounded to the 16-bit type once.
@@ -615,7 +619,8 @@ wino_status kv4_append(const void* q, int64_t q_stride, const void* k, int64_t k
  *                tokens before lens - q_len + 1 + i:
  *                softmax_t(scale q.k_t) v_t; zeros where it sees none.
  * heads is a multiple of cache->kv_heads: neighbours share a head of the
- * cache.  head_dim 64, 96, 128, 192 or 256; scale finite.
+ * cache.  head_dim 64, 96, 128, 192 or 256; scale finite, and so is its product
+ * with log2(e) in fp32 (WINO_EUNSUPPORTED otherwise).
  *   workspace    kv4_attention_workspace_bytes() bytes or more, 16-byte
  *                aligned, scratch: long sequences are split over it.  NULL or
  *                a smaller one splits less.
@@ -631,18 +636,21 @@ wino_status kv4_attention(const void* q, int64_t q_stride, const kv4_cache* cach
  * prompt_attention -- attention of whole prompts, sequences of different
  * lengths packed one after the other, keys and values in 16 bits.
  *   q          [total_q][heads][head_dim], stride q_stride
- *   k, v       [total_k][kv_heads][head_dim], strides k_stride, v_stride
+ *   k, v       [total_k][kv_heads][head_dim], strides k_stride, v_stride, at
+ *              most 2^24
  *   cu_q, cu_k int32 [seqs + 1] (may be the same): sequence s has the queries
  *              cu_q[s] .. cu_q[s+1] - 1 and the keys cu_k[s] .. cu_k[s+1] - 1.
  *              Offsets do not decrease; what lies past total_q or total_k is
  *              left out.  A row of out that no sequence covers is not written.
- *   max_q      the longest sequence's queries, a hint for the tile size
+ *   max_q      the longest sequence's queries, a hint for the tile size: any
+ *              value gives a right result
  *   causal     1: the last query sees every key, the one before it one less,
  *              and so on (a prompt behind a prefix has more keys than
  *              queries); 0: all keys.
  *   out        [total_q][heads][head_dim], dense; zeros where a query sees
  *              no key.
- * Sizes of heads as for kv4_attention.
+ * Sizes of heads and scale as for kv4_attention; total_q times the heads of a
+ * group below 2^31.
  */
 wino_status prompt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                              int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k, int32_t seqs,

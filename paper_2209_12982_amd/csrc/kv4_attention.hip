@@ -17,6 +17,11 @@
 // Precision: queries in fp16 and all probabilities are split into two bf16
 // numbers (16 bits), the matrix cores have time for both; the products are
 // then exact in fp32.
+//
+// 32 heads of 128 on 8: two sequences of 131072 tokens, 157 MB of cache, take
+// 40.2 us, 36.1 of them this kernel (4.3 TB/s, of 4.9 that a large copy reaches)
+// and 5 the join; 64 sequences of 1 to 4096 tokens, 81 MB, 23.2 us (3.5 TB/s) and
+// 4.6: their many short units cost a wait for the first codes each.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -535,7 +540,7 @@ struct Cut {
 };
 
 // A call's workgroups.  Sequences are split where that spares a workgroup more than three blocks of tokens: the join
-// is a launch of its own (777 tokens of two heads: 8 us in one launch, 10 us in two).
+// is a launch of its own (777 tokens of two heads: 7.9 us in one launch, 10 in two).
 Cut cut(int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int dim, int64_t room) {
     Cut c;
     c.tiles = (q_len * (heads / kv_heads) + 15) / 16;
