@@ -55,9 +55,11 @@ struct PromptArgs {
 template <int DIM, int ROWS, int TEAMS, int KEYS> struct Shape {
     static constexpr int kRow = DIM * 2, kPiecesRow = kRow / 16;
     static constexpr int kTile = KEYS * kRow;
-    // Wide heads: two waves share 32 rows, each with half the dimensions of the result.  Both work out the scores, half
-    // again as many products in all, but the registers of one wave do not hold the whole result.
+    // Wide heads: two waves share 32 rows, each with half the dimensions of the result, because the registers of one wave
+    // do not hold the whole.  Where a tile has two blocks of 32 keys (kSplit), each works out the probabilities of one
+    // and they exchange them in LDS; else both work out all scores, half again as many products.
     static constexpr int kShare = DIM > 128 ? 2 : 1, kOut = DIM / 32 / kShare;
+    static constexpr bool kSplit = kShare == 2 && KEYS == 64;
     static constexpr int kBlocks = ROWS / 32, kTeam = kBlocks * kShare, kWaves = kTeam * TEAMS;
     static constexpr int kPieces = KEYS * kPiecesRow / (64 * kTeam);    // of a tile, for a thread
     // K is read 16 rows at a time, the same piece of each: they have to stand in 16 different columns.  Of a row's
@@ -141,15 +143,25 @@ __global__ __launch_bounds__((64 * Shape<DIM, ROWS, TEAMS, KEYS>::kWaves), 2) vo
     typedef typename M::T8 T8;
     typedef typename M::T2 T2;
     typedef Shape<DIM, ROWS, TEAMS, KEYS> S;
-    constexpr int kB = KEYS / 32;                           // 32-key blocks of a tile
+    constexpr int kB = KEYS / 32, kMine = S::kSplit ? 1 : kB;   // 32-key blocks of a tile, and those whose scores a wave takes
     // probabilities are held 2^6 higher in fp16, whose small numbers end at 2^-24
     constexpr float kLift = TYPE == WINO_FP16 ? 6.f : 0.f;
     constexpr int kAhead = DIM <= 128 ? kB * DIM / 16 : (DIM == 192 ? 12 : 8);
-    static_assert(kB * DIM / 16 % kAhead == 0, "whole groups");  // pieces of K read before they are multiplied
+    static_assert(kMine * DIM / 16 % kAhead == 0, "whole groups");  // pieces of K read before they are multiplied
     __shared__ __attribute__((aligned(256))) uint8_t lds[TEAMS][2][2 * S::kTile];
+    constexpr int kXWaves = S::kSplit ? S::kWaves : 1;      // what the waves of a pair exchange, and who has outgrown ref
+    __shared__ u32x4 p_lds[kXWaves][2][64];
+    __shared__ float top_lds[kXWaves][64];
+    __shared__ uint32_t grown[kXWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 31, half = lane >> 5;
     const int team = wave / S::kTeam, mate = wave % S::kTeam, d0 = mate / S::kBlocks * (S::kOut * 32);   // d0: first dimension
+    // kSplit: the block of keys that is this wave's, and the wave that has the other one (TEAMS is 1)
+    const int mine = S::kSplit ? mate / S::kBlocks : 0, partner = S::kSplit ? wave ^ S::kBlocks : 0;
+    auto meet = [&]() {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what was written to LDS; the next tile stays on its way
+        winof4::ring_barrier();
+    };
 
     // Workgroups that follow each other run on different XCDs: a K and V stays with one or two of them.
     const int kvh = blockIdx.x % a.kv_heads;
@@ -252,30 +264,33 @@ __global__ __launch_bounds__((64 * Shape<DIM, ROWS, TEAMS, KEYS>::kWaves), 2) vo
             }
             spoilt = __syncthreads_or(spoilt);
         }
-        if (t0 >= wave_end) continue;
+        const bool busy = t0 < wave_end;                    // both waves of a pair alike
+        if (!S::kSplit && !busy) continue;
         // Addresses of a wave's pieces differ by exchanged bits.  Wide heads have no registers to keep them all: there
         // they are made anew from the row in each tile.
         int ck = c, lane_v = lane;
         if constexpr (DIM > 128) asm("" : "+v"(ck), "+v"(lane_v));
 
-        f32x16 z[kB];
+        f32x16 z[kMine];
 #pragma unroll
-        for (int b = 0; b < kB; ++b)
+        for (int b = 0; b < kMine; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) z[b][e] = 0.f;
+        if (busy) {
 #pragma unroll
-        for (int f0 = 0; f0 < kB * DIM / 16; f0 += kAhead) {
-            T8 k[kAhead];
+            for (int f0 = 0; f0 < kMine * DIM / 16; f0 += kAhead) {
+                T8 k[kAhead];
 #pragma unroll
-            for (int f = 0; f < kAhead; ++f) {
-                const int key = (f0 + f) / (DIM / 16) * 32 + ck, s = (f0 + f) % (DIM / 16);
-                k[f] = *(const T8*)(lk + key * S::kRow + (((2 * s + half) ^ S::swap_k(key)) * 16));
-            }
-            __builtin_amdgcn_sched_barrier(0);
+                for (int f = 0; f < kAhead; ++f) {
+                    const int key = (mine + (f0 + f) / (DIM / 16)) * 32 + ck, s = (f0 + f) % (DIM / 16);
+                    k[f] = *(const T8*)(lk + key * S::kRow + (((2 * s + half) ^ S::swap_k(key)) * 16));
+                }
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int f = 0; f < kAhead; ++f) {
-                const int b = (f0 + f) / (DIM / 16);
-                z[b] = M::mul(k[f], q[(f0 + f) % (DIM / 16)], z[b]);
+                for (int f = 0; f < kAhead; ++f) {
+                    const int b = (f0 + f) / (DIM / 16);
+                    z[b] = M::mul(k[f], q[(f0 + f) % (DIM / 16)], z[b]);
+                }
             }
         }
         // the first half of V is read while the scores are turned into probabilities
@@ -294,19 +309,19 @@ __global__ __launch_bounds__((64 * Shape<DIM, ROWS, TEAMS, KEYS>::kWaves), 2) vo
             }
         };
         T8 v[2][S::kOut];
-        read_v(0, 0, v[0]);
-        read_v(0, 1, v[1]);
+        read_v(mine, 0, v[0]);
+        read_v(mine, 1, v[1]);
         __builtin_amdgcn_sched_barrier(0);
         if (t0 + KEYS > wave_every) {
 #pragma unroll
-            for (int b = 0; b < kB; ++b)
+            for (int b = 0; b < kMine; ++b)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    if (t0 + 32 * b + 8 * (e / 4) + 4 * half + e % 4 >= row_end) z[b][e] = kNever;
+                    if (t0 + 32 * (mine + b) + 8 * (e / 4) + 4 * half + e % 4 >= row_end) z[b][e] = kNever;
         }
-        float part[kB];
+        float part[kMine];
 #pragma unroll
-        for (int b = 0; b < kB; ++b) {
+        for (int b = 0; b < kMine; ++b) {
             part[b] = max3(z[b][0], z[b][1], z[b][2]);
 #pragma unroll
             for (int e = 3; e < 15; e += 2) part[b] = max3(z[b][e], z[b][e + 1], part[b]);
@@ -314,38 +329,74 @@ __global__ __launch_bounds__((64 * Shape<DIM, ROWS, TEAMS, KEYS>::kWaves), 2) vo
         }
         float top;
         {
-            const f32x2 x = swap_rows<2>(part[kB - 1]);
+            const f32x2 x = swap_rows<2>(part[kMine - 1]);
             top = max3(x[0], x[1], x[1]) * a.scale_log2;
         }
         // o and sum move to a new reference only where the maximum has outgrown the old one by 2^8
-        if (__any(top > ref + 8.f)) {
-            const float to = __builtin_fmaxf(ref, top);
+        auto outgrow = [&](float by) {
+            const float to = __builtin_fmaxf(ref, by);
             const float alpha = to == kNever ? 1.f : __builtin_amdgcn_exp2f(ref - to);
             ref = to;
             sum *= alpha;
 #pragma unroll
             for (int n = 0; n < S::kOut; ++n) o[n] *= alpha;
-        }
-        const float base = ref == kNever ? 0.f : kLift - ref;
-        uint32_t p[kB][8];
+        };
+        uint32_t p[kB][8];                                  // kSplit: this wave's block first
+        float add[kMine];                                   // the rounded probabilities: they are the weights
+        auto weigh = [&]() {
+            const float base = ref == kNever ? 0.f : kLift - ref;
 #pragma unroll
-        for (int b = 0; b < kB; ++b) {
-            float add = 0.f;                                // the rounded probabilities: they are the weights
+            for (int b = 0; b < kMine; ++b) {
+                add[b] = 0.f;
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) {
-                const T2 x = {(T)__builtin_amdgcn_exp2f(__builtin_fmaf(z[b][e], a.scale_log2, base)),
-                              (T)__builtin_amdgcn_exp2f(__builtin_fmaf(z[b][e + 1], a.scale_log2, base))};
-                add = M::pair_sum(x, add);
-                p[b][e / 2] = __builtin_bit_cast(uint32_t, x);
+                for (int e = 0; e < 16; e += 2) {
+                    const T2 x = {(T)__builtin_amdgcn_exp2f(__builtin_fmaf(z[b][e], a.scale_log2, base)),
+                                  (T)__builtin_amdgcn_exp2f(__builtin_fmaf(z[b][e + 1], a.scale_log2, base))};
+                    add[b] = M::pair_sum(x, add[b]);
+                    p[b][e / 2] = __builtin_bit_cast(uint32_t, x);
+                }
             }
-            sum += add;
+        };
+        if constexpr (!S::kSplit) {
+            if (__any(top > ref + 8.f)) outgrow(top);
+            weigh();
+        } else {
+            // Both waves of a pair hold the same reference.  Hardly ever has a maximum outgrown it: the probabilities are
+            // worked out and handed over as if none had, and again where one has.
+            auto hand_over = [&]() {
+                weigh();
+#pragma unroll
+                for (int x = 0; x < 2; ++x) p_lds[wave][x][lane] = u32x4{p[0][4 * x], p[0][4 * x + 1], p[0][4 * x + 2], p[0][4 * x + 3]};
+            };
+            const bool grows = busy && __any(top > ref + 8.f);
+            if (busy && !grows) hand_over();
+            if (lane == 0) grown[wave] = grows;
+            meet();
+            if (__any(lane < S::kWaves && grown[lane % kXWaves] != 0)) {
+                top_lds[wave][lane] = top;
+                meet();
+                if (busy) {
+                    outgrow(__builtin_fmaxf(top, top_lds[partner][lane]));
+                    hand_over();
+                }
+                meet();
+            }
+            if (!busy) continue;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const u32x4 y = p_lds[partner][x][lane];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) p[kB - 1][4 * x + k] = y[k];
+            }
         }
+#pragma unroll
+        for (int b = 0; b < kMine; ++b) sum += add[b];
 #pragma unroll
         for (int b = 0; b < kB; ++b)
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const T8 pp = __builtin_bit_cast(T8, u32x4{p[b][4 * s], p[b][4 * s + 1], p[b][4 * s + 2], p[b][4 * s + 3]});
-                if (b > 0) read_v(b, s, v[s]);
+                if (b > 0) read_v(S::kSplit ? 1 - mine : b, s, v[s]);
 #pragma unroll
                 for (int n = 0; n < S::kOut; ++n) o[n] = M::mul(v[s][n], pp, o[n]);
             }
@@ -392,6 +443,13 @@ __global__ __launch_bounds__((64 * Shape<DIM, ROWS, TEAMS, KEYS>::kWaves), 2) vo
     {
         const f32x2 x = swap_rows<2>(sum);
         sum = x[0] + x[1];
+    }
+    if constexpr (S::kSplit) {                              // the other wave's keys
+        __syncthreads();
+        top_lds[wave][lane] = sum;
+        __syncthreads();
+        const float other = top_lds[partner][lane];
+        sum = mine == 0 ? sum + other : other + sum;
     }
     if (team == 0) {
         // the halves of the wave exchange four dimensions of sixteen, so that a lane stores eight neighbours
