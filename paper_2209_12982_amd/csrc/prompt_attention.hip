@@ -23,6 +23,7 @@
 // 57% of the cycles, at the clock that this load leaves (1.6 to 1.8 GHz).  Twelve
 // packed ones of up to 2048, 32 heads on 8: 143 us, 0.78 PFLOP/s, 40%: their
 // workgroups walk over eight tiles on average, and begin and end in between.
+// Heads of 256: four sequences of 4096, 16 heads on 4, 659 us, 0.84 PFLOP/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -484,17 +485,17 @@ template <int TYPE, int DIM, int ROWS, int TEAMS, int KEYS> wino_status launch(c
                        dim3(64 * Shape<DIM, ROWS, TEAMS, KEYS>::kWaves), 0, stream, a);
     return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
 }
-// Tiles of 128 rows by one team once they fill the device twice over (once for wide heads, whose workgroups take a whole
-// compute unit); before that 64 rows by two teams, and by four where the keys are many and the tiles very few.  Heads of
+// Tiles of 128 rows by one team once they fill the device twice over (more than once for wide heads, whose workgroups
+// take a whole compute unit); before that 64 rows by two teams, and by four where the keys are many and the tiles very few.  Heads of
 // 128, causal, us for one team of 128 / two of 64 / four of 64:
 //   1 x 256, 16 heads (32 tiles) 11.8 / 9.8 / 11.2      1 x 512 on 4096 keys, 8 heads (32) 80 / 53 / 44
 //   1 x 1024, 16 heads (128) 26.0 / 19.4 / 19.0         1 x 2048, 16 heads (256) 45 / 35 / 38
 //   4 x 512, 32 heads (512) 25.6 / 27.3 / 42.9          8 x 512, 32 heads (1024) 41 / 49 / 84
-// and of 256 for one / two: 1 x 2048, 16 heads (256) 85 / 72, 1 x 3000 (376) 127 / 148.
+// and of 256 for one / two: 1 x 1700, 16 heads (216) 67 / 56, 1 x 2048 (256) 80 / 72, 1 x 2500 (316) 94 / 108.
 template <int TYPE, int DIM> wino_status pick(const PromptArgs& a, int max_q, hipStream_t stream) {
     // tiles of 128 rows that have something to do, by the longest sequence's length
     const int64_t busy = std::min(tiles(a, 128), (((int64_t)max_q * a.group + 127) / 128) * a.seqs * a.kv_heads);
-    if (busy >= (DIM > 128 ? 320 : 512)) return launch<TYPE, DIM, 128, 1, 64>(a, stream);
+    if (busy >= (DIM > 128 ? 257 : 512)) return launch<TYPE, DIM, 128, 1, 64>(a, stream);
     if constexpr (DIM <= 128)
         if (busy <= 128 && a.total_k / a.seqs >= 1024) return launch<TYPE, DIM, 64, 4, 32>(a, stream);
     return launch<TYPE, DIM, 64, 2, 32>(a, stream);

@@ -206,6 +206,32 @@ def test_prompt_few_queries_on_many_keys(d, name):
         _hold(host(out), ref, bound)
 
 
+@pytest.mark.parametrize("name", ["bf16", "fp16"])
+@pytest.mark.parametrize("d", [128, 192, 256])
+def test_prompt_maxima_that_keep_growing(d, name):
+    """Keys that grow along the sequence, so that the largest score is outgrown
+    again and again, in one wave or another; a sample of the rows."""
+    torch = torch_dev()
+    rng = np.random.default_rng(d + 5)
+    lens, heads = [700, 690, 701, 650], 16
+    n = sum(lens)
+    grow = np.concatenate([np.linspace(0.1, 4, m) for m in lens])[:, None, None]
+    q, qv = half(torch, 3 * rng.normal(0, 1, (n, heads, d)), name)
+    k, kv = half(torch, grow * rng.normal(0, 1, (n, heads, d)), name)
+    v, vv = half(torch, rng.normal(0, 1, (n, heads, d)), name)
+    out = torch.full(q.shape, float("nan"), dtype=q.dtype, device="cuda")
+    W.prompt_attention(q, k, v, _cu(torch, lens), _cu(torch, lens), max(lens), out, d ** -0.5)
+    got = host(out)
+    begin = 0
+    for m in lens:
+        for i in [0, 31, 32, 63, 64, 127, 128, m - 1] + list(range(50, m, 113)):
+            for h in (0, 7, 15):
+                r, w, z = decoder.attend(qv[begin + i, h], kv[begin:begin + m, h], vv[begin:begin + m, h],
+                                         np.arange(i + 1), d ** -0.5)
+                _hold(got[begin + i, h], r, attention_bound(r, w, z, i + 1, d, name, ROUND[name]))
+        begin += m
+
+
 def test_prompt_offsets_that_fall():
     """Offsets below 0 and falling ones, down to the type's lowest value: such
     sequences are empty, the others are not touched by it."""
