@@ -211,6 +211,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
     const int first_end = len - a.q_len + 1;                // tokens that query 0 sees; every row sees those
     const int begin = max(blk - 1, 0) * kBlock;
     const int end = a.pages == 0 ? begin : min((int64_t)len, (int64_t)(blk + take - 1) * kBlock);
+    // one step or less is one wave's work, and needs no join
+    const bool alone = WAVES == 8 && end <= S::kTok;
+    if (alone && wave > 0) return;
 
     // this lane's row: query i, head h
     const int row = tile * 16 + r;
@@ -407,6 +410,16 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
         have = have_next;
     }
     sum = sum_rows(sum);
+    if (alone) {
+        typedef T T4 __attribute__((ext_vector_type(4)));
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        T* out = (T*)a.out + (((int64_t)b * a.q_len + i) * a.heads + h) * DIM + 4 * g;
+#pragma unroll
+        for (int n = 0; n < DIM / 16; ++n)
+            if (real)
+                *(T4*)(out + 16 * n) = sum == 0.f ? T4{} : T4{(T)(o[n][0] * inv), (T)(o[n][1] * inv), (T)(o[n][2] * inv), (T)(o[n][3] * inv)};
+        return;
+    }
 
     // join the waves: [wave][row][dim + 4]
     const int rows = min(16, a.q_len * a.group - tile * 16);
