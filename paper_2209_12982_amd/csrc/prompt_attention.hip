@@ -419,6 +419,7 @@ __global__ __launch_bounds__((64 * Shape<DIM, ROWS, TEAMS, KEYS>::kWaves), 2) vo
     // the upper half of the teams hands over to the lower half, until one is left
 #pragma unroll
     for (int left = TEAMS / 2; left > 0; left /= 2) {
+        if (end <= left * KEYS) continue;                   // that half had no keys
         float* at = (float*)lds + ((team % left) * S::kTeam + mate) * (S::kOut * 16 + 2) * 64 + lane;
         __syncthreads();
         if (team >= left && team < 2 * left) {
