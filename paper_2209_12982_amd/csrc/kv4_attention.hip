@@ -19,9 +19,9 @@
 // then exact in fp32.
 //
 // 32 heads of 128 on 8: two sequences of 131072 tokens, 157 MB of cache, take
-// 40.2 us, 36.1 of them this kernel (4.3 TB/s, of 4.9 that a large copy reaches)
-// and 5 the join; 64 sequences of 1 to 4096 tokens, 81 MB, 23.2 us (3.5 TB/s) and
-// 4.6: their many short units cost a wait for the first codes each.
+// 39.7 us, 35 of them this kernel (4.5 TB/s, of 4.9 that a large copy reaches);
+// 64 sequences of 1 to 4096 tokens, 81 MB, 23 us (3.5 TB/s) and 4.5 for the
+// join: their many short units cost a wait for the first codes each.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -479,10 +479,10 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
 
 // Joins the parts of units that several workgroups shared: one workgroup per query row and head; groups of DIM / 4
 // threads take the parts in turn.
-template <int TYPE, int DIM> __global__ __launch_bounds__(256) void kv4_join_kernel(DecodeArgs a) {
+template <int TYPE, int DIM, int THREADS> __global__ __launch_bounds__(THREADS) void kv4_join_kernel(DecodeArgs a) {
     typedef typename Half<TYPE>::type T;
     typedef T T4 __attribute__((ext_vector_type(4)));
-    constexpr int kCols = DIM / 4, kTeams = 256 / kCols;
+    constexpr int kCols = DIM / 4, kTeams = THREADS / kCols;
     __shared__ f32x4 acc_s[kTeams][kCols];
     __shared__ float m_s[kTeams], total_s[kTeams];
     const int token = divide((int)blockIdx.x, a.by_heads), h = (int)blockIdx.x - token * a.heads;
@@ -553,7 +553,7 @@ struct Cut {
 };
 
 // A call's workgroups.  Sequences are split where that spares a workgroup more than three blocks of tokens: the join
-// is a launch of its own (777 tokens of two heads: 7.9 us in one launch, 10 in two).
+// is a launch of its own (777 tokens of two heads: 8.0 us in one launch, 10 in two).
 Cut cut(int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int dim, int64_t room) {
     Cut c;
     c.tiles = (q_len * (heads / kv_heads) + 15) / 16;
@@ -573,7 +573,11 @@ template <int TYPE, int DIM> wino_status launch(const DecodeArgs& a, int64_t row
     }
     hipLaunchKernelGGL((kv4_attention_kernel<TYPE, DIM, 4>), grid, dim3(256), 0, stream, a);
     if (hipGetLastError() != hipSuccess) return WINO_EHIP;
-    hipLaunchKernelGGL((kv4_join_kernel<TYPE, DIM>), dim3((unsigned)rows), dim3(256), 0, stream, a);
+    // few rows have many parts each (64 rows of 48: 39.7 us the call, with 256 threads 40.3), many rows few
+    if (rows <= 256)
+        hipLaunchKernelGGL((kv4_join_kernel<TYPE, DIM, 512>), dim3((unsigned)rows), dim3(512), 0, stream, a);
+    else
+        hipLaunchKernelGGL((kv4_join_kernel<TYPE, DIM, 256>), dim3((unsigned)rows), dim3(256), 0, stream, a);
     return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
 }
 
