@@ -515,7 +515,9 @@ template <int TYPE, int DIM, int THREADS> __global__ __launch_bounds__(THREADS) 
             acc *= f;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                if (mw[k] == kNever) continue;              // also what stands in for a part that is not there
+                // what stands in for a part that is not there is left out by its index: a part of minus infinity may be
+                // one whose scores are all NaN, whose total says so (0 times NaN is NaN; a part that saw nothing adds 0)
+                if (w + k * kTeams > w1) continue;
                 const float fw = __builtin_amdgcn_exp2f(mw[k] - base);
                 total += tw[k] * fw;
                 acc += x[k] * fw;
