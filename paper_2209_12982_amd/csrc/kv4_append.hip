@@ -151,12 +151,12 @@ extern "C" wino_status kv4_append(const void* q, int64_t q_stride, const void* k
     const kv4_cache& c = *cache;
     if (c.pages < 0 || c.kv_heads < 1 || c.page_size < 1 || tokens < 0 || heads < 0 || table_rows < 0 || rot < 0)
         return WINO_EINVAL;
-    if (c.head_dim < 1 || rot > c.head_dim || (heads > 0) != (q_out != nullptr)) return WINO_EINVAL;
+    if (c.head_dim < 1 || rot > c.head_dim) return WINO_EINVAL;
     if (c.page_size % 16 || c.head_dim % kGroup || c.head_dim > 256 || rot % 16) return WINO_EUNSUPPORTED;
     if (c.kv_heads > 4096 || heads > 65536 || c.pages > (int64_t)1 << 40 || c.page_size > 1 << 20)
         return WINO_EUNSUPPORTED;
-    if (tokens == 0) return WINO_OK;
-    if ((heads > 0 && !q) || !k || !v || (rot > 0 && !cos_sin) || !positions || !slots) return WINO_EINVAL;
+    if (tokens == 0) return WINO_OK;                    // empty tensors may have no address
+    if ((heads > 0) != (q_out != nullptr) || (heads > 0 && !q) || !k || !v || (rot > 0 && !cos_sin) || !positions || !slots) return WINO_EINVAL;
     if (c.pages > 0 && (!c.k_codes || !c.k_scales || !c.v_codes || !c.v_scales)) return WINO_EINVAL;
     const int64_t dim = c.head_dim;
     if (tokens > 1 && ((heads > 0 && q_stride < heads * dim) || k_stride < c.kv_heads * dim || v_stride < c.kv_heads * dim))

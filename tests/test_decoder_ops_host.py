@@ -119,3 +119,12 @@ def test_refusals_without_a_device():
                      ({"scale": float("nan")}, -1), ({"qs": 200}, -1), ({"ks": 100}, -1), ({"vs": 100}, -1),
                      ({"vs": 132}, -2), ({"v": p + 4}, -2), ({"tq": 0}, 0)):
         assert prompt(**kw) == want, kw
+
+
+def test_append_of_no_tokens_needs_no_addresses():
+    """An empty tensor's address may be null: queries of no tokens are no reason to refuse."""
+    lib = _lib()
+    c = W.binding._KV4Cache(k_codes=64, k_scales=64, v_codes=64, v_scales=64, pages=2, kv_heads=2, page_size=16, head_dim=64)
+    for heads in (0, 4):
+        assert lib.kv4_append(None, 256, None, 128, None, 128, 0, heads, None, 0, 64, None, None, ctypes.byref(c), None,
+                              None, None, 0, 0, 0, None) == 0

@@ -203,3 +203,12 @@ def test_append_refuses_other_tensors():
         with pytest.raises(W.WinoError) as e:
             bad()
         assert e.value.status == status
+
+
+def test_append_no_tokens_with_queries():
+    torch = torch_dev()
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt, device="cuda")  # noqa: E731
+    cache = _cache(torch, 2, 2, 16, 64)
+    W.kv4_append(z(0, 4, 64), z(0, 2, 64), z(0, 2, 64), z(9, 64, dt=torch.float32), z(0, dt=torch.int32),
+                 z(0, dt=torch.int64), cache, z(0, 4, 64), z(0, 2, 64), z(0, 2, 64))
+    assert all(bool((c == 0xA5).all()) for c in cache)
