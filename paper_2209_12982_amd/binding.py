@@ -593,6 +593,31 @@ class _KV4Cache(ctypes.Structure):
 
 
 _MARSHAL = None
+_CURRENT = _CURRENT_STREAM = None     # index of the current GPU, and the raw handle of a GPU's current stream
+
+
+def _place(stream):
+    """The stream's handle, and the index of the GPU that a launch goes to."""
+    if stream is None and _CURRENT:
+        device = _CURRENT()
+        return _CURRENT_STREAM(device), device
+    return _find_place(stream)
+
+
+def _find_place(stream):
+    """_place of a stream that is given, or of the first call."""
+    import torch
+    global _CURRENT, _CURRENT_STREAM
+    if not _CURRENT:
+        torch.cuda.current_stream()              # initializes the device state
+        _CURRENT_STREAM = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda device: torch.cuda.current_stream(device).cuda_stream)
+        _CURRENT = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    device = _CURRENT()
+    own = getattr(stream, "device", None)        # a plain handle is taken to be one of the current GPU's
+    if own is not None and own.index != device:
+        raise ValueError(f"stream: expected one of the current GPU ({device}), got one of {own}")
+    return _CURRENT_STREAM(device) if stream is None else _stream(stream), device
 
 
 def _marshal():
@@ -626,7 +651,8 @@ def w4_matvec_workspace_bytes(m, n, k):
 
 def w4_matvec(x, codes, scales, y, bias=None, workspace=None, stream=None):
     """y [m, n] = x [m, k] times the 4-bit weights [n, k] transposed, + bias."""
-    st = (_MARSHAL or _marshal()).w4_matvec(x, codes, scales, y, bias, workspace, _stream(stream))
+    handle, device = _place(stream)
+    st = (_MARSHAL or _marshal()).w4_matvec(x, codes, scales, y, bias, workspace, handle, device)
     if st:
         _check(st, "w4_matvec")
 
@@ -635,8 +661,9 @@ def kv4_append(q, k, v, cos_sin, positions, slots, cache, q_out=None, k_out=None
                values=KV4_ROTATED, stream=None):
     """Turns q [tokens, heads, d] (or None) and k [tokens, kv_heads, d], puts k
     and v into `cache` (k_codes, k_scales, v_codes, v_scales) at `slots`."""
+    handle, device = _place(stream)
     st = (_MARSHAL or _marshal()).kv4_append(q, k, v, cos_sin, positions, slots, cache, q_out, k_out, v_out, rotary,
-                                             values, _stream(stream))
+                                             values, handle, device)
     if st:
         _check(st, "kv4_append")
 
@@ -649,7 +676,8 @@ def kv4_attention_workspace_bytes(batch, q_len, heads, kv_heads, head_dim, max_p
 def kv4_attention(q, cache, block_table, lens, out, scale, workspace=None, stream=None):
     """out = attention of q [batch * q_len, heads, d] over the cached tokens of
     each sequence; block_table int32 [batch, max_pages], lens int32 [batch]."""
-    st = (_MARSHAL or _marshal()).kv4_attention(q, cache, block_table, lens, out, scale, workspace, _stream(stream))
+    handle, device = _place(stream)
+    st = (_MARSHAL or _marshal()).kv4_attention(q, cache, block_table, lens, out, scale, workspace, handle, device)
     if st:
         _check(st, "kv4_attention")
 
@@ -657,6 +685,7 @@ def kv4_attention(q, cache, block_table, lens, out, scale, workspace=None, strea
 def prompt_attention(q, k, v, cu_q, cu_k, max_q, out, scale, causal=True, stream=None):
     """out = attention of the packed queries q [total_q, heads, d] over k, v
     [total_k, kv_heads, d]; cu_q, cu_k int32 [seqs + 1]."""
-    st = (_MARSHAL or _marshal()).prompt_attention(q, k, v, cu_q, cu_k, max_q, out, scale, causal, _stream(stream))
+    handle, device = _place(stream)
+    st = (_MARSHAL or _marshal()).prompt_attention(q, k, v, cu_q, cu_k, max_q, out, scale, causal, handle, device)
     if st:
         _check(st, "prompt_attention")
