@@ -128,3 +128,15 @@ def test_append_of_no_tokens_needs_no_addresses():
     for heads in (0, 4):
         assert lib.kv4_append(None, 256, None, 128, None, 128, 0, heads, None, 0, 64, None, None, ctypes.byref(c), None,
                               None, None, 0, 0, 0, None) == 0
+
+
+def test_matvec_parts_count_the_rows_of_x():
+    """k is cut into parts only to make 256 workgroups of 64 x 64 results at most; many rows of x are workgroups
+    enough, so the parts' sums never need more than their 4 MiB."""
+    _lib()
+    for n in (40, 1000, 4096, 4100, 8192, 16384):
+        for k in (1024, 4096, 8192, 16384, 1 << 20):
+            for m in (1, 16, 17, 64, 65, 130, 512, 2048, 8192, 65535):
+                assert W.w4_matvec_workspace_bytes(m, n, k) <= 4 << 20, (m, n, k)
+    assert W.w4_matvec_workspace_bytes(64, 4096, 16384) > 0          # a few rows still are cut
+    assert W.w4_matvec_workspace_bytes(128, 1024, 16384) > 0
