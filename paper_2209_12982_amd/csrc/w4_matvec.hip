@@ -437,41 +437,60 @@ struct Cut {
     int waves = 8;
 };
 
-// Few workgroups read x few times, many keep the device busy; a second launch, for the join, costs 3 us.  Measured (us,
-// bf16, rows of x / n / k; r, parts):
-//   x in LDS             1/4096/4096: 16 waves 4.7, 8 waves 5.1      4/4096/4096: r1 5.9, r2 7.7
-//                        4/16384/4096: r2 12.2, r1 15.4, wide 13.8
-//                        64/2048/1248: 16 waves 4.3, wide 6.8     64/4096/1248: 16 waves 7.0, wide 6.9
-//   x beside the codes   8/4096/4096: r1 6.6, wide in 2 7.8          8/8192/8192: r2 14.9, wide in 2 15.8
-//                        1/1024/16384: r2 in 8 7.9, r1 10.9          4/4096/16384: r2 in 2 15.9, wide in 4 16.3
-//   wide, one tile of x  8/32768/2048: r2 12.6, x in LDS 14.1        16/32768/2048: r2 13.2, beside the codes 16.4
-//                        16/16384/4096: r1 14.4, r2 14.6, beside 15.1
-//                        16/1024/16384: r1 in 8 9.6, beside in 4 12.4   16/4096/16384: r2 in 4 18.0, beside 18.4
-//   two                  32/4096/4096: r1 in 2 9.4, r2 in 4 9.9      32/2048/4096: r1 in 4 8.0, r2 in 4 9.5
-//                        32/8192/8192: r2 in 2 19.3, r1 20.9         32/16384/4096: r2 16.5, r1 18.2
-//   four                 64/4096/1024: r1 5.8, r2 7.7                64/4096/16384: r2 in 4 24.2, r1 in 2 30.4
-//                        64/8192/8192: r2 in 2 23.8, r1 28.5         64/16384/4096: r2 20.4, r1 29.4
-Cut cut(int64_t m, int64_t n, int64_t k) {
-    // as many parts as make a workgroup for each of 256 compute units, no more, with 1024 of k in each at least; more than
-    // 64 rows of x are tiles of their own (2048 rows by 4096 x 16384 in 4 parts took 534 us and 128 MB, whole 430)
-    const int64_t x_tiles = (m + 63) / 64;
-    auto parts = [&](int rows) {
-        const int64_t groups = (n + rows - 1) / rows * x_tiles;
-        return (int)std::max<int64_t>(1, std::min<int64_t>(256 / groups, k / 1024));
-    };
-    const bool fits = std::min<int64_t>(m, 16) * (2 * k + 16) <= 40960;
-    if (k >= 128 && ((m > 16 && !(fits && n <= 4096)) || (n > 8192 && (m > 4 || !fits)) || (m > 8 && n <= 4096 && k >= 8192))) {
-        const int r = n > 8192 || (n >= 4096 && k >= 8192) ? 2 : 1;
-        return Cut{true, r, parts(32 * r)};
+// A kernel that does not hold x in LDS whole, and what it takes (us, measured): `step` for 1024 of k and `start` beside
+// it, for as many workgroups as there are compute units (256) or fewer; `pair` times that for twice as many, side by side.
+struct Form {
+    bool wide;
+    int r;
+    double step, start, pair;
+    // k in `splits` parts: whole rounds of the device, and the join, a second launch
+    double time(int64_t m, int64_t n, int64_t k, int splits) const {
+        const int64_t rows = (wide ? 32 : 16) * r, x_tiles = wide ? (m + 63) / 64 : 1;
+        const int64_t groups = (n + rows - 1) / rows * x_tiles * splits, rest = groups % 512;
+        const double rounds = pair * (double)(groups / 512) + (rest == 0 ? 0 : (rest <= 256 ? 1 : pair));
+        const double join = splits > 1 ? 2.2 + 0.21 * splits + 3.8e-6 * (double)(splits * m * n) : 0;
+        return (start + step * (double)k / (1024 * splits)) * rounds + join;
     }
-    if (n <= 4096 && k >= 8192 && (!fits || (n <= 2048 && k >= 12288))) return Cut{false, 2, parts(32)};
-    if (fits) return Cut{false, n <= 8192 ? 1 : 2, 1, true, n <= 4096 ? 16 : 8};
-    return Cut{false, n <= 4096 ? 1 : 2, 1};
+};
+
+// x in LDS while it fits and there is little of it beside W: one row of 4096 x 4096 4.7 us (beside the codes 5.3), four
+// 5.2 (5.9); with 16 waves for few outputs (eight: 5.2 and 5.8).  64 rows by 2048 x 1248: 4.3 (wide 6.8).  Else what is
+// estimated to be the shortest: over 737 sizes of 1 to 64 rows, 512 to 32768 outputs and k of 1024 to 16384 (bf16) that is
+// 1% longer than the shortest measured one on average, 20% at most.  With parts only while a workgroup for each compute unit
+// holds them all it was 6% on average and 50% at most, beside whole rounds.  Some of them (us; w: wide, n: beside the codes,
+// tiles of W, parts):
+//   16 rows, k 16384   4096 outputs w1 in 4 17.8, w2 in 4 17.8, w1 30.4     4160 w1 in 3 22.0, w1 in 4 22.6, n2 31.3, w1 30.9
+//                      5120 w1 in 3 22.6, w2 in 3 22.3, n2 31.8             8256 w2 in 3 33.8, w2 46.1
+//   8 rows             4096 x 4096 n1 6.6, w1 in 2 7.8                      8192 x 8192 n2 14.9, w1 in 2 15.9
+//   32 rows            4096 x 4096 w1 in 2 9.5, w2 in 4 9.9                 8192 x 8192 w1 20.5, w2 in 2 19.1 (taken: w1)
+//   64 rows            16384 x 4096 w2 20.1, w1 29.3
+//   2048 rows          4096 x 16384 whole 430, in 4 parts 534 and 128 MB of sums
+Cut cut(int64_t m, int64_t n, int64_t k) {
+    const bool fits = std::min<int64_t>(m, 16) * (2 * k + 16) <= 40960;
+    const bool little = (m <= 16 || n <= 4096) && (m <= 4 || n <= 8192) && !(n <= 2048 && k >= 12288);
+    if (fits && (little || k < 128)) return Cut{false, n <= 8192 ? 1 : 2, 1, true, n <= 4096 ? 16 : 8};
+    const double rows = 1 + 0.062 * (double)m;              // beside the codes, each row of x is read by each wave
+    const Form one[] = {{false, 1, 0.64 * rows, 0.23, 2}, {false, 2, 0.93 * rows, 0.23, 2}, {true, 1, 1.64, 0.15, 1.52}, {true, 2, 3.2, 0.15, 1.52}};
+    const Form two[] = {{true, 1, 2.03, 0.3, 1.6}, {true, 2, 3.25, 0.3, 1.6}};
+    const Form four[] = {{true, 1, 3.3, 0.1, 1.8}, {true, 2, 4.69, 0.1, 1.8}};
+    const Form* forms = m <= 16 ? one : (m <= 32 ? two : four);
+    Cut best{};
+    double least = 0;
+    for (int f = 0; f < (m <= 16 ? 4 : 2); ++f)
+        for (const int splits : {1, 2, 3, 4, 6, 8}) {
+            // 1024 of k in a part at least, and 4 MiB of sums at most
+            if (splits > 1 && (k < 1024 * splits || splits * m * n > 1 << 20)) break;
+            const double t = forms[f].time(m, n, k, splits);
+            if (least == 0 || t < least) least = t, best = Cut{forms[f].wide, forms[f].r, splits};
+        }
+    return best;
 }
 
-template <int TYPE> void pick(const MatvecArgs& a, bool room, hipStream_t stream) {
+size_t part_bytes(const Cut& c, int64_t m, int64_t n) { return c.splits > 1 ? (size_t)(c.splits * m * n) * sizeof(float) : 0; }
+
+template <int TYPE> void pick(const MatvecArgs& a, size_t bytes, hipStream_t stream) {
     const Cut c = cut(a.m, a.n, a.k);
-    const int s = room ? c.splits : 1;
+    const int s = a.part && bytes >= part_bytes(c, a.m, a.n) ? c.splits : 1;
     if (c.wide && a.m > 32)
         c.r == 1 ? launch_wide<TYPE, 1, 4>(a, s, stream) : launch_wide<TYPE, 2, 4>(a, s, stream);
     else if (c.wide && a.m > 16)
@@ -489,8 +508,7 @@ template <int TYPE> void pick(const MatvecArgs& a, bool room, hipStream_t stream
 
 extern "C" size_t w4_matvec_workspace_bytes(int32_t m, int32_t n, int32_t k) {
     if (m < 1 || n < 1 || k < 1) return 0;
-    const int splits = cut(m, n, k).splits;
-    return splits > 1 ? (size_t)splits * m * n * sizeof(float) : 0;
+    return part_bytes(cut(m, n, k), m, n);
 }
 
 extern "C" wino_status w4_matvec(const void* x, int64_t x_stride, const uint8_t* codes, const uint8_t* scales,
@@ -504,10 +522,9 @@ extern "C" wino_status w4_matvec(const void* x, int64_t x_stride, const uint8_t*
     if (m > 65535 || n > (1 << 24) || k > (1 << 20)) return WINO_EUNSUPPORTED;
     if (!aligned16(x) || !aligned16(codes) || !aligned16(workspace) || (k > 0 && m > 1 && (x_stride & 7))) return WINO_EUNSUPPORTED;
     MatvecArgs a = {x, codes, scales, bias, y, x_stride, y_stride, m, n, k, 0, (float*)workspace};
-    const bool room = workspace && workspace_bytes >= w4_matvec_workspace_bytes(m, n, k);
     if (type == WINO_BF16)
-        pick<WINO_BF16>(a, room, stream);
+        pick<WINO_BF16>(a, workspace_bytes, stream);
     else
-        pick<WINO_FP16>(a, room, stream);
+        pick<WINO_FP16>(a, workspace_bytes, stream);
     return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
 }

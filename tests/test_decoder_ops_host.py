@@ -140,3 +140,12 @@ def test_matvec_parts_count_the_rows_of_x():
                 assert W.w4_matvec_workspace_bytes(m, n, k) <= 4 << 20, (m, n, k)
     assert W.w4_matvec_workspace_bytes(64, 4096, 16384) > 0          # a few rows still are cut
     assert W.w4_matvec_workspace_bytes(128, 1024, 16384) > 0
+
+
+def test_matvec_parts_do_not_end_beside_a_size():
+    """A long k of few outputs is shared out to workgroups whatever the number of outputs: one more than a round
+    number of tiles is no reason to leave half of the device idle."""
+    _lib()
+    for m in (4, 8, 9, 12, 16, 48):
+        for n in (1024, 2560, 3584, 4000, 4095, 4096, 4097, 4128, 4160, 5003, 5120, 6000):
+            assert W.w4_matvec_workspace_bytes(m, n, 16384) > 0, (m, n)

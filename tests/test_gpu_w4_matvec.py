@@ -173,3 +173,19 @@ def test_matvec_refuses_other_tensors():
     with pytest.raises(W.WinoError) as e:
         W.w4_matvec(z(2, 68)[:, :64], c, s, y)
     assert e.value.status == -2
+
+
+@pytest.mark.parametrize("name", ["bf16", "fp16"])
+@pytest.mark.parametrize("m,n,k", [(16, 4128, 8224), (9, 5003, 6176), (4, 4097, 8192), (13, 8257, 4128), (24, 4161, 6144),
+                                   (48, 3585, 6176), (130, 1025, 4096), (200, 300, 2112)])
+def test_matvec_beside_round_sizes(m, n, k, name):
+    """One tile more than a whole round of the device, and many rows of x, in parts and whole."""
+    torch = torch_dev()
+    rng = np.random.default_rng(m + n + k)
+    codes, scales, w = _weights(rng, n, k)
+    x, xv = half(torch, rng.normal(0, 0.02, (m, k)), name)
+    cd, sd = torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda()
+    for ws in (None, torch.full((W.w4_matvec_workspace_bytes(m, n, k) + 16,), 255, dtype=torch.uint8, device="cuda")):
+        y = torch.full((m, n), float("nan"), dtype=dtype(torch, name), device="cuda")
+        W.w4_matvec(x, cd, sd, y, workspace=ws)
+        _check(host(y), xv, w, None, name)
