@@ -486,6 +486,8 @@ Cut cut(int64_t m, int64_t n, int64_t k) {
     return best;
 }
 
+bool beyond(int32_t m, int32_t n, int32_t k) { return m > 65535 || n > (1 << 24) || k > (1 << 20); }
+
 size_t part_bytes(const Cut& c, int64_t m, int64_t n) { return c.splits > 1 ? (size_t)(c.splits * m * n) * sizeof(float) : 0; }
 
 template <int TYPE> void pick(const MatvecArgs& a, size_t bytes, hipStream_t stream) {
@@ -507,7 +509,7 @@ template <int TYPE> void pick(const MatvecArgs& a, size_t bytes, hipStream_t str
 }  // namespace
 
 extern "C" size_t w4_matvec_workspace_bytes(int32_t m, int32_t n, int32_t k) {
-    if (m < 1 || n < 1 || k < 1) return 0;
+    if (m < 1 || n < 1 || k < 1 || beyond(m, n, k)) return 0;
     return part_bytes(cut(m, n, k), m, n);
 }
 
@@ -519,7 +521,7 @@ extern "C" wino_status w4_matvec(const void* x, int64_t x_stride, const uint8_t*
     if (m == 0 || n == 0) return WINO_OK;
     if (!y || (k > 0 && (!x || !codes || !scales))) return WINO_EINVAL;
     if (m > 1 && (x_stride < k || y_stride < n)) return WINO_EINVAL;
-    if (m > 65535 || n > (1 << 24) || k > (1 << 20)) return WINO_EUNSUPPORTED;
+    if (beyond(m, n, k)) return WINO_EUNSUPPORTED;
     if (!aligned16(x) || !aligned16(codes) || !aligned16(workspace) || (k > 0 && m > 1 && (x_stride & 7))) return WINO_EUNSUPPORTED;
     MatvecArgs a = {x, codes, scales, bias, y, x_stride, y_stride, m, n, k, 0, (float*)workspace};
     if (type == WINO_BF16)

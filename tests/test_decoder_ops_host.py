@@ -149,3 +149,10 @@ def test_matvec_parts_do_not_end_beside_a_size():
     for m in (4, 8, 9, 12, 16, 48):
         for n in (1024, 2560, 3584, 4000, 4095, 4096, 4097, 4128, 4160, 5003, 5120, 6000):
             assert W.w4_matvec_workspace_bytes(m, n, 16384) > 0, (m, n)
+
+
+def test_matvec_sizes_that_are_refused_need_no_workspace():
+    _lib()
+    top = 2 ** 31 - 1
+    for a in ((65536, 4096, 16384), (16, (1 << 24) + 1, 4096), (16, 64, (1 << 20) + 32), (top, top, top), (1, top, 8192)):
+        assert W.w4_matvec_workspace_bytes(*a) == 0, a
