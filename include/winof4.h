@@ -577,7 +577,7 @@ typedef struct kv4_cache {
 typedef enum wino_rotary { WINO_ROTARY_HALVES = 0, WINO_ROTARY_PAIRS = 1 } wino_rotary;
 
 /* What k_out and v_out receive: the turned keys and the values as they came,
- * or what the cache now holds for them. */
+ * or what the cache now holds for them, rounded to the type of the call. */
 typedef enum kv4_values { KV4_ROTATED = 0, KV4_CACHED = 1 } kv4_values;
 
 /*
@@ -595,8 +595,11 @@ typedef enum kv4_values { KV4_ROTATED = 0, KV4_CACHED = 1 } kv4_values;
  *               Two tokens of a call must not share a slot.
  *   q_out       [tokens][heads][head_dim], dense (NULL with heads 0)
  *   k_out, v_out  [tokens][kv_heads][head_dim], dense, or NULL; see kv4_values.
- *               A prompt whose attention reads KV4_CACHED values sees exactly
- *               what later tokens will see.
+ *               A prompt whose attention reads KV4_CACHED values in bf16 sees
+ *               exactly what later tokens will see.  fp16 rounds them: a key
+ *               of 60000 is cached as 65536, which kv4_attention reads and
+ *               fp16 has as infinity, and values under scales below 2^-23
+ *               lose bits.
  * Rotation: (u, w) -> (u c - w s, w c + u s), every product and sum rounded
  * once to fp32; keys and values are quantized from there, so equal inputs
  * always give equal codes.  head_dim a multiple of 32, at most 256.

@@ -212,3 +212,25 @@ def test_append_no_tokens_with_queries():
     W.kv4_append(z(0, 4, 64), z(0, 2, 64), z(0, 2, 64), z(9, 64, dt=torch.float32), z(0, dt=torch.int32),
                  z(0, dt=torch.int64), cache, z(0, 4, 64), z(0, 2, 64), z(0, 2, 64))
     assert all(bool((c == 0xA5).all()) for c in cache)
+
+
+def test_append_cached_values_that_fp16_rounds():
+    """The cache holds 65536 for keys of 60000 and exact values under small scales; k_out has them rounded to fp16,
+    infinity for the former."""
+    torch = torch_dev()
+    d, tokens = 64, 2
+    cs = np.concatenate((np.full((1, 16), 2.0 ** -5), np.zeros((1, 16))), -1).astype(np.float32)     # "cosines" that scale
+    k = np.zeros((tokens, 1, d), np.float32)
+    k[0, 0, :], k[0, 0, 40] = 60000.0, -65504.0
+    k[1, 0, :32] = 2.0 ** -24 * (1 + np.arange(32) % 3)
+    kt, kv = half(torch, k, "fp16")
+    cache, out = _cache(torch, 1, 1, 16, d, 0), torch.zeros_like(kt)
+    i = lambda t: torch.zeros(tokens, dtype=t, device="cuda")  # noqa: E731
+    W.kv4_append(None, kt, kt, torch.from_numpy(cs).cuda(), i(torch.int32), torch.arange(tokens, device="cuda"), cache,
+                 k_out=out, values=W.KV4_CACHED)
+    held = decoder.decode(cache[0].cpu().numpy()[0, 0, :tokens], cache[1].cpu().numpy()[0, 0, :tokens])
+    assert (held[0, 32:] == np.where(np.arange(32, 64) == 40, -65536.0, 65536.0)).all()
+    assert np.isinf(host(out)[0, 0, 32:]).all()
+    assert (held[1, :32] == kv[1, 0, :32] * 2.0 ** -5).all() and (held[1, :32] > 0).all()
+    assert (host(out)[:, 0] == torch.from_numpy(held).to(torch.float16).double().numpy()).all()
+    assert (host(out)[1, 0, :32] == 0).all()
