@@ -626,8 +626,9 @@ wino_status kv4_append(const void* q, int64_t q_stride, const void* k, int64_t k
  * cache.  head_dim 64, 96, 128, 192 or 256; scale finite, and so is its product
  * with log2(e) in fp32 (WINO_EUNSUPPORTED otherwise).
  *   workspace    kv4_attention_workspace_bytes() bytes or more, 16-byte
- *                aligned, scratch: long sequences are split over it.  NULL or
- *                a smaller one splits less.
+ *                aligned, scratch: long sequences are split over it.  With
+ *                NULL or a smaller one they are not split: the same result up
+ *                to the order of the sums, more slowly.
  */
 size_t kv4_attention_workspace_bytes(int32_t batch, int32_t q_len, int32_t heads, int32_t kv_heads,
                                      int32_t head_dim, int32_t max_pages, int32_t page_size);
