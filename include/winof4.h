@@ -648,7 +648,7 @@ wino_status kv4_attention(const void* q, int64_t q_stride, const kv4_cache* cach
  *              Offsets do not decrease; what lies past total_q or total_k is
  *              left out.  A row of out that no sequence covers is not written.
  *   max_q      the longest sequence's queries, a hint for the tile size: any
- *              value gives a right result
+ *              value from 0 on gives a right result
  *   causal     1: the last query sees every key, the one before it one less,
  *              and so on (a prompt behind a prefix has more keys than
  *              queries); 0: all keys.
