@@ -522,7 +522,11 @@ wino_status wino_f4_conv_float(const int8_t* x, const float* w_oihw, float* y, i
  * kv4_attention that see them infinite or NaN.
  * Activations are bf16 or fp16 (wino_float_type, one type for a call); every
  * sum, maximum and softmax statistic is held in fp32 and each result is
- * rounded to the 16-bit type once.
+ * rounded to the 16-bit type once.  Attention rounds its probabilities too,
+ * for the matrix cores: prompt_attention to the 16-bit type (and divides by
+ * the sum of the rounded ones; against 64 bits its error is a fifth to a
+ * quarter above that of fp32 probabilities), kv4_attention to two bf16
+ * numbers, 16 bits.
  *
  * Tensors are row-major device memory; a stride is the distance between two
  * rows (tokens) in elements, and a row itself is dense.  Base addresses of
