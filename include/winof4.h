@@ -518,8 +518,8 @@ wino_status wino_f4_conv_float(const int8_t* x, const float* w_oihw, float* y, i
  *   - two codes a byte, the lower index in the low half.
  * Kernels read weights and cache as 16-bit numbers.  Values past their range,
  * which only the scale bytes 253 and 254 reach (2^126 and 2^127), count as
- * infinite there; cached values under such a scale make the rows of
- * kv4_attention that see them infinite or NaN.
+ * infinite there; cached values under such a scale can make the rows of
+ * kv4_attention that see them infinite or NaN, small codes among them.
  * Activations are bf16 or fp16 (wino_float_type, one type for a call); every
  * sum, maximum and softmax statistic is held in fp32 and each result is
  * rounded to the 16-bit type once.  Attention rounds its probabilities too,
