@@ -555,7 +555,7 @@ wino_status w4_quantize_weights(const float* w, int32_t n, int32_t k, uint8_t* c
  *   codes    uint8 [n][k/2], scales uint8 [n][k/32], dense.
  *   bias     [n] in the type of x, or NULL.
  *   m <= 65535 (made for m up to 64: more rows read the weights again for
- *   every 64; where k is up to 1264 and n up to 4096, or k below 128, for
+ *   every 64; where k is up to 1248 and n up to 4096, or k below 128, for
  *   every 16), n <= 2^24, k a multiple of 32 up to 2^20.
  *   workspace  w4_matvec_workspace_bytes(m, n, k) bytes or more, 16-byte
  *            aligned, scratch; NULL or a smaller one gives the same result
