@@ -189,3 +189,38 @@ def test_matvec_beside_round_sizes(m, n, k, name):
         y = torch.full((m, n), float("nan"), dtype=dtype(torch, name), device="cuda")
         W.w4_matvec(x, cd, sd, y, workspace=ws)
         _check(host(y), xv, w, None, name)
+
+
+@pytest.mark.parametrize("m", [2, 20, 40])
+def test_matvec_largest_scales(m):
+    """Every code under the scales 2^126 and 2^127 in bf16: its value where bf16 holds it, infinite from 2^128 on (NaN
+    times an x of zero); and the largest scale at which fp16 holds all codes, 2^13, exactly."""
+    torch = torch_dev()
+    k = 160
+    codes, scales = np.zeros((32, k // 2), np.uint8), np.full((32, k // 32), 127, np.uint8)
+    codes[:, 50] = np.tile(np.arange(16), 2) << 4                        # index 101
+    scales[:16, 3], scales[16:, 3] = 253, 254
+    with np.errstate(over="ignore"):
+        w = decoder.decode(codes, scales)
+    past = np.abs(w[:, 101]) >= 2.0 ** 128
+    assert past.sum() == 2 * 2 + 2 * 4
+    x = np.zeros((m, k))
+    x[0, 101], x[m - 1, 101], x[:, 7] = 2.0 ** -100, -2.0 ** -100, 1.0
+    xt, xv = half(torch, x, "bf16")
+    y = torch.zeros((m, 32), dtype=torch.bfloat16, device="cuda")
+    W.w4_matvec(xt, torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), y)
+    got = host(y)
+    assert (got[:, ~past] == (xv @ w.T)[:, ~past]).all()
+    for row, sign in ((0, 1), (m - 1, -1)):
+        assert (got[row, past] == sign * np.sign(w[past, 101]) * np.inf).all()
+    assert np.isnan(got[1:m - 1][:, past]).all()
+
+    rng = np.random.default_rng(m)
+    codes = rng.integers(0, 256, (40, k // 2), dtype=np.uint8)
+    scales = np.full((40, k // 32), 140, np.uint8)
+    xt, xv = half(torch, rng.normal(0, 2.0 ** -10, (m, k)), "fp16")
+    y = torch.zeros((m, 40), dtype=torch.float16, device="cuda")
+    W.w4_matvec(xt, torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), y)
+    w = decoder.decode(codes, scales)
+    assert (np.abs(xv) @ np.abs(w).T).max() < 0.9 * TOP["fp16"]          # no result is past fp16
+    _check(host(y), xv, w, None, "fp16")
