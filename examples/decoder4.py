@@ -44,6 +44,7 @@ class Decoder:
         self.caches = [tuple(torch.zeros((sequences * per, kv_heads, page, w), dtype=torch.uint8, device="cuda")
                              for w in widths) for _ in range(layers)]
         self.lens = torch.zeros(sequences, dtype=torch.int32, device="cuda")
+        self.capacity, self.longest = per * page, 0         # tokens of a sequence: the table's, and held by the longest
         angle = np.arange(per * page)[:, None] * 10000.0 ** (-np.arange(0, head_dim, 2) / head_dim)
         self.cos_sin = torch.from_numpy(np.concatenate((np.cos(angle), np.sin(angle)), -1).astype(np.float32)).cuda()
 
@@ -81,10 +82,19 @@ class Decoder:
             x = x + self._product(torch.nn.functional.silu(gate) * up, weights["down"])
         return self._product(self._norm(x), self.head)
 
+    def _room(self, longest):
+        """Refuses what the table has no pages for: an index past it would be one past its memory."""
+        if longest > self.capacity:
+            raise ValueError(f"{longest} tokens in a sequence, the cache holds {self.capacity}")
+        self.longest = longest
+
     def prompt(self, prompts):
         """Fills the cache with the prompts (lists of tokens, one a sequence) and
         returns the logits of all their tokens [total, vocab]."""
         counts = [len(p) for p in prompts]
+        if len(counts) != len(self.lens):
+            raise ValueError(f"{len(counts)} prompts for {len(self.lens)} sequences")
+        self._room(max(counts))
         tokens = torch.tensor([t for p in prompts for t in p], dtype=torch.int64, device="cuda")
         at = torch.tensor([i for n in counts for i in range(n)], dtype=torch.int64, device="cuda")
         seq = torch.repeat_interleave(torch.arange(len(counts)), torch.tensor(counts)).cuda()
@@ -98,6 +108,7 @@ class Decoder:
 
     def step(self, tokens):
         """Appends one token to each sequence; returns their logits [sequences, vocab]."""
+        self._room(self.longest + 1)
         at = self.lens.long()
         slots = self.table.gather(1, (at // self.page)[:, None])[:, 0].long() * self.page + at % self.page
         positions = self.lens.clone()
@@ -109,18 +120,21 @@ class Decoder:
 
     def capture(self):
         """step() as a HIP graph: returns a function with the same arguments."""
-        tokens, held = torch.zeros_like(self.lens, dtype=torch.int64), self.lens.clone()
+        tokens, held, longest = torch.zeros_like(self.lens, dtype=torch.int64), self.lens.clone(), self.longest
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):                       # once outside of the graph: what is laid out at the first use
             self.step(tokens)
         torch.cuda.current_stream().wait_stream(side)
         self.lens.copy_(held)                               # the token written there is overwritten by the next one
+        self.longest = longest
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
             logits = self.step(tokens)
+        self.longest = longest                              # nothing has run: a replay counts its token
 
         def replay(new):
+            self._room(self.longest + 1)
             tokens.copy_(new)
             graph.replay()
             return logits

@@ -64,3 +64,25 @@ def test_the_captured_step_is_the_eager_one():
         assert (x == y).all(), f"step {i}"
         new = x.argmax(-1)
     assert eager.lens.tolist() == graph.lens.tolist() == [n + 30 for n in lens]
+
+
+def test_tokens_past_the_capacity_are_refused():
+    """On the host, before anything is launched: eagerly, captured, and for prompts."""
+    torch = torch_dev()
+    make = _example().Decoder
+    model = make(2, 48, vocab=512, page=16)
+    with pytest.raises(ValueError, match="holds 48"):
+        model.prompt([[1] * 49, [1]])
+    with pytest.raises(ValueError, match="2 sequences"):
+        model.prompt([[1]])
+    model.prompt([[1, 2, 3] * 15, [4]])
+    new = torch.tensor([3, 4], device="cuda")
+    model.step(new)
+    replay = model.capture()
+    for _ in range(2):
+        assert bool(torch.isfinite(replay(new)).all())
+    assert model.lens.tolist() == [48, 4]
+    for call in (model.step, replay):
+        with pytest.raises(ValueError, match="49 tokens"):
+            call(new)
+    assert model.lens.tolist() == [48, 4]
