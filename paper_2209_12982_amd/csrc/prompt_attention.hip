@@ -455,7 +455,8 @@ __global__ __launch_bounds__((64 * Shape<DIM, ROWS, TEAMS, KEYS>::kWaves), 2) vo
     }
     if (team == 0) {
         // the halves of the wave exchange four dimensions of sixteen, so that a lane stores eight neighbours
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        // a row that sees keys has a sum, or scores that are all minus infinity and is not a number (0 times infinity)
+        const float inv = 1.f / sum;
         T* out = (T*)a.out + ((int64_t)(w.q0 + i) * a.heads + h) * DIM + d0 + 8 * half;
 #pragma unroll
         for (int n = 0; n < S::kOut; ++n)
@@ -465,7 +466,7 @@ __global__ __launch_bounds__((64 * Shape<DIM, ROWS, TEAMS, KEYS>::kWaves), 2) vo
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const T2 x = {(T)(o[n][e + 2 * k] * inv), (T)(o[n][e + 2 * k + 1] * inv)};
-                    y[k] = sum == 0.f ? 0u : __builtin_bit_cast(uint32_t, x);
+                    y[k] = row_end == 0 ? 0u : __builtin_bit_cast(uint32_t, x);
                 }
                 const auto s02 = __builtin_amdgcn_permlane32_swap(y[0], y[2], false, false);
                 const auto s13 = __builtin_amdgcn_permlane32_swap(y[1], y[3], false, false);

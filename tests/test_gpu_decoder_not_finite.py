@@ -5,9 +5,12 @@ are those of the operators' own tests)."""
 import numpy as np
 import pytest
 
-from decoder_util import host
+import paper_2209_12982_amd as W
+from decoder_util import half, host
 from gpu_util import torch_dev
 from test_gpu_kv4_attention import _call, _hold, _reference, _setup, _workspace
+from test_gpu_prompt_attention import _cu
+from test_gpu_prompt_attention import _reference as prompt_reference
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +56,37 @@ def test_split_decode_keeps_keys_that_are_not_numbers(length, begins, name):
             got = host(_call(torch, q, cache, table, lens, d ** -0.5, w))
             assert np.isnan(got[0]).all(), f"keys from {begin} on"
             _hold(got[1], ref[1], bound[1])
+
+
+@pytest.mark.parametrize("name", ["bf16", "fp16"])
+@pytest.mark.parametrize("lens,hq,hkv,d", [([5, 40], 4, 2, 64), ([3, 70], 2, 1, 96), ([200, 90], 3, 1, 128), ([700], 16, 16, 256),
+                                           ([1100, 3], 12, 12, 192)])
+def test_prompt_scores_that_are_all_minus_infinity(lens, hq, hkv, d, name):
+    """A row that sees keys, each of them infinitely far away, is not a number: its softmax is infinity less itself.
+    A row that sees no key is zeros, whatever its query."""
+    torch = torch_dev()
+    rng = np.random.default_rng(d)
+    k_lens = [n - 2 for n in lens]                                       # the first two rows of a sequence see nothing
+    qn, kn = sum(lens), sum(k_lens)
+    q, qv = half(torch, rng.normal(0, 1, (qn, hq, d)), name)
+    k, kv = half(torch, rng.normal(0, 1, (kn, hkv, d)), name)
+    v, vv = half(torch, rng.normal(0, 1, (kn, hkv, d)), name)
+    k[:, :, 7] = -k[:, :, 7].abs() - 0.5
+    kv = host(k)
+    rows = [0, 1, 2, lens[0] - 1, qn - 1]
+    ref, bound = prompt_reference(qv, kv, vv, lens, k_lens, d ** -0.5, True, name) if qn < 300 else (None, None)
+    for r in rows:
+        q[r, hq - 1, 7] = float("inf")
+    out = torch.full_like(q, 3.0)
+    W.prompt_attention(q, k, v, _cu(torch, lens), _cu(torch, k_lens), max(lens), out, d ** -0.5)
+    got = host(out)
+    hit = np.zeros((qn, hq), bool)
+    hit[rows, hq - 1] = True
+    blind = np.zeros((qn, hq), bool)
+    for b in np.cumsum([0] + lens[:-1]):
+        blind[b:b + 2] = True
+    assert (got[blind] == 0).all()
+    assert np.isnan(got[hit & ~blind]).all()
+    assert np.isfinite(got[~hit]).all()
+    if ref is not None:
+        _hold(got[~hit], ref[~hit], bound[~hit])
