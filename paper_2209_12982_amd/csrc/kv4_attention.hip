@@ -221,8 +221,11 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
     const bool real = i < a.q_len;
     const int row_end = real ? (first_end + i < len ? first_end + i : len) : 0;
 
+    // An infinite element makes all scores infinite, of one sign or another: not a number where any is seen.  It becomes a
+    // NaN here (0 times it; the second part in fp16 is one), because scores that are all minus infinity would look like none.
     bf16x8 q[kParts][S::kSteps];
     {
+        float none = 0.f;
         const T* p = (const T*)a.q + ((int64_t)b * a.q_len + (real ? i : 0)) * a.q_stride + (int64_t)(real ? h : 0) * DIM +
                      g * (DIM / 4);
 #pragma unroll
@@ -230,6 +233,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
             const T8 x = __builtin_bit_cast(T8, (*(const u32x4*)(p + 8 * j) & a.q_and) ^ a.q_xor);
             if constexpr (TYPE == WINO_BF16) {
                 q[0][j] = x;
+#pragma unroll
+                for (int e = 0; e < 8; e += 2)
+                    none = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{x[e], x[e + 1]}, bf16x2{(__bf16)0.f, (__bf16)0.f}, none, false);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -239,6 +245,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || DIM > 128 ? 2 : 3) void k
                 }
             }
         }
+        if constexpr (TYPE == WINO_BF16) q[0][0][0] = (__bf16)((float)q[0][0][0] + none);
     }
 
     f32x4 o[DIM / 16];                                      // lane: dimensions 16 n + 4 g + e of row r

@@ -90,3 +90,27 @@ def test_prompt_scores_that_are_all_minus_infinity(lens, hq, hkv, d, name):
     assert np.isfinite(got[~hit]).all()
     if ref is not None:
         _hold(got[~hit], ref[~hit], bound[~hit])
+
+
+@pytest.mark.parametrize("name", ["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 96, 128, 192, 256])
+def test_decode_scores_that_are_all_minus_infinity(d, name):
+    """An infinite query on keys that are all negative there, in sequences of one token to many parts: not a number
+    where any token is seen, zeros where none is (an empty sequence, pages that are not there)."""
+    torch = torch_dev()
+    rng = np.random.default_rng(d + 3)
+    lens, hq, hkv, page = [1, 30, 3000, 0, 40], 5, 1, 16
+    table, cache, q, qv = _setup(torch, rng, lens, 1, hq, hkv, d, page, name)
+    cache[0][..., 3] |= 0xB0                                      # dimension 7: -3 to -6
+    table[4, :3] = -1
+    hidden = {(4, t) for t in range(40)}
+    ref, bound = _reference(cache, table, lens, qv, 1, hq, hkv, d, page, d ** -0.5, name, hidden)
+    hit = np.zeros((5, hq), bool)
+    hit[:, 2] = hit[2, 4] = True
+    q[torch.from_numpy(hit).cuda(), 7] = float("inf")
+    ws = _workspace(torch, lens, 1, hq, hkv, d, table, page)
+    assert ws.numel() > 16
+    for w in (None, ws):
+        got = host(_call(torch, q, cache, table, lens, d ** -0.5, w))
+        assert np.isnan(got[:3][hit[:3]]).all() and (got[3:] == 0).all()
+        _hold(got[~hit], ref[~hit], bound[~hit])
