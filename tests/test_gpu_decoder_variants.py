@@ -288,3 +288,21 @@ def test_what_is_no_tensor_is_refused():
                                           z(4, dt=torch.int64), cache)):
             with pytest.raises((ValueError, TypeError)):
                 call()
+
+
+@pytest.mark.parametrize("d,hq,hkv,seqs", [(64, 2, 1, 65), (128, 16, 8, 130), (256, 4, 4, 200), (64, 1, 1, 1000)])
+def test_prompt_more_sequences_than_a_wave(d, hq, hkv, seqs):
+    """Sequences are ranked 64 at a time: several such groups, with empty sequences and ones without keys in each."""
+    torch = torch_dev()
+    rng = np.random.default_rng(seqs)
+    q_lens = [int(x) for x in rng.integers(0, 5, seqs)]
+    k_lens = [max(0, n + int(x)) for n, x in zip(q_lens, rng.integers(-3, 20, seqs))]
+    q_lens[63], k_lens[63], q_lens[64], k_lens[64], q_lens[-1], k_lens[-1] = 140, 150, 0, 9, 3, 80
+    q, qv = half(torch, rng.normal(0, 1, (sum(q_lens), hq, d)), "bf16")
+    k, kv = half(torch, rng.normal(0, 1.5, (sum(k_lens), hkv, d)), "bf16")
+    v, vv = half(torch, rng.normal(0, 1, (sum(k_lens), hkv, d)), "bf16")
+    ref, bound = prompt_reference(qv, kv, vv, q_lens, k_lens, d ** -0.5, True, "bf16")
+    for hint in (140, 100000):
+        out = torch.full(q.shape, float("nan"), dtype=q.dtype, device="cuda")
+        W.prompt_attention(q, k, v, _cu(torch, q_lens), _cu(torch, k_lens), hint, out, d ** -0.5)
+        _hold(host(out), ref, bound)
