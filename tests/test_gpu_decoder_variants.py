@@ -306,3 +306,51 @@ def test_prompt_more_sequences_than_a_wave(d, hq, hkv, seqs):
         out = torch.full(q.shape, float("nan"), dtype=q.dtype, device="cuda")
         W.prompt_attention(q, k, v, _cu(torch, q_lens), _cu(torch, k_lens), hint, out, d ** -0.5)
         _hold(host(out), ref, bound)
+
+
+@pytest.mark.parametrize("seqs,hq,hkv,offset", [(5000, 1, 1, 0), (130, 6, 2, 40), (64, 6, 2, 40), (8300, 2, 1, 3)])
+def test_prompt_sets_of_sequences_are_found(seqs, hq, hkv, offset):
+    """Thousands of sequences, of no tokens to 300, rows before the first one and offsets past the last row."""
+    torch = torch_dev()
+    rng = np.random.default_rng(seqs)
+    d = 64
+    lens = rng.integers(0, 3, seqs)
+    lens[[0, seqs // 2, seqs - 1]] = 3, 300, 70
+    cu = (offset + np.concatenate([[0], np.cumsum(lens)])).astype(np.int32)
+    n = int(cu[-1]) - (20 if offset else 0)                       # the last sequence is cut off
+    cut = np.minimum(cu, n)
+    q, qv = half(torch, rng.normal(0, 1, (n, hq, d)), "bf16")
+    k, kv = half(torch, rng.normal(0, 1, (n, hkv, d)), "bf16")
+    v, vv = half(torch, rng.normal(0, 1, (n, hkv, d)), "bf16")
+    got_lens = [int(x) for x in np.diff(cut)]
+    ref, bound = prompt_reference(qv[offset:], kv[offset:], vv[offset:], got_lens, got_lens, 0.1, True, "bf16")
+    t = torch.from_numpy(cu).cuda()
+    for hint in (300, 3, 1 << 20):
+        out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+        W.prompt_attention(q, k, v, t, t, hint, out, 0.1)
+        _hold(host(out)[offset:], ref, bound)
+        assert (out[:offset] == 7).all()
+
+
+def test_prompt_work_grows_with_the_sequences_not_their_square():
+    """Sixteen times as many sequences take about sixteen times as long; looking at all of them in each workgroup took
+    a hundred and thirty times as long."""
+    torch = torch_dev()
+
+    def time(seqs):
+        q = torch.zeros((4 * seqs, 16, 128), dtype=torch.bfloat16, device="cuda")
+        k, out = q[:, :4], torch.empty_like(q)
+        cu = (4 * torch.arange(seqs + 1, device="cuda")).to(torch.int32)
+        took = []
+        for _ in range(6):
+            begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            begin.record()
+            for _ in range(4):
+                W.prompt_attention(q, k, k, cu, cu, 4, out, 0.1)
+            end.record()
+            torch.cuda.synchronize()
+            took.append(begin.elapsed_time(end))
+        return min(took)
+
+    few, many = time(256), time(4096)
+    assert many < 50 * few, (few, many)
