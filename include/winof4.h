@@ -526,7 +526,8 @@ wino_status wino_f4_conv_float(const int8_t* x, const float* w_oihw, float* y, i
  * for the matrix cores: prompt_attention to the 16-bit type (and divides by
  * the sum of the rounded ones; against 64 bits its error is a fifth to a
  * quarter above that of fp32 probabilities), kv4_attention to two bf16
- * numbers, 16 bits.
+ * numbers, 16 bits.  Rows of attention that see nothing are zeros; rows whose
+ * scores are all minus infinity, or any of them NaN or plus infinity, are NaN.
  *
  * Tensors are row-major device memory; a stride is the distance between two
  * rows (tokens) in elements, and a row itself is dense.  Base addresses of

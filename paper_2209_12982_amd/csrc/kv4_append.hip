@@ -36,8 +36,9 @@ struct AppendArgs {
 // wave.  With halves rotated it reads the 8 partners too (from the cache:
 // another thread reads them as its own), which needs neither LDS nor a barrier.
 // Its indices are 32 bits wide, divided by multiplying: with 64-bit divisions it
-// took 50.0 us for 8200 tokens of 32 + 2 x 8 heads of 128, now 46.2, 4.6 TB/s
-// (a large copy: 4.9).
+// took 50.0 us for 8200 tokens of 32 + 2 x 8 heads of 128, now 46.6, 4.6 TB/s
+// (a copy of 2 GiB: 4.8); the first hundred calls of a burst, before the clock
+// settles, take 53.
 // LARGE: outputs that no L2 holds until somebody reads them do not go through it, 2.6 us of those 50.
 template <int TYPE, int ROTARY, bool LARGE>
 __global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {

@@ -18,10 +18,13 @@
 // numbers (16 bits), the matrix cores have time for both; the products are
 // then exact in fp32.
 //
-// 32 heads of 128 on 8: two sequences of 131072 tokens, 157 MB of cache, take
-// 39.7 us, 35 of them this kernel (4.5 TB/s, of 4.9 that a large copy reaches);
-// 64 sequences of 1 to 4096 tokens, 81 MB, 23 us (3.5 TB/s) and 4.5 for the
-// join: their many short units cost a wait for the first codes each.
+// 32 heads of 128 on 8, bf16: two sequences of 131072 tokens, 157 MB of cache,
+// take 39.5 us, 35 of them this kernel (4.5 TB/s, of 4.8 that a copy of 2 GiB
+// reaches); 64 sequences of 1 to 4096 tokens, 81 MB, 22 us (3.7 TB/s) and 4.6 for
+// the join: their many short units cost a wait for the first codes each.  In fp16
+// the two take 50.6 us, and the 64 with the append 37.2 instead of 31.0: queries
+// take twice the registers and score products, and 14 registers are spilled under
+// the limit of three workgroups a compute unit.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -562,7 +565,9 @@ struct Cut {
 };
 
 // A call's workgroups.  Sequences are split where that spares a workgroup more than three blocks of tokens: the join
-// is a launch of its own (777 tokens of two heads: 8.0 us in one launch, 10 in two).
+// is a launch of its own (777 tokens of two heads: 8.0 us in one launch, 10 in two).  The host knows no lengths, so it
+// goes by what the table has room for: 500 tokens of 8 heads take 8.0 us with a table of their length and 10.9 with one for
+// 131072, 64 such sequences 14.4 and 15.6.
 Cut cut(int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int dim, int64_t room) {
     Cut c;
     c.tiles = (q_len * (heads / kv_heads) + 15) / 16;
