@@ -524,9 +524,8 @@ wino_status wino_f4_conv_float(const int8_t* x, const float* w_oihw, float* y, i
  * sum, maximum and softmax statistic is held in fp32 and each result is
  * rounded to the 16-bit type once.  Attention rounds its probabilities too,
  * for the matrix cores: prompt_attention to the 16-bit type (and divides by
- * the sum of the rounded ones; against 64 bits its error is a fifth to a
- * quarter above that of fp32 probabilities), kv4_attention to two bf16
- * numbers, 16 bits.  Rows of attention that see nothing are zeros; rows whose
+ * the sum of the rounded ones; against 64 bits its error is 1.1 to 1.4 times
+ * that of fp32 probabilities), kv4_attention to two bf16 numbers, 16 bits.  Rows of attention that see nothing are zeros; rows whose
  * scores are all minus infinity, or any of them NaN or plus infinity, are NaN.
  *
  * Tensors are row-major device memory; a stride is the distance between two

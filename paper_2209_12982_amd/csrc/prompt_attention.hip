@@ -18,13 +18,13 @@
 // product (fp16 ones held 2^6 higher, clear of its smallest numbers), and their
 // sum is that of the rounded ones, so that the weights of a row add up to 1.
 //
-// One sequence of 16384 tokens, 16 heads of 128 on 4: 1010 us, 1.09 PFLOP/s (a
-// large library product of the same type: 1.25 to 1.38); the matrix cores work 57%
-// of the cycles, at the clock that this load leaves (1.6 to 1.8 GHz).  Twelve
-// packed ones of up to 2048, 32 heads on 8: 143 us, 0.78 PFLOP/s, 39%: their
-// workgroups walk over eight tiles on average, and begin and end in between.  Both
-// once the clock has settled: the first hundred calls of a burst take 1035 and 167
-// us on average, and one device needed 1066 and 150.
+// One sequence of 16384 tokens, 16 heads of 128 on 4: 1010 to 1030 us on most
+// devices, 1.07 to 1.09 PFLOP/s (a large library product of the same type: 1.25 to
+// 1.38); the matrix cores work 57% of the cycles, at the clock that this load leaves
+// (1.6 to 1.8 GHz).  Twelve packed ones of up to 2048, 32 heads on 8: 143 to 150 us,
+// 0.74 to 0.78 PFLOP/s, 40%: their workgroups walk over eight tiles on average, and
+// begin and end in between.  Both once the clock has settled: the first hundred
+// calls of a burst take 1035 to 1050 and 167 us on average.
 // Heads of 256: four sequences of 4096, 16 heads on 4, 659 us, 0.84 PFLOP/s.
 #include <hip/hip_runtime.h>
 
