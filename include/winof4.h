@@ -628,7 +628,8 @@ wino_status kv4_append(const void* q, int64_t q_stride, const void* k, int64_t k
  *                softmax_t(scale q.k_t) v_t; zeros where it sees none.
  * heads is a multiple of cache->kv_heads: neighbours share a head of the
  * cache.  head_dim 64, 96, 128, 192 or 256; scale finite, and so is its product
- * with log2(e) in fp32 (WINO_EUNSUPPORTED otherwise).
+ * with log2(e) in fp32; batch times the sets of 16 rows at each cache head
+ * below 2^23 (WINO_EUNSUPPORTED otherwise).
  *   workspace    kv4_attention_workspace_bytes() bytes or more, 16-byte
  *                aligned, scratch: long sequences are split over it.  With
  *                NULL or a smaller one they are not split: the same result up

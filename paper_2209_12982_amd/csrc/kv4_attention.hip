@@ -567,14 +567,14 @@ struct Cut {
 // A call's workgroups.  Sequences are split where that spares a workgroup more than three blocks of tokens: the join
 // is a launch of its own (777 tokens of two heads: 8.0 us in one launch, 10 in two).  The host knows no lengths, so it
 // goes by what the table has room for: 500 tokens of 8 heads take 8.0 us with a table of their length and 10.9 with one for
-// 131072, 64 such sequences 14.4 and 15.6.
+// 131072, 64 such sequences 14.4 and 15.6.  A launch has less than 2^32 threads: the join's 256 a row set an end to splitting.
 Cut cut(int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int dim, int64_t room) {
     Cut c;
     c.tiles = (q_len * (heads / kv_heads) + 15) / 16;
     c.units = kv_heads * c.tiles;
     const int64_t blocks = std::max<int64_t>(1, (room + kBlock - 1) / kBlock), all = batch * c.units * blocks;
     c.groups = std::min<int64_t>(all, dim <= 128 ? kGroups : kGroups * 2 / 3);
-    c.split = blocks - (all + c.groups - 1) / c.groups > 3;
+    c.split = blocks - (all + c.groups - 1) / c.groups > 3 && batch * q_len * heads < 1 << 24;
     c.bytes = c.split ? (size_t)(2 * c.groups * 16 * (dim + 2) * 4 + batch * c.units * sizeof(Parts)) : 0;
     return c;
 }
@@ -640,8 +640,8 @@ extern "C" wino_status kv4_attention(const void* q, int64_t q_stride, const kv4_
     if (rows > 0x7fffffffll) return WINO_EUNSUPPORTED;
     const int64_t room = std::min<int64_t>((int64_t)max_pages * c.page_size, 0x7fffffff - 65536);
     const Cut k = cut(batch, q_len, heads, c.kv_heads, c.head_dim, room);
-    if (batch * k.units > 0x7fffffffll) return WINO_EUNSUPPORTED;
     const bool split = k.split && workspace && workspace_bytes >= k.bytes;
+    if (!split && batch * k.units >= 1 << 23) return WINO_EUNSUPPORTED;     // workgroups of 512 threads
     DecodeArgs a = {q, out, c.k_codes, c.k_scales, c.v_codes, c.v_scales, block_table, lens,
                     split ? (float*)workspace : nullptr, q_stride, c.pages, q_len, heads, c.kv_heads,
                     heads / c.kv_heads, c.page_size, max_pages, (int32_t)k.tiles, batch, (int32_t)k.units,

@@ -156,3 +156,15 @@ def test_matvec_sizes_that_are_refused_need_no_workspace():
     top = 2 ** 31 - 1
     for a in ((65536, 4096, 16384), (16, (1 << 24) + 1, 4096), (16, 64, (1 << 20) + 32), (top, top, top), (1, top, 8192)):
         assert W.w4_matvec_workspace_bytes(*a) == 0, a
+
+
+def test_attention_of_more_rows_than_a_launch_holds():
+    """A launch has less than 2^32 threads, 512 for each sequence and set of 16 rows: more is refused before anything
+    is launched, and rows that the join could not hold (256 threads each) are not split."""
+    lib = _lib()
+    c = W.binding._KV4Cache(k_codes=64, k_scales=64, v_codes=64, v_scales=64, pages=2, kv_heads=2, page_size=16, head_dim=64)
+    for batch, q_len, heads in ((1 << 22, 1, 2), (1 << 21, 20, 4), ((1 << 23) - 1, 1, 16)):
+        assert lib.kv4_attention(64, 64 * heads, ctypes.byref(c), 64, 2, 64, 64, batch, q_len, heads, 1.0, 0, None, 0,
+                                 None) == -2, (batch, q_len, heads)
+    assert W.kv4_attention_workspace_bytes(2, 1, 32, 8, 128, 2048, 64) > 0
+    assert W.kv4_attention_workspace_bytes(1 << 17, 1, 128, 8, 128, 2048, 64) == 0
