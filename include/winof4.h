@@ -660,7 +660,9 @@ wino_status kv4_attention(const void* q, int64_t q_stride, const kv4_cache* cach
  *   out        [total_q][heads][head_dim], dense; zeros where a query sees
  *              no key.
  * Sizes of heads and scale as for kv4_attention; total_q times the heads of a
- * group below 2^31.
+ * group below 2^31; at most 65536 sequences.  A launch holds the workgroups of
+ * (total_q * heads / kv_heads / 64 + seqs) * kv_heads < 2^23 in any case
+ * (WINO_EUNSUPPORTED where it does not).
  */
 wino_status prompt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                              int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k, int32_t seqs,

@@ -500,9 +500,10 @@ int64_t tiles(const PromptArgs& a, int rows) { return ((int64_t)a.total_q * a.gr
 
 template <int TYPE, int DIM, int ROWS, int TEAMS, int KEYS> wino_status launch(const PromptArgs& a, hipStream_t stream) {
     const int64_t blocks = tiles(a, ROWS);
-    if (blocks > 0x7fffffffll) return WINO_EUNSUPPORTED;
-    hipLaunchKernelGGL((prompt_attention_kernel<TYPE, DIM, ROWS, TEAMS, KEYS>), dim3((unsigned)blocks),
-                       dim3(64 * Shape<DIM, ROWS, TEAMS, KEYS>::kWaves), 0, stream, a);
+    constexpr int kThreads = 64 * Shape<DIM, ROWS, TEAMS, KEYS>::kWaves;
+    if (blocks * kThreads > 0xffffffffll) return WINO_EUNSUPPORTED;         // of a launch
+    hipLaunchKernelGGL((prompt_attention_kernel<TYPE, DIM, ROWS, TEAMS, KEYS>), dim3((unsigned)blocks), dim3(kThreads), 0,
+                       stream, a);
     return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
 }
 // Tiles of 128 rows by one team once they fill the device twice over (more than once for wide heads, whose workgroups

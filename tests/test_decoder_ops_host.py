@@ -168,3 +168,10 @@ def test_attention_of_more_rows_than_a_launch_holds():
                                  None) == -2, (batch, q_len, heads)
     assert W.kv4_attention_workspace_bytes(2, 1, 32, 8, 128, 2048, 64) > 0
     assert W.kv4_attention_workspace_bytes(1 << 17, 1, 128, 8, 128, 2048, 64) == 0
+
+
+def test_prompt_of_more_sequences_than_a_launch_holds():
+    lib = _lib()
+    for d, heads, kv_heads in ((64, 256, 256), (256, 128, 128), (192, 1024, 256)):
+        assert lib.prompt_attention(64, heads * d, 64, kv_heads * d, 64, kv_heads * d, 64, 64, 65536, 64, 64, 1, heads,
+                                    kv_heads, d, 1.0, 1, 64, 0, None) == -2, (d, heads)
