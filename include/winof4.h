@@ -537,7 +537,7 @@ wino_status wino_f4_conv_float(const int8_t* x, const float* w_oihw, float* y, i
  * and page numbers are device data that the host does not see: the kernels
  * check them, and what lies outside its range is left out as each call says.
  */
-typedef enum wino_float_type { WINO_BF16 = 0, WINO_FP16 = 1 } wino_float_type;
+typedef enum wino_float_type { WINO_BF16 = 0, WINO_FP16 = 1, WINO_FP32 = 2 } wino_float_type;   /* WINO_FP32: route_experts alone */
 
 /*
  * w4_quantize_weights -- fp32 weights to the 4-bit format, exact host
@@ -669,6 +669,117 @@ wino_status prompt_attention(const void* q, int64_t q_stride, const void* k, int
                              int32_t total_q, int32_t total_k, int32_t max_q, int32_t heads, int32_t kv_heads,
                              int32_t head_dim, float scale, int32_t causal, void* out, wino_float_type type,
                              hipStream_t stream);
+
+/*
+ * ---- Decoder operators in 8 bits ------------------------------------------
+ *
+ * What a decoder runs for many rows at once, prompts among them, and for
+ * layers of experts.  Operands are signed 8-bit codes with an fp32 scale for
+ * each row: of activations a token's, of weights an output's.  A sum of
+ * products of codes is exact in int32, so it has one value, however it is cut
+ * and whatever workspace there is.  It becomes a result in fp32: (float)sum,
+ * times x_scale, and times w_scale plus bias, each of the three rounded once;
+ * the result is rounded to the 16-bit type once.  Tensors, strides (multiples of 16
+ * codes), alignment, streams and graphs as for the operators in 4 bits.
+ */
+
+/*
+ * w8_quantize -- rows of 16-bit numbers to codes and scales: a = max|x| of the
+ * row, scale = a / 127 in fp32, code = R(127 x / a) of the exact quotient, R
+ * the library's rounding (halves up).  A row of zeros has scale 0; one that
+ * holds an infinity or a NaN has a NaN for its scale and codes 0, so that all
+ * its products are NaN.  Weights are quantized by the same call, a row an
+ * output.
+ *   x        [m][k], row stride x_stride >= k;  codes: int8 [m][k], dense;
+ *   scales   fp32 [m].  k a multiple of 16.
+ */
+wino_status w8_quantize(const void* x, int64_t x_stride, int8_t* codes, float* scales, int32_t m, int32_t k,
+                        wino_float_type type, hipStream_t stream);
+
+/*
+ * w8_matmul -- y[i][j] = (sum_k x[i][k] w[j][k]) x_scales[i] w_scales[j] + bias[j].
+ *   x         int8 [m][k], row stride x_stride >= k;  x_scales: fp32 [m]
+ *   w         int8 [n][k], dense;  w_scales: fp32 [n]
+ *   bias      [n] in the type of y, or NULL
+ *   y         [m][n], row stride y_stride >= n (any alignment)
+ *   m <= 2^20, n <= 2^24, (m / 128)(n / 128), both rounded up, below 2^23, k a
+ *   multiple of 16 below 2^17 (no sum of products of codes from -128 on
+ *   passes int32 there).
+ *   workspace w8_matmul_workspace_bytes(m, n, k) bytes or more, 16-byte
+ *             aligned, scratch; NULL or a smaller one gives the same result,
+ *             more slowly.
+ */
+size_t w8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k);
+wino_status w8_matmul(const int8_t* x, int64_t x_stride, const float* x_scales, const int8_t* w, const float* w_scales,
+                      const void* bias, void* y, int64_t y_stride, int32_t m, int32_t n, int32_t k, wino_float_type type,
+                      void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* How route_experts turns logits into scores. */
+typedef enum wino_score { WINO_SCORE_SOFTMAX = 0, WINO_SCORE_SIGMOID = 1 } wino_score;
+
+/*
+ * route_experts -- which experts a token goes to, with what weights, and the
+ * routes (token * top + rank) in the order of their experts.
+ *   s = softmax(logits) or sigmoid(logits) over a token's experts, c = s + bias;
+ *   the value of a group (experts / groups neighbours) is the sum of its
+ *   group_best (1 or 2) largest c, and the top_groups groups of the largest
+ *   values stay; chosen are the `top` largest c of their experts, the largest
+ *   first.  Ties go to the lower index; a c or a value of a group that is not
+ *   a number counts as minus infinity.  weight = s, divided by the sum of the
+ *   chosen s with `normalise` (0 where that is 0), times scale.  A NaN among
+ *   the s that a weight is made of makes it NaN; the choice is valid all the same.
+ * Everything up to the weights is held in 64 bits, because a choice hangs on
+ * the difference of two values.
+ *   logits   [tokens][experts] bf16, fp16 or fp32, row stride `stride`, any
+ *            alignment of whole numbers
+ *   bias     fp32 [experts] or NULL
+ *   live     int32 [1] or NULL: the tokens from *live on are padding, which
+ *            has no routes: chosen -1, weights 0
+ *   chosen   int32 [tokens][top];  weights: fp32 [tokens][top]
+ *   order    int32 [tokens * top] or NULL: the routes by expert, those of an
+ *            expert in ascending order; what lies behind the last is not written
+ *   ends     int32 [experts + 1] (with order): expert e has order[ends[e]] to
+ *            order[ends[e + 1] - 1]
+ *   experts <= 1024 (a multiple of groups), groups <= 64, top <= 32 and at most
+ *   the experts of top_groups groups, tokens * top <= 2^22.
+ *   workspace  route_experts_workspace_bytes(tokens, experts, top) bytes or
+ *            more, 16-byte aligned, scratch: needed with order.
+ */
+size_t route_experts_workspace_bytes(int32_t tokens, int32_t experts, int32_t top);
+wino_status route_experts(const void* logits, int64_t stride, const float* bias, int32_t tokens, int32_t experts, int32_t top,
+                          wino_score score, int32_t groups, int32_t top_groups, int32_t group_best, int32_t normalise,
+                          float scale, const int32_t* live, int32_t* chosen, float* weights, int32_t* order, int32_t* ends,
+                          wino_float_type type, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * w8_experts_matmul -- the products of routes with their experts' weights: route
+ * r of expert e has p[r][j] = (sum_k x[r / share][k] w[e][j][k]) x_scales[r / share]
+ * w_scales[e][j], share = routes / x_rows.  x has a row for each token (share
+ * is then the experts of a token) or for each route (share 1).
+ *   x         int8 [x_rows][k], row stride x_stride >= k;  x_scales fp32 [x_rows]
+ *   w         int8 [experts][n][k], dense;  w_scales fp32 [experts][n]
+ *   order, ends  as route_experts gives them.  Ends are cut to 0 .. routes and
+ *             routes that are not in 0 .. routes - 1 are left out; a route must
+ *             not appear twice.
+ *   y         without weights: [routes][n], y[r] = p[r]; a row whose route is
+ *             not in the order is left as it was.
+ *             With weights: [routes / top][n], y[t] = sum_j weights[t][j]
+ *             p[t * top + j] in fp32, in the order of j, over the j whose
+ *             chosen[t][j] is an expert; zeros where none is.  The order has to
+ *             hold exactly those routes.
+ *   weights   fp32 [routes / top][top] or NULL;  chosen: int32, the same (with weights)
+ *   routes <= 2^22, experts <= 1024, n <= 2^20, k a multiple of 16 below 2^17;
+ *   a launch holds 2^23 workgroups: (routes / 128 + experts) n / 128, experts
+ *   n / 16, and with weights (routes / top) n / 256 stay below that.
+ *   workspace w8_experts_matmul_workspace_bytes(routes, n, weights != NULL)
+ *             bytes or more, 16-byte aligned, scratch: needed with weights.
+ */
+size_t w8_experts_matmul_workspace_bytes(int32_t routes, int32_t n, int32_t combine);
+wino_status w8_experts_matmul(const int8_t* x, int64_t x_stride, const float* x_scales, int32_t x_rows, const int8_t* w,
+                              const float* w_scales, const int32_t* order, const int32_t* ends, int32_t routes,
+                              int32_t experts, const int32_t* chosen, const float* weights, int32_t top, void* y,
+                              int64_t y_stride, int32_t n, int32_t k, wino_float_type type, void* workspace,
+                              size_t workspace_bytes, hipStream_t stream);
 
 /* Static description of a status code; never NULL. */
 const char* wino_strerror(wino_status status);

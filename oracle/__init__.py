@@ -14,6 +14,7 @@ Modules
   quant     round / clamp / power-of-two exponent rules (Sec. III, Eq. quant)
   direct    direct 3x3 convolution: float64, integer, and brute force
   decoder   the 4-bit format and the decoder operators in float64
+  decoder8  the 8-bit decoder operators in whole numbers, rationals and float64
   tapwise   the tap-wise quantized integer Winograd F4 pipeline (Sec. III),
             its offline plan, input/output calibration, and analytic bounds
 """

@@ -25,4 +25,7 @@ from .binding import (  # noqa: F401
     ROTARY_HALVES, ROTARY_PAIRS, KV4_ROTATED, KV4_CACHED,
     w4_quantize_weights, w4_matvec_workspace_bytes, w4_matvec, kv4_append,
     kv4_attention_workspace_bytes, kv4_attention, prompt_attention,
+    SCORE_SOFTMAX, SCORE_SIGMOID,
+    w8_quantize, w8_matmul_workspace_bytes, w8_matmul, route_experts_workspace_bytes, route_experts,
+    w8_experts_matmul_workspace_bytes, w8_experts_matmul,
 )

@@ -18,6 +18,7 @@ NOALLOC_SCRATCH_BYTES = 64 << 20   # WINO_NOALLOC_SCRATCH_BYTES
 ALGO_DIRECT, ALGO_F2, ALGO_F4 = 0, 2, 4
 ROTARY_HALVES, ROTARY_PAIRS = 0, 1
 KV4_ROTATED, KV4_CACHED = 0, 1
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
@@ -35,6 +36,8 @@ EXPORTS = [
     "direct_conv_quantize_weights", "direct_conv_int8", "wino_f4_conv_float", "wino_strerror",
     "w4_quantize_weights", "w4_matvec_workspace_bytes", "w4_matvec", "kv4_append",
     "kv4_attention_workspace_bytes", "kv4_attention", "prompt_attention",
+    "w8_quantize", "w8_matmul_workspace_bytes", "w8_matmul", "route_experts_workspace_bytes", "route_experts",
+    "w8_experts_matmul_workspace_bytes", "w8_experts_matmul",
 ]
 # include/winof4_probe.h: the measurement probes, outside the method's interface.
 PROBE_EXPORTS = ["wino_probe_mfma_int8", "wino_probe_conv_kernels"]
@@ -118,6 +121,13 @@ def load_library():
         "kv4_attention": (I32, [P, I64, P, P, I32, P, P, I32, I32, I32, F32, I32, P, SZ, P]),
         "prompt_attention": (I32, [P, I64, P, I64, P, I64, P, P, I32, I32, I32, I32, I32, I32, I32, F32, I32, P, I32,
                                    P]),
+        "w8_quantize": (I32, [P, I64, P, P, I32, I32, I32, P]),
+        "w8_matmul_workspace_bytes": (SZ, [I32, I32, I32]),
+        "w8_matmul": (I32, [P, I64, P, P, P, P, P, I64, I32, I32, I32, I32, P, SZ, P]),
+        "route_experts_workspace_bytes": (SZ, [I32, I32, I32]),
+        "route_experts": (I32, [P, I64, P, I32, I32, I32, I32, I32, I32, I32, I32, F32, P, P, P, P, P, I32, P, SZ, P]),
+        "w8_experts_matmul_workspace_bytes": (SZ, [I32, I32, I32]),
+        "w8_experts_matmul": (I32, [P, I64, P, I32, P, P, P, P, I32, I32, P, P, I32, P, I64, I32, I32, I32, P, SZ, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -582,7 +592,7 @@ def wino_probe_conv_kernels(plan, x, n, h, w, layout=NCHW):
     return dict(d, xform=PROBE_XFORMS[d["xform"]], gemm=PROBE_GEMMS[d["gemm"]])
 
 
-# ---- Decoder operators in 4 bits: tensors carry the sizes and the type, and
+# ---- Decoder operators in 4 and 8 bits: tensors carry the sizes and the type, and
 # are checked in _marshal.so (csrc/marshal.cpp).
 
 class _KV4Cache(ctypes.Structure):
@@ -689,3 +699,52 @@ def prompt_attention(q, k, v, cu_q, cu_k, max_q, out, scale, causal=True, stream
     st = (_MARSHAL or _marshal()).prompt_attention(q, k, v, cu_q, cu_k, max_q, out, scale, causal, handle, device)
     if st:
         _check(st, "prompt_attention")
+
+
+def w8_quantize(x, codes, scales, stream=None):
+    """Codes int8 [m, k] and scales fp32 [m] of the rows of x [m, k]."""
+    handle, device = _place(stream)
+    st = (_MARSHAL or _marshal()).w8_quantize(x, codes, scales, handle, device)
+    if st:
+        _check(st, "w8_quantize")
+
+
+def w8_matmul_workspace_bytes(m, n, k):
+    return int(load_library().w8_matmul_workspace_bytes(m, n, k))
+
+
+def w8_matmul(x, x_scales, w, w_scales, y, bias=None, workspace=None, stream=None):
+    """y [m, n] = codes x [m, k] times codes w [n, k] transposed, scaled by x_scales [m] and w_scales [n], + bias."""
+    handle, device = _place(stream)
+    st = (_MARSHAL or _marshal()).w8_matmul(x, x_scales, w, w_scales, y, bias, workspace, handle, device)
+    if st:
+        _check(st, "w8_matmul")
+
+
+def route_experts_workspace_bytes(tokens, experts, top):
+    return int(load_library().route_experts_workspace_bytes(tokens, experts, top))
+
+
+def route_experts(logits, chosen, weights, order=None, ends=None, bias=None, score=SCORE_SOFTMAX, groups=1, top_groups=1,
+                  group_best=1, normalise=True, scale=1.0, live=None, workspace=None, stream=None):
+    """chosen int32 and weights fp32 [tokens, top] of logits [tokens, experts]; order int32 [tokens * top] and ends
+    int32 [experts + 1]: the routes by expert (with a workspace)."""
+    handle, device = _place(stream)
+    st = (_MARSHAL or _marshal()).route_experts(logits, chosen, weights, order, ends, bias, score, groups, top_groups,
+                                                group_best, normalise, scale, live, workspace, handle, device)
+    if st:
+        _check(st, "route_experts")
+
+
+def w8_experts_matmul_workspace_bytes(routes, n, combine):
+    return int(load_library().w8_experts_matmul_workspace_bytes(routes, n, int(bool(combine))))
+
+
+def w8_experts_matmul(x, x_scales, w, w_scales, order, ends, y, chosen=None, weights=None, workspace=None, stream=None):
+    """Products of the routes' rows of x with their experts' codes w [experts, n, k]: y [routes, n], or with chosen and
+    weights [tokens, top] their weighted sums y [tokens, n]; x has a row for each token or for each route."""
+    handle, device = _place(stream)
+    st = (_MARSHAL or _marshal()).w8_experts_matmul(x, x_scales, w, w_scales, order, ends, y, chosen, weights, workspace,
+                                                    handle, device)
+    if st:
+        _check(st, "w8_experts_matmul")

@@ -17,7 +17,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libwinof4.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")
 SOURCES = ["plan.cpp", "plan_device.hip", "wino_kernels.hip", "wino_fused.hip", "direct_conv.hip", "wino_float.hip", "probe.hip",
-           "w4_quantize.cpp", "w4_matvec.hip", "kv4_append.hip", "kv4_attention.hip", "prompt_attention.hip"]
+           "w4_quantize.cpp", "w4_matvec.hip", "kv4_append.hip", "kv4_attention.hip", "prompt_attention.hip",
+           "w8_quantize.hip", "w8_matmul.hip", "w8_experts.hip", "route_experts.hip"]
 ARCH = "gfx950"
 # Packed fp32 instructions are disabled for every HIP translation unit; the
 # host pass prints a harmless note that it does not know the feature.

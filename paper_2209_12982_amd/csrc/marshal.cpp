@@ -277,11 +277,123 @@ PyObject* prompt(PyObject*, PyObject* const* a, Py_ssize_t given) {
     });
 }
 
+// x, codes, scales, stream, device
+PyObject* quantize8(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return call(given, 5, [&]() -> long {
+        const Gpu gpu{integer(a[4])};
+        const at::Tensor& x = gpu.tensor(a[0], "x");
+        dims(x, 2, "x");
+        const wino_float_type kind = float_type(x, "x");
+        const int64_t m = x.size(0), k = x.size(1);
+        int64_t xs;
+        const void* xp = gpu.rows(a[0], x.scalar_type(), {m, k}, "x", &xs);
+        int8_t* cp = (int8_t*)gpu.dense(a[1], at::kChar, {m, k}, "codes");
+        float* sp = (float*)gpu.dense(a[2], at::kFloat, {m}, "scales");
+        return w8_quantize(xp, xs, cp, sp, fit32(m, "rows of x"), fit32(k, "columns"), kind, stream_of(a[3]));
+    });
+}
+
+// x, x_scales, w, w_scales, y, bias, workspace, stream, device
+PyObject* matmul8(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return call(given, 9, [&]() -> long {
+        const Gpu gpu{integer(a[8])};
+        const at::Tensor &x = gpu.tensor(a[0], "x"), &w = gpu.tensor(a[2], "w"), &y = gpu.tensor(a[4], "y");
+        dims(x, 2, "x");
+        dims(w, 2, "w");
+        const wino_float_type kind = float_type(y, "y");
+        const int64_t m = x.size(0), k = x.size(1), n = w.size(0);
+        int64_t xs, ys;
+        size_t bytes;
+        const int8_t* xp = (const int8_t*)gpu.rows(a[0], at::kChar, {m, k}, "x", &xs);
+        const float* sp = (const float*)gpu.dense(a[1], at::kFloat, {m}, "x_scales");
+        const int8_t* wp = (const int8_t*)gpu.dense(a[2], at::kChar, {n, k}, "w");
+        const float* tp = (const float*)gpu.dense(a[3], at::kFloat, {n}, "w_scales");
+        void* yp = gpu.rows(a[4], y.scalar_type(), {m, n}, "y", &ys);
+        const void* bp = gpu.dense_or_none(a[5], y.scalar_type(), {n}, "bias");
+        void* ws = gpu.scratch(a[6], &bytes);
+        return w8_matmul(xp, xs, sp, wp, tp, bp, yp, ys, fit32(m, "rows of x"), fit32(n, "rows of the weights"), fit32(k, "columns"),
+                         kind, ws, bytes, stream_of(a[7]));
+    });
+}
+
+// logits, chosen, weights, order, ends, bias, score, groups, top_groups, group_best, normalise, scale, live, workspace,
+// stream, device
+PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return call(given, 16, [&]() -> long {
+        const Gpu gpu{integer(a[15])};
+        const at::Tensor &logits = gpu.tensor(a[0], "logits"), &chosen = gpu.tensor(a[1], "chosen");
+        dims(logits, 2, "logits");
+        dims(chosen, 2, "chosen");
+        const wino_float_type kind = logits.scalar_type() == at::kFloat ? WINO_FP32 : float_type(logits, "logits");
+        const int64_t tokens = logits.size(0), experts = logits.size(1), top = chosen.size(1);
+        int64_t stride;
+        size_t bytes;
+        const void* lp = gpu.rows(a[0], logits.scalar_type(), {tokens, experts}, "logits", &stride);
+        int32_t* cp = (int32_t*)gpu.dense(a[1], at::kInt, {tokens, top}, "chosen");
+        float* wp = (float*)gpu.dense(a[2], at::kFloat, {tokens, top}, "weights");
+        if ((a[3] == Py_None) != (a[4] == Py_None)) throw Misfit{"order and ends go together"};
+        int32_t* op = (int32_t*)gpu.dense_or_none(a[3], at::kInt, {tokens * top}, "order");
+        int32_t* ep = (int32_t*)gpu.dense_or_none(a[4], at::kInt, {experts + 1}, "ends");
+        const float* bp = (const float*)gpu.dense_or_none(a[5], at::kFloat, {experts}, "bias");
+        const int normalise = PyObject_IsTrue(a[10]);
+        if (normalise < 0) throw Misfit{""};
+        const float scale = real(a[11]);
+        const int32_t* vp = (const int32_t*)gpu.dense_or_none(a[12], at::kInt, {1}, "live");
+        void* ws = gpu.scratch(a[13], &bytes);
+        return route_experts(lp, stride, bp, fit32(tokens, "tokens"), fit32(experts, "experts"), fit32(top, "experts of a token"),
+                             (wino_score)small(a[6], "score"), small(a[7], "groups"), small(a[8], "top_groups"),
+                             small(a[9], "group_best"), normalise, scale, vp, cp, wp, op, ep, kind, ws, bytes, stream_of(a[14]));
+    });
+}
+
+// x, x_scales, w, w_scales, order, ends, y, chosen, weights, workspace, stream, device
+PyObject* experts8(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return call(given, 12, [&]() -> long {
+        const Gpu gpu{integer(a[11])};
+        const at::Tensor &x = gpu.tensor(a[0], "x"), &w = gpu.tensor(a[2], "w"), &order = gpu.tensor(a[4], "order"),
+                         &y = gpu.tensor(a[6], "y");
+        dims(x, 2, "x");
+        dims(w, 3, "w");
+        dims(order, 1, "order");
+        const wino_float_type kind = float_type(y, "y");
+        const int64_t x_rows = x.size(0), k = x.size(1), experts = w.size(0), n = w.size(1), routes = order.size(0);
+        if ((a[7] == Py_None) != (a[8] == Py_None)) throw Misfit{"chosen and weights go together"};
+        int64_t top = 1, xs, ys;
+        const int32_t* cp = nullptr;
+        const float* gp = nullptr;
+        if (a[8] != Py_None) {
+            const at::Tensor& weights = gpu.tensor(a[8], "weights");
+            dims(weights, 2, "weights");
+            top = weights.size(1);
+            if (weights.numel() != routes) throw Misfit{"weights: as many as routes in the order are expected"};
+            gp = (const float*)gpu.dense(a[8], at::kFloat, {weights.size(0), top}, "weights");
+            cp = (const int32_t*)gpu.dense(a[7], at::kInt, {weights.size(0), top}, "chosen");
+        }
+        if (x_rows ? routes % x_rows : routes) throw Misfit{"x: a row for each token or for each route is expected"};
+        size_t bytes;
+        const int8_t* xp = (const int8_t*)gpu.rows(a[0], at::kChar, {x_rows, k}, "x", &xs);
+        const float* sp = (const float*)gpu.dense(a[1], at::kFloat, {x_rows}, "x_scales");
+        const int8_t* wp = (const int8_t*)gpu.dense(a[2], at::kChar, {experts, n, k}, "w");
+        const float* tp = (const float*)gpu.dense(a[3], at::kFloat, {experts, n}, "w_scales");
+        const int32_t* op = (const int32_t*)gpu.dense(a[4], at::kInt, {routes}, "order");
+        const int32_t* ep = (const int32_t*)gpu.dense(a[5], at::kInt, {experts + 1}, "ends");
+        void* yp = gpu.rows(a[6], y.scalar_type(), {top ? routes / top : 0, n}, "y", &ys);
+        void* ws = gpu.scratch(a[9], &bytes);
+        return w8_experts_matmul(xp, xs, sp, fit32(x_rows, "rows of x"), wp, tp, op, ep, fit32(routes, "routes"),
+                                 fit32(experts, "experts"), cp, gp, fit32(top, "experts of a token"), yp, ys,
+                                 fit32(n, "rows of the weights"), fit32(k, "columns"), kind, ws, bytes, stream_of(a[10]));
+    });
+}
+
 PyMethodDef methods[] = {
     {"w4_matvec", (PyCFunction)(void (*)())matvec, METH_FASTCALL, nullptr},
     {"kv4_append", (PyCFunction)(void (*)())append, METH_FASTCALL, nullptr},
     {"kv4_attention", (PyCFunction)(void (*)())attention, METH_FASTCALL, nullptr},
     {"prompt_attention", (PyCFunction)(void (*)())prompt, METH_FASTCALL, nullptr},
+    {"w8_quantize", (PyCFunction)(void (*)())quantize8, METH_FASTCALL, nullptr},
+    {"w8_matmul", (PyCFunction)(void (*)())matmul8, METH_FASTCALL, nullptr},
+    {"route_experts", (PyCFunction)(void (*)())route, METH_FASTCALL, nullptr},
+    {"w8_experts_matmul", (PyCFunction)(void (*)())experts8, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalling of the decoder operators.", -1, methods};

@@ -1,0 +1,92 @@
+// w8_experts_matmul: each route's row of 8-bit codes times its expert's 8-bit weights, routes in the order of their
+// experts; optionally the weighted sum of a token's routes.
+#include <algorithm>
+
+#include "w8_rows.h"
+#include "w8_tiles.h"
+
+namespace {
+using namespace w8;
+
+// out[t] = sum_j weights[t][j] products[t top + j], in the order of j; routes without an expert add nothing.
+template <int TYPE>
+__global__ __launch_bounds__(256) void w8_combine_kernel(Args a, const int32_t* chosen, const float* weights, int top) {
+    typedef typename Half<TYPE>::type T;
+    const int col = blockIdx.y * 256 + threadIdx.x;
+    const int64_t token = blockIdx.x;
+    if (col >= a.n) return;
+    float sum = 0.f;
+    for (int j = 0; j < top; ++j) {
+        const int64_t route = token * top + j;
+        if ((uint32_t)chosen[route] < (uint32_t)a.experts) sum += weights[route] * a.products[route * a.n + col];
+    }
+    ((T*)a.y)[token * a.y_stride + col] = (T)sum;
+}
+
+template <int TYPE, int MT, int NT> void launch_rows(const Args& a, hipStream_t stream) {
+    const dim3 grid((unsigned)((a.n + 16 * NT - 1) / (16 * NT)), (unsigned)a.experts);
+    hipLaunchKernelGGL((w8_rows_kernel<TYPE, MT, NT, 8, true>), grid, dim3(512), 0, stream, a);
+}
+template <int TYPE, class S> void launch_tiles(const Args& a, hipStream_t stream) {
+    const int n_tiles = (a.n + S::kOuts - 1) / S::kOuts;
+    // whole tiles of the rows, and one more for each expert's last
+    const int m_tiles = a.routes / S::kRows + std::min(a.experts, a.routes);
+    hipLaunchKernelGGL((w8_tiles_kernel<TYPE, S, true>), dim3((unsigned)n_tiles * (unsigned)m_tiles), dim3(S::kThreads), 0, stream,
+                       a, n_tiles, m_tiles);
+}
+
+template <int TYPE> void pick(const Args& a, hipStream_t stream) {
+    if (a.routes <= 32 * a.experts)
+        launch_rows<TYPE, 1, 2>(a, stream);
+    else
+        launch_tiles<TYPE, Tile<2, 1, 2, 4, 128, 2>>(a, stream);
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
+
+}  // namespace
+
+extern "C" size_t w8_experts_matmul_workspace_bytes(int32_t routes, int32_t n, int32_t combine) {
+    if (routes < 1 || n < 1 || !combine) return 0;
+    return (size_t)routes * n * sizeof(float);
+}
+
+extern "C" wino_status w8_experts_matmul(const int8_t* x, int64_t x_stride, const float* x_scales, int32_t x_rows, const int8_t* w,
+                                         const float* w_scales, const int32_t* order, const int32_t* ends, int32_t routes,
+                                         int32_t experts, const int32_t* chosen, const float* weights, int32_t top, void* y,
+                                         int64_t y_stride, int32_t n, int32_t k, wino_float_type type, void* workspace,
+                                         size_t workspace_bytes, hipStream_t stream) {
+    if (type != WINO_BF16 && type != WINO_FP16) return WINO_EINVAL;
+    if (x_rows < 0 || routes < 0 || experts < 1 || n < 0 || k < 0 || k % 16 != 0) return WINO_EINVAL;
+    if ((weights != nullptr) != (chosen != nullptr) || (weights && (top < 1 || routes % top != 0))) return WINO_EINVAL;
+    if (routes == 0 || n == 0) return WINO_OK;
+    if (x_rows < 1 || routes % x_rows != 0) return WINO_EINVAL;
+    if (!y || !x_scales || !w_scales || !order || !ends || (k > 0 && (!x || !w))) return WINO_EINVAL;
+    const int32_t y_rows = weights ? routes / top : routes;
+    if ((x_rows > 1 && x_stride < k) || (y_rows > 1 && y_stride < n)) return WINO_EINVAL;
+    if (routes > 1 << 22 || experts > 1024 || n > 1 << 20 || k >= 1 << 17) return WINO_EUNSUPPORTED;
+    if (!aligned16(x) || !aligned16(w) || !aligned16(workspace) || !aligned4(x_scales) || !aligned4(w_scales) || !aligned4(order) ||
+        !aligned4(ends) || !aligned4(chosen) || !aligned4(weights) || ((uintptr_t)y & 1) || (k > 0 && x_rows > 1 && (x_stride & 15)))
+        return WINO_EUNSUPPORTED;
+    if (!launch_holds((int64_t)(routes / 128 + experts) * ((n + 127) / 128)) || !launch_holds((int64_t)((n + 15) / 16) * experts) ||
+        (weights && !launch_holds((int64_t)y_rows * ((n + 255) / 256))))
+        return WINO_EUNSUPPORTED;
+    Args a = {};
+    a.x = x, a.w = w, a.x_scales = x_scales, a.w_scales = w_scales, a.y = y, a.x_stride = x_stride, a.y_stride = y_stride;
+    a.n = n, a.k = k, a.order = order, a.ends = ends, a.experts = experts, a.routes = routes;
+    a.share = winof4::make_fastdiv((uint32_t)(routes / x_rows));
+    if (weights) {
+        if (!workspace || workspace_bytes < w8_experts_matmul_workspace_bytes(routes, n, 1)) return WINO_EINVAL;
+        a.products = (float*)workspace;
+    }
+    type == WINO_BF16 ? pick<WINO_BF16>(a, stream) : pick<WINO_FP16>(a, stream);
+    if (weights && hipGetLastError() == hipSuccess) {
+        const dim3 grid((unsigned)y_rows, (unsigned)((n + 255) / 256));
+        if (type == WINO_BF16)
+            hipLaunchKernelGGL((w8_combine_kernel<WINO_BF16>), grid, dim3(256), 0, stream, a, chosen, weights, top);
+        else
+            hipLaunchKernelGGL((w8_combine_kernel<WINO_FP16>), grid, dim3(256), 0, stream, a, chosen, weights, top);
+    }
+    return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
+}

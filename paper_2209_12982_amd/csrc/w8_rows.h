@@ -1,0 +1,100 @@
+// Few rows times 8-bit weights (at most 64 at a time): every byte of the weights is read once and used by one wave.
+// A workgroup has 16 NT outputs; its V waves share out k in steps of 128 bytes, and their sums meet in LDS.
+//
+// Rows of the weights are rows of the first operand of mfma 16x16x64, rows of x columns of the second.  Which part of k
+// stands where in an operand is free as long as both agree: a lane reads 32 neighbouring bytes of its row, the first 16 for
+// one product and the rest for the next, so that the two loads of a wave take whole lines of 128 bytes.
+#pragma once
+#include "w8_device.h"
+
+namespace w8 {
+
+template <int TYPE, int MT, int NT, int V, bool EXPERTS>
+__global__ __launch_bounds__(64 * V) void w8_rows_kernel(Args a) {
+    typedef typename Half<TYPE>::type T;
+    constexpr int kRows = 16 * MT, kOuts = 16 * NT, kAhead = NT * MT >= 8 ? 1 : 2;     // steps whose loads are on their way together
+    __shared__ int sums[kRows][kOuts + 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, quarter = lane >> 4;
+    const int n0 = blockIdx.x * kOuts;
+    int begin = 0, end = a.m, expert = 0;
+    if (EXPERTS) {
+        expert = blockIdx.y;
+        rows_of(a, expert, begin, end);
+    }
+    const int8_t* w[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+        w[i] = a.w + ((int64_t)expert * a.n + min(n0 + 16 * i + r, a.n - 1)) * a.k + 32 * quarter;
+    const int all = (a.k + 127) / 128;
+    const int first = EXPERTS ? 0 : (int)blockIdx.z * a.steps, last = EXPERTS ? all : min(first + a.steps, all);
+    for (int m0 = begin + (EXPERTS ? 0 : (int)blockIdx.y * kRows); m0 < end; m0 += kRows) {
+        const int8_t* x[MT];
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+            const int at = min(m0 + 16 * j + r, end - 1);
+            x[j] = a.x + (EXPERTS ? x_row(a, a.order[at]) : at) * a.x_stride + 32 * quarter;
+        }
+        for (int o = threadIdx.x; o < kRows * kOuts; o += 64 * V) sums[o / kOuts][o % kOuts] = 0;
+        i32x4 acc[NT][MT];
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int j = 0; j < MT; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+        for (int s0 = first + wave; s0 < last; s0 += V * kAhead) {
+            i32x4 wv[kAhead][NT][2], xv[kAhead][MT][2];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int64_t at = (int64_t)(s0 + u * V) * 128;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const bool there = s0 + u * V < last && at + 32 * quarter + 16 * h < a.k;   // k is a multiple of 16
+                    const int64_t off = at + 16 * h;
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) wv[u][i][h] = *(const i32x4*)(there ? w[i] + off : (const int8_t*)kZeros);
+#pragma unroll
+                    for (int j = 0; j < MT; ++j) xv[u][j][h] = *(const i32x4*)(there ? x[j] + off : (const int8_t*)kZeros);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < NT; ++i)
+#pragma unroll
+                        for (int j = 0; j < MT; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[u][i][h], xv[u][j][h], acc[i][j], 0, 0, 0);
+        }
+        __syncthreads();                                    // the zeros are there
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int j = 0; j < MT; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) atomicAdd(&sums[16 * j + r][16 * i + 4 * quarter + e], acc[i][j][e]);
+        __syncthreads();
+        for (int o = threadIdx.x; o < kRows * kOuts; o += 64 * V) {
+            const int at = m0 + o / kOuts, c = n0 + o % kOuts;
+            if (at >= end || c >= a.n) continue;
+            const int sum = sums[o / kOuts][o % kOuts];
+            if (EXPERTS) {
+                const int route = a.order[at];
+                if ((uint32_t)route >= (uint32_t)a.routes) continue;
+                const float y = finish(sum, a.x_scales[x_row(a, route)], a.w_scales[(int64_t)expert * a.n + c], 0.f);
+                if (a.products)
+                    a.products[(int64_t)route * a.n + c] = y;
+                else
+                    ((T*)a.y)[route * a.y_stride + c] = (T)y;
+            } else if (a.part) {
+                a.part[((int64_t)blockIdx.z * a.m + at) * a.n + c] = sum;
+            } else {
+                ((T*)a.y)[at * a.y_stride + c] =
+                    (T)finish(sum, a.x_scales[at], a.w_scales[c], a.bias ? (float)((const T*)a.bias)[c] : 0.f);
+            }
+        }
+        __syncthreads();                                    // before the sums are cleared again
+    }
+}
+
+}  // namespace w8
