@@ -46,9 +46,12 @@ __device__ inline int64_t x_row(const Args& a, int route) {
     return (uint32_t)route < (uint32_t)a.routes ? winof4::fast_div((uint32_t)route, a.share) : 0;
 }
 
-// The result of a sum; written out so that every kernel rounds at the same places.
+// The result of a sum, the same bits in every kernel: the last step is kept apart from a conversion to fp16 after it, which
+// the compiler would otherwise take together with it in some kernels (v_fma_mixlo_f16, one rounding instead of two).
 __device__ inline float finish(int sum, float x_scale, float w_scale, float bias) {
-    return __builtin_fmaf((float)sum * x_scale, w_scale, bias);
+    float y = __builtin_fmaf((float)sum * x_scale, w_scale, bias);
+    asm("" : "+v"(y));
+    return y;
 }
 
 // Whether a launch holds so many workgroups (of 512 threads; it counts threads in 32 bits).

@@ -27,19 +27,20 @@ template <int TYPE, int MT, int NT> void launch_rows(const Args& a, hipStream_t 
     const dim3 grid((unsigned)((a.n + 16 * NT - 1) / (16 * NT)), (unsigned)a.experts);
     hipLaunchKernelGGL((w8_rows_kernel<TYPE, MT, NT, 8, true>), grid, dim3(512), 0, stream, a);
 }
-template <int TYPE, class S> void launch_tiles(const Args& a, hipStream_t stream) {
+template <int TYPE, class S, bool FAR = false> void launch_tiles(const Args& a, hipStream_t stream) {
     const int n_tiles = (a.n + S::kOuts - 1) / S::kOuts;
     // whole tiles of the rows, and one more for each expert's last
     const int m_tiles = a.routes / S::kRows + std::min(a.experts, a.routes);
-    hipLaunchKernelGGL((w8_tiles_kernel<TYPE, S, true>), dim3((unsigned)n_tiles * (unsigned)m_tiles), dim3(S::kThreads), 0, stream,
+    hipLaunchKernelGGL((w8_tiles_kernel<TYPE, S, true, FAR>), dim3((unsigned)n_tiles * (unsigned)m_tiles), dim3(S::kThreads), 0, stream,
                        a, n_tiles, m_tiles);
 }
 
-template <int TYPE> void pick(const Args& a, hipStream_t stream) {
+template <int TYPE> void pick(const Args& a, int64_t x_rows, hipStream_t stream) {
+    if (far(x_rows, a.x_stride, a.k)) return launch_tiles<TYPE, Tile64x128, true>(a, stream);
     if (a.routes <= 32 * a.experts)
         launch_rows<TYPE, 1, 2>(a, stream);
     else
-        launch_tiles<TYPE, Tile<2, 1, 2, 4, 128, 2>>(a, stream);
+        launch_tiles<TYPE, Tile128x128>(a, stream);
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
@@ -80,7 +81,7 @@ extern "C" wino_status w8_experts_matmul(const int8_t* x, int64_t x_stride, cons
         if (!workspace || workspace_bytes < w8_experts_matmul_workspace_bytes(routes, n, 1)) return WINO_EINVAL;
         a.products = (float*)workspace;
     }
-    type == WINO_BF16 ? pick<WINO_BF16>(a, stream) : pick<WINO_FP16>(a, stream);
+    type == WINO_BF16 ? pick<WINO_BF16>(a, x_rows, stream) : pick<WINO_FP16>(a, x_rows, stream);
     if (weights && hipGetLastError() == hipSuccess) {
         const dim3 grid((unsigned)y_rows, (unsigned)((n + 255) / 256));
         if (type == WINO_BF16)

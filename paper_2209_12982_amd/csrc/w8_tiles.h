@@ -6,20 +6,34 @@
 // the same piece fall into the sixteen columns of the 256-byte banks.  Within 32 rows of weights the copy puts row
 // 16 h + 4 q + e where operand row 8 q + 4 h + e is read: a lane's sixteen sums are then neighbouring outputs of one row.
 #pragma once
+#include <type_traits>
+
 #include "w8_device.h"
 
 namespace w8 {
 
-template <int WN_, int WM_, int GN_, int GM_, int BK_, int STAGES_> struct Tile {
-    static constexpr int WN = WN_, WM = WM_, GN = GN_, GM = GM_, BK = BK_, STAGES = STAGES_;
-    static constexpr int kWaves = GN * GM, kThreads = 64 * kWaves;
+template <int N> using Int = std::integral_constant<int, N>;
+
+template <int WN_, int WM_, int GN_, int GM_, int GK_, int BK_, int STAGES_> struct Tile {
+    static constexpr int WN = WN_, WM = WM_, GN = GN_, GM = GM_, GK = GK_, BK = BK_, STAGES = STAGES_;
+    static constexpr int kWaves = GN * GM * GK, kThreads = 64 * kWaves;
     static constexpr int kOuts = 32 * WN * GN, kRows = 32 * WM * GM;        // of a workgroup
     static constexpr int kRowPieces = BK / 16;
     static constexpr int kPiecesW = kOuts * kRowPieces / kThreads, kPiecesX = kRows * kRowPieces / kThreads;    // of a thread
     static constexpr int kBytesW = kOuts * BK, kBytes = kBytesW + kRows * BK;
     static_assert(kOuts * kRowPieces % kThreads == 0 && kRows * kRowPieces % kThreads == 0, "whole copies");
-    static __device__ int swap(int row) { return BK == 128 ? (row >> 1) & 7 : (row >> 2) & 3; }
+    static __device__ int swap(int row) { return BK >= 256 ? row & 15 : (BK == 128 ? (row >> 1) & 7 : (row >> 2) & 3); }
 };
+
+// 16 bytes a lane from base + off to LDS at dst + 16 lane, which is on its way until vmcnt says otherwise; in assembly
+// because the compiler would wait for all copies before each read of LDS.  A scalar base moves on from stage to stage
+// without vector instructions, which take issue slots from the matrix products.
+__device__ inline void copy16(const void* base, uint32_t off, uint32_t dst) {
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(dst) : "memory");
+}
+__device__ inline void copy16_from(const void* from, uint32_t dst) {
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(dst) : "memory");
+}
 
 // The tile of the experts' rows that is the index-th: its expert, and where its rows begin and end in the order.
 template <int ROWS> __device__ inline bool find(const Args& a, int index, int& expert, int& begin, int& end) {
@@ -47,12 +61,13 @@ template <int ROWS> __device__ inline bool find(const Args& a, int index, int& e
     return false;
 }
 
-template <int TYPE, class S, bool EXPERTS>
+// FAR: rows of x whose distance from the first of a tile (experts: of x) does not fit 32 bits.
+template <int TYPE, class S, bool EXPERTS, bool FAR = false>
 __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_tiles, int m_tiles) {
     typedef typename Half<TYPE>::type T;
     typedef __attribute__((ext_vector_type(2))) T T2;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[S::STAGES][S::kBytes];
-    __shared__ float w_scale[S::kOuts], bias[S::kOuts], x_scale[S::kRows];
+    __shared__ __attribute__((aligned(16))) float w_scale[S::kOuts], bias[S::kOuts], x_scale[S::kRows];
     __shared__ int out_row[S::kRows];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 31, half = lane >> 5;
@@ -88,7 +103,8 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
         out_row[o] = m0 + o < m1 && (!EXPERTS || (uint32_t)route < (uint32_t)a.routes) ? route : -1;
     }
 
-    const int8_t *from_w[S::kPiecesW], *from_x[S::kPiecesX];
+    // pieces that this thread copies: where they come from, relative to the tile's weights and to x
+    uint32_t from_w[S::kPiecesW], from_x[S::kPiecesX];
     auto place = [&](int p, int& row, int& piece) {
         row = p / S::kRowPieces;
         piece = (p % S::kRowPieces) ^ S::swap(row);
@@ -98,32 +114,49 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
         int row, piece;
         place((i * S::kWaves + wave) * 64 + lane, row, piece);
         const int w_row = (row & ~31) | (row >> 2 & 1) << 4 | (row >> 3 & 3) << 2 | (row & 3);
-        from_w[i] = a.w + ((int64_t)expert * a.n + min(n0 + w_row, a.n - 1)) * a.k + (int64_t)first * S::BK + 16 * piece;
+        from_w[i] = (uint32_t)(min(n0 + w_row, a.n - 1) - n0) * (uint32_t)a.k + 16 * piece;
     }
 #pragma unroll
     for (int i = 0; i < S::kPiecesX; ++i) {
         int row, piece;
         place((i * S::kWaves + wave) * 64 + lane, row, piece);
         const int at = min(m0 + row, m1 - 1);
-        from_x[i] = a.x + (EXPERTS ? x_row(a, a.order[at]) : at) * a.x_stride + (int64_t)first * S::BK + 16 * piece;
+        const int64_t row_x = EXPERTS ? x_row(a, a.order[at]) : at - m0;
+        from_x[i] = FAR ? (uint32_t)row_x : (uint32_t)(row_x * a.x_stride) + 16 * piece;
     }
-    typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
-    const lds_ptr to = (lds_ptr)&lds[0][0] + wave * 1024;
+    const int8_t* w_base = a.w + ((int64_t)expert * a.n + n0) * a.k;
+    const int8_t* x_base = a.x + (EXPERTS ? 0 : m0 * a.x_stride);
+    const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&lds[0][0] + wave * 1024;
+    // Piece i of stage s on its way.  cut: the end of k lies inside the stage, what is behind it becomes 0.
+    auto copy_piece = [&](int s, int buf, int i, bool cut) {
+        const bool is_w = i < S::kPiecesW;
+        const int j = is_w ? i : i - S::kPiecesW;
+        const int8_t* base = (is_w ? w_base : x_base) + (int64_t)s * S::BK;
+        int row, piece;
+        place((j * S::kWaves + wave) * 64 + lane, row, piece);
+        const auto off = [&]() -> std::conditional_t<FAR, int64_t, uint32_t> {
+            if (is_w) return from_w[j];
+            if constexpr (FAR) return from_x[j] * a.x_stride + 16 * piece;
+            return from_x[j];
+        }();
+        const uint32_t dst = to + buf * S::kBytes + (is_w ? 0 : S::kBytesW) + j * (1024 * S::kWaves);
+        if (!cut) {
+            if constexpr (FAR)
+                copy16_from(base + off, dst);
+            else
+                copy16(base, off, dst);
+        } else {
+            copy16_from(s * S::BK + 16 * piece < a.k ? base + off : (const int8_t*)kZeros, dst);
+        }
+    };
+    constexpr int kPieces = S::kPiecesW + S::kPiecesX;
     auto copy = [&](int s, int buf) {
-        const bool cut = (s + 1) * S::BK > a.k;              // the end of k lies inside this stage
+        if ((s + 1) * S::BK <= a.k) {
 #pragma unroll
-        for (int i = 0; i < S::kPiecesW + S::kPiecesX; ++i) {
-            const bool is_w = i < S::kPiecesW;
-            const int j = is_w ? i : i - S::kPiecesW;
-            const int8_t*& from = is_w ? from_w[j] : from_x[j];
-            const int8_t* src = from;
-            if (cut) {
-                int row, piece;
-                place((j * S::kWaves + wave) * 64 + lane, row, piece);
-                if (s * S::BK + 16 * piece >= a.k) src = (const int8_t*)kZeros;
-            }
-            winof4::lds_copy16(src, to + buf * S::kBytes + (is_w ? 0 : S::kBytesW) + j * (1024 * S::kWaves));
-            from += S::BK;
+            for (int i = 0; i < kPieces; ++i) copy_piece(s, buf, i, false);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) copy_piece(s, buf, i, true);
         }
     };
 
@@ -135,84 +168,202 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
 
-    const int wn = wave % S::GN, wm = wave / S::GN;
-    constexpr int kPieces = S::kPiecesW + S::kPiecesX;
-#pragma unroll
-    for (int s = 0; s < S::STAGES - 1; ++s)
-        if (first + s < last) copy(first + s, s);
-    int buf = 0, next = S::STAGES - 1;
-    for (int s = first; s < last; ++s) {
-        // this stage has arrived once no more than the later ones are on their way
-        if (s + S::STAGES - 2 < last)
-            WINO_WAIT_VM_LDS((S::STAGES - 2) * kPieces);
-        else
-            WINO_WAIT_VM_LDS(0);
-        winof4::ring_barrier();                             // all waves' copies, and nobody reads the buffer that is filled next
-        if (s + S::STAGES - 1 < last) copy(s + S::STAGES - 1, next);
+    const int wn = wave % S::GN, wm = wave / S::GN % S::GM, wk = wave / (S::GN * S::GM);
+    constexpr int kSteps = S::BK / 32 / S::GK;              // of a wave
+    i32x4 w[2][S::WN], x[2][S::WM];                         // operands of a step of 32 of k, and of the next one
+    auto read = [&](int buf, int t, int to) {
         const uint8_t* lw = lds[buf] + (32 * S::WN * wn + c) * S::BK;
         const uint8_t* lx = lds[buf] + S::kBytesW + (32 * S::WM * wm + c) * S::BK;
+        const int at = ((2 * (kSteps * wk + t) + half) ^ S::swap(c)) * 16;
 #pragma unroll
-        for (int t = 0; t < S::BK / 32; ++t) {
-            const int at = ((2 * t + half) ^ S::swap(c)) * 16;
-            i32x4 w[S::WN], x[S::WM];
+        for (int i = 0; i < S::WN; ++i) w[to][i] = *(const i32x4*)(lw + i * (32 * S::BK) + at);
 #pragma unroll
-            for (int i = 0; i < S::WN; ++i) w[i] = *(const i32x4*)(lw + i * (32 * S::BK) + at);
+        for (int j = 0; j < S::WM; ++j) x[to][j] = *(const i32x4*)(lx + j * (32 * S::BK) + at);
+    };
+    auto multiply = [&](int from, int i) {
 #pragma unroll
-            for (int j = 0; j < S::WM; ++j) x[j] = *(const i32x4*)(lx + j * (32 * S::BK) + at);
+        for (int j = 0; j < S::WM; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[from][i], x[from][j], acc[i][j], 0, 0, 0);
+    };
+    int buf = 0, s = first;
+    // Takes stage s.  Before its last step the next one has to have arrived, for all waves, with no more than `later` stages
+    // on their way; all reads of this stage are done by then, so its buffer is filled again (FILL 1; 2: with the end of k).
+    auto stage = [&](auto fill, auto later) {
+        constexpr int FILL = decltype(fill)::value, LATER = decltype(later)::value;
+        const int after = buf + 1 == S::STAGES ? 0 : buf + 1;
 #pragma unroll
-            for (int i = 0; i < S::WN; ++i)
+        for (int t = 0; t < kSteps - 1; ++t) {
+            read(buf, t + 1, (t + 1) & 1);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int j = 0; j < S::WM; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[i], x[j], acc[i][j], 0, 0, 0);
+            for (int i = 0; i < S::WN; ++i) multiply(t & 1, i);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        buf = buf + 1 == S::STAGES ? 0 : buf + 1;
-        next = next + 1 == S::STAGES ? 0 : next + 1;
-    }
-    __syncthreads();                                        // the scales, where there was no stage
-
-#pragma unroll
-    for (int j = 0; j < S::WM; ++j) {
-        const int at = 32 * (S::WM * wm + j) + c, row = out_row[at];
-        if (row < 0) continue;
-        const float xs = x_scale[at];
+        if constexpr (LATER >= 0) {
+            WINO_WAIT_VM_LDS(LATER * kPieces);
+            winof4::ring_barrier();
+            read(after, 0, kSteps & 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < S::WN; ++i) {
-            const int o = 32 * (S::WN * wn + i) + 16 * half, col = n0 + o;
-            if (!EXPERTS && a.part) {
-                int32_t* to = a.part + ((int64_t)blockIdx.y * a.m + row) * a.n + col;
+            multiply((kSteps - 1) & 1, i);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (FILL != 0) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (col + e < a.n) to[e] = acc[i][j][e];
-                continue;
-            }
-            float y[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) y[e] = finish(acc[i][j][e], xs, w_scale[o + e], bias[o + e]);
-            if (EXPERTS && a.products) {
-                float* to = a.products + (int64_t)row * a.n + col;
-                if (col + 16 <= a.n && (a.n & 3) == 0) {
-#pragma unroll
-                    for (int e = 0; e < 16; e += 4) *(f32x4*)(to + e) = f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]};
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (col + e < a.n) to[e] = y[e];
-                }
-                continue;
-            }
-            T* to = (T*)a.y + row * a.y_stride + col;
-            if (col + 16 <= a.n && ((uintptr_t)to & 15) == 0) {
-                u32x4 out[2];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) out[e / 4][e % 4] = __builtin_bit_cast(uint32_t, T2{(T)y[2 * e], (T)y[2 * e + 1]});
-                *(u32x4*)to = out[0];
-                *(u32x4*)(to + 8) = out[1];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (col + e < a.n) to[e] = (T)y[e];
+                for (int p = i * kPieces / S::WN; p < (i + 1) * kPieces / S::WN; ++p) copy_piece(s + S::STAGES, buf, p, FILL == 2);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
+        buf = after;
+        ++s;
+    };
+#pragma unroll
+    for (int i = 0; i < S::STAGES; ++i)
+        if (first + i < last) copy(first + i, i);
+    if (first < last) {
+        WINO_WAIT_VM_LDS(0);
+        winof4::ring_barrier();
+        read(0, 0, 0);
+        const int whole = min(last, a.k / S::BK);           // stages without the end of k
+        while (s + S::STAGES < whole) stage(Int<1>(), Int<S::STAGES - 2>());
+        if (s + S::STAGES < last) stage(Int<2>(), Int<S::STAGES - 2>());
+        while (s + 1 < last) stage(Int<0>(), Int<0>());
+        stage(Int<0>(), Int<-1>());
     }
+    __syncthreads();                                        // nobody reads a stage any more
+
+    if constexpr (S::GK > 1) {                              // the parts of k meet
+        typedef __attribute__((ext_vector_type(4))) int Sum;
+        constexpr int kSums = S::WN * S::WM * 4;            // pieces of 16 bytes a lane
+        static_assert((S::GK - 1) * S::GN * S::GM * kSums * 1024 <= S::STAGES * S::kBytes, "room for the parts");
+        uint8_t* parts = &lds[0][0] + 16 * lane;
+        if (wk > 0) {
+#pragma unroll
+            for (int p = 0; p < kSums; ++p) {
+                const i32x16& z = acc[p / 4 / S::WM][p / 4 % S::WM];
+                *(Sum*)(parts + ((wave - S::GN * S::GM) * kSums + p) * 1024) = Sum{z[p % 4 * 4], z[p % 4 * 4 + 1], z[p % 4 * 4 + 2], z[p % 4 * 4 + 3]};
+            }
+        }
+        __syncthreads();
+        if (wk > 0) return;
+#pragma unroll
+        for (int k = 0; k < S::GK - 1; ++k)
+#pragma unroll
+            for (int p = 0; p < kSums; ++p) {
+                const Sum v = *(const Sum*)(parts + ((wave + k * S::GN * S::GM) * kSums + p) * 1024);
+                i32x16& z = acc[p / 4 / S::WM][p / 4 % S::WM];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[p % 4 * 4 + e] += v[e];
+            }
+    }
+
+    // 32 rows at a time, each wave turns its own results in LDS, so that sixteen lanes store 256 neighbouring bytes.  The
+    // 16-byte pieces of a row are exchanged by the row's number: both ways sixteen lanes meet sixteen columns of the banks.
+    uint8_t* mine = &lds[0][0] + (S::GK > 1 ? (S::GK - 1) * S::GN * S::GM * S::WN * S::WM * 4096 : 0) + wave * (S::WN * 4096);
+    static_assert((S::GK > 1 ? (S::GK - 1) * S::GN * S::GM * S::WN * S::WM * 4096 : 0) + S::GN * S::GM * S::WN * 4096 <= S::STAGES * S::kBytes, "room to turn");
+    const int col0 = n0 + 32 * S::WN * wn;
+    auto at = [&](int row, int byte) {
+        const int swap = S::WN == 1 ? (row >> 1) & 7 : row & 15;    // a row has 8 S::WN pieces
+        return mine + row * (128 * S::WN) + 16 * ((byte >> 4) ^ swap) + (byte & 15);
+    };
+    auto put = [&](int piece, u32x4 v) { *(u32x4*)at(c, 16 * piece) = v; };
+    auto turned = [&](int j, auto* out, int64_t stride) {
+        typedef std::remove_reference_t<decltype(*out)> E;
+        constexpr int kRowBytes = 32 * S::WN * (int)sizeof(E);
+        const int* to_row = out_row + 32 * (S::WM * wm + j);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (col0 + 32 * S::WN <= a.n && (((uintptr_t)out | (uintptr_t)stride * sizeof(E)) & 15) == 0) {
+#pragma unroll
+            for (int i = 0; i < 32 * kRowBytes / 1024; ++i) {
+                const int p = 16 * (64 * i + lane), row = p / kRowBytes, byte = p % kRowBytes;
+                const u32x4 v = *(const u32x4*)at(row, byte);
+                if (to_row[row] >= 0) *(u32x4*)((uint8_t*)(out + to_row[row] * stride + col0) + byte) = v;
+            }
+        } else {
+            // rows that do not begin at multiples of 16 bytes, or end inside: 64 neighbours one by one (a lane's own eight,
+            // each lane at another line, took 2.9 us longer for 333 x 5003)
+#pragma unroll 4
+            for (int i = 0; i < 16 * S::WN; ++i) {
+                const int p = 64 * i + lane, row = p / (32 * S::WN), col = p % (32 * S::WN);
+                const E v = *(const E*)at(row, col * (int)sizeof(E));
+                if (to_row[row] >= 0 && col0 + col < a.n) out[to_row[row] * stride + col0 + col] = v;
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
+#pragma unroll
+    for (int j = 0; j < S::WM; ++j) {
+        const bool whole = !EXPERTS && a.part, single = EXPERTS && a.products;
+        const float xs = x_scale[32 * (S::WM * wm + j) + c];
+#pragma unroll
+        for (int i = 0; i < S::WN; ++i) {
+            float y[16];
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const int o = 32 * (S::WN * wn + i) + 16 * half + e;
+                const f32x4 sc = *(const f32x4*)(w_scale + o), bi = *(const f32x4*)(bias + o);
+#pragma unroll
+                for (int f = 0; f < 4; ++f) y[e + f] = finish(acc[i][j][e + f], xs, sc[f], bi[f]);
+            }
+            if (whole) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    put(8 * i + 4 * half + e, u32x4{(uint32_t)acc[i][j][4 * e], (uint32_t)acc[i][j][4 * e + 1], (uint32_t)acc[i][j][4 * e + 2], (uint32_t)acc[i][j][4 * e + 3]});
+            } else if (single) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    put(8 * i + 4 * half + e, __builtin_bit_cast(u32x4, f32x4{y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]}));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    u32x4 v;
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) v[f] = __builtin_bit_cast(uint32_t, T2{(T)y[8 * e + 2 * f], (T)y[8 * e + 2 * f + 1]});
+                    put(4 * i + 2 * half + e, v);
+                }
+            }
+        }
+        if (whole)
+            turned(j, a.part + (int64_t)blockIdx.y * a.m * a.n, (int64_t)a.n);
+        else if (single)
+            turned(j, a.products, (int64_t)a.n);
+        else
+            turned(j, (T*)a.y, a.y_stride);
+    }
+}
+
+// The tiles that calls are cut into (outputs x rows of a workgroup), largest first, and rows alone (w8_rows.h).
+typedef Tile<4, 2, 2, 4, 1, 128, 2> Tile256x256;
+typedef Tile<2, 2, 4, 2, 1, 128, 2> Tile256x128;
+typedef Tile<2, 1, 2, 4, 1, 128, 4> Tile128x128;
+typedef Tile<1, 1, 2, 4, 1, 128, 4> Tile64x128;
+typedef Tile<1, 1, 2, 2, 1, 128, 4> Tile64x64;
+typedef Tile<1, 1, 1, 1, 4, 256, 4> Tile32x32;
+enum Kernel { kTile256x256, kTile256x128, kTile128x128, kTile64x128, kTile64x64, kTile32x32, kRows16, kRows32, kKernels };
+
+// Whether rows that far apart need the kernel for that, Tile64x128 with FAR.
+inline bool far(int64_t rows, int64_t stride, int64_t k) { return (rows - 1) * stride + k > (int64_t)0xffffffff; }
+
+// What a kernel takes (us): `start` beside the loop, `step` for 1024 of k, `step` times 1 + `full` with a workgroup on each
+// of the 256 compute units (rows: with 16 rows), and `pair` times that for two workgroups each.  Fitted to 510 calls of 1 to
+// 8192 rows, 64 to 32768 outputs and k of 128 to 16384, off by 8 to 19% (root mean square).
+struct Form {
+    int outs, rows;
+    double start, step, pair, full;
+};
+constexpr Form kForms[kKernels] = {
+    {256, 256, 11.1, 7.9, 2.45, 0.43}, {256, 128, 6.6, 5.15, 2.17, 0.71}, {128, 128, 3.8, 2.6, 2.5, 0.42},
+    {64, 128, 2.5, 1.7, 2.2, 0.53},    {64, 64, 2.3, 1.24, 1.44, 0.65},   {32, 32, 2.4, 0.42, 1.2, 1.1},
+    {16, 16, 0.56, 0.40, 1.92, 1.32},  {32, 16, 0.46, 0.83, 1.76, 1.0},
+};
+// The time of a kernel that has so many tiles, for k of a part and so many bytes of weights.
+inline double estimate(Kernel kernel, int64_t tiles, int64_t k, int64_t bytes, int64_t m) {
+    const Form& f = kForms[kernel];
+    const int64_t rest = tiles % 512;
+    const double rounds = f.pair * (double)(tiles / 512) + (rest == 0 ? 0 : (rest <= 256 ? 1 : f.pair));
+    const double fill = kernel >= kRows16 ? (double)m / 16 : (tiles < 256 ? (double)tiles / 256 : 1);
+    const double t = (f.start + f.step * (1 + f.full * fill) * (double)k / 1024) * rounds, memory = (double)bytes / 5.2e6;
+    return t > memory ? t : memory;
 }
 
 }  // namespace w8
