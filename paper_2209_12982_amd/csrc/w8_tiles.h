@@ -35,28 +35,45 @@ __device__ inline void copy16_from(const void* from, uint32_t dst) {
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(dst) : "memory");
 }
 
-// The tile of the experts' rows that is the index-th: its expert, and where its rows begin and end in the order.
-template <int ROWS> __device__ inline bool find(const Args& a, int index, int& expert, int& begin, int& end) {
+// The experts' tile that a workgroup takes, or false where it has none: its expert, where its rows begin and end in the
+// order, and which of n_tiles outputs.  An expert's tiles stand together, those of the same outputs next to each other, and
+// each XCD takes a piece of that list (workgroup i runs on XCD i % 8): weights stay in its L2 for all rows that need them.
+template <int ROWS> __device__ inline bool find(const Args& a, int n_tiles, int& expert, int& begin, int& end, int& n_tile) {
     const int lane = threadIdx.x & 63;
-    for (int e0 = 0; e0 < a.experts; e0 += 64) {
-        int b = 0, e = 0;
+    // the tiles of rows of 64 experts: where their rows are, how many, and how many up to each lane
+    int b, e, count, upto;
+    auto set = [&](int e0) {
+        b = 0, e = 0;
         if (e0 + lane < a.experts) rows_of(a, e0 + lane, b, e);
-        const int count = (e - b + ROWS - 1) / ROWS;
-        int upto = count;
+        count = (e - b + ROWS - 1) / ROWS;
+        upto = count;
 #pragma unroll
         for (int s = 1; s < 64; s <<= 1) {
             const int other = __shfl_up(upto, s);
             if (lane >= s) upto += other;
         }
-        const uint64_t here = __ballot(index < upto);
+    };
+    int all = 0;
+    for (int e0 = 0; e0 < a.experts; e0 += 64) {
+        set(e0);
+        all += __builtin_amdgcn_readlane(upto, 63);
+    }
+    const int each = (all * n_tiles + 7) / 8, index = (int)(blockIdx.x % 8) * each + (int)(blockIdx.x / 8);
+    if ((int)(blockIdx.x / 8) >= each || index >= all * n_tiles) return false;
+    int before = 0;
+    for (int e0 = 0; e0 < a.experts; e0 += 64) {
+        if (a.experts > 64) set(e0);
+        const uint64_t here = __ballot(index < (before + upto) * n_tiles);
         if (here) {
             const int l = __builtin_ctzll(here);
+            const int tiles = __builtin_amdgcn_readlane(count, l), in = index - (before + __builtin_amdgcn_readlane(upto, l) - tiles) * n_tiles;
             expert = e0 + l;
-            begin = __shfl(b, l) + (index - (__shfl(upto, l) - __shfl(count, l))) * ROWS;
-            end = __shfl(e, l);
+            begin = __builtin_amdgcn_readlane(b, l) + in % tiles * ROWS;
+            end = __builtin_amdgcn_readlane(e, l);
+            n_tile = in / tiles;
             return true;
         }
-        index -= __shfl(upto, 63);
+        before += __builtin_amdgcn_readlane(upto, 63);
     }
     return false;
 }
@@ -74,11 +91,8 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
 
     int m0, m1, n0, expert = 0;
     if (EXPERTS) {
-        n0 = (int)(blockIdx.x % n_tiles) * S::kOuts;
-        if (!find<S::kRows>(a, blockIdx.x / n_tiles, expert, m0, m1)) return;
-        expert = __builtin_amdgcn_readfirstlane(expert);
-        m0 = __builtin_amdgcn_readfirstlane(m0);
-        m1 = __builtin_amdgcn_readfirstlane(m1);
+        if (!find<S::kRows>(a, n_tiles, expert, m0, m1, n0)) return;
+        n0 *= S::kOuts;
     } else {
         // workgroup i runs on XCD i % 8: each gets neighbouring tiles, eight rows of them at a time
         const int tiles = n_tiles * m_tiles, each = (tiles + 7) / 8;
@@ -180,6 +194,7 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
 #pragma unroll
         for (int j = 0; j < S::WM; ++j) x[to][j] = *(const i32x4*)(lx + j * (32 * S::BK) + at);
     };
+    const bool busy = m0 + 32 * S::WM * wm < m1 && n0 + 32 * S::WN * wn < a.n;      // else the wave only copies
     auto multiply = [&](int from, int i) {
 #pragma unroll
         for (int j = 0; j < S::WM; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[from][i], x[from][j], acc[i][j], 0, 0, 0);
@@ -192,6 +207,7 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
         const int after = buf + 1 == S::STAGES ? 0 : buf + 1;
 #pragma unroll
         for (int t = 0; t < kSteps - 1; ++t) {
+            if (!busy) break;
             read(buf, t + 1, (t + 1) & 1);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -201,12 +217,12 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
         if constexpr (LATER >= 0) {
             WINO_WAIT_VM_LDS(LATER * kPieces);
             winof4::ring_barrier();
-            read(after, 0, kSteps & 1);
+            if (busy) read(after, 0, kSteps & 1);
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < S::WN; ++i) {
-            multiply((kSteps - 1) & 1, i);
+            if (busy) multiply((kSteps - 1) & 1, i);
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (FILL != 0) {
 #pragma unroll
@@ -363,7 +379,7 @@ inline double estimate(Kernel kernel, int64_t tiles, int64_t k, int64_t bytes, i
     const double rounds = f.pair * (double)(tiles / 512) + (rest == 0 ? 0 : (rest <= 256 ? 1 : f.pair));
     const double fill = kernel >= kRows16 ? (double)m / 16 : (tiles < 256 ? (double)tiles / 256 : 1);
     const double t = (f.start + f.step * (1 + f.full * fill) * (double)k / 1024) * rounds, memory = (double)bytes / 5.2e6;
-    return t > memory ? t : memory;
+    return t > memory ? t + 0.05 * memory : memory + 0.05 * t;      // what is less decides between equal ones
 }
 
 }  // namespace w8
