@@ -743,7 +743,8 @@ typedef enum wino_score { WINO_SCORE_SOFTMAX = 0, WINO_SCORE_SIGMOID = 1 } wino_
  *   experts <= 1024 (a multiple of groups), groups <= 64, top <= 32 and at most
  *   the experts of top_groups groups, tokens * top <= 2^22.
  *   workspace  route_experts_workspace_bytes(tokens, experts, top) bytes or
- *            more, 16-byte aligned, scratch: needed with order.
+ *            more, 16-byte aligned, scratch: needed with order where that is
+ *            more than 0 (it is 0 for few tokens).
  */
 size_t route_experts_workspace_bytes(int32_t tokens, int32_t experts, int32_t top);
 wino_status route_experts(const void* logits, int64_t stride, const float* bias, int32_t tokens, int32_t experts, int32_t top,

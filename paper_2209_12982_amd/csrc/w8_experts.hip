@@ -8,19 +8,24 @@
 namespace {
 using namespace w8;
 
-// out[t] = sum_j weights[t][j] products[t top + j], in the order of j; routes without an expert add nothing.
-template <int TYPE>
+// out[t] = sum_j weights[t][j] products[t top + j], in the order of j; routes without an expert add nothing.  Memory bounds
+// it; COLS columns a thread, four where rows of products begin at multiples of 16 bytes.
+template <int TYPE, int COLS>
 __global__ __launch_bounds__(256) void w8_combine_kernel(Args a, const int32_t* chosen, const float* weights, int top) {
     typedef typename Half<TYPE>::type T;
-    const int col = blockIdx.y * 256 + threadIdx.x;
+    typedef __attribute__((ext_vector_type(COLS))) float Row;
+    const int col = ((int)blockIdx.y * 256 + (int)threadIdx.x) * COLS;
     const int64_t token = blockIdx.x;
     if (col >= a.n) return;
-    float sum = 0.f;
+    Row sum = {};
+#pragma unroll 4
     for (int j = 0; j < top; ++j) {
         const int64_t route = token * top + j;
-        if ((uint32_t)chosen[route] < (uint32_t)a.experts) sum += weights[route] * a.products[route * a.n + col];
+        if ((uint32_t)chosen[route] < (uint32_t)a.experts) sum += weights[route] * *(const Row*)(a.products + route * a.n + col);
     }
-    ((T*)a.y)[token * a.y_stride + col] = (T)sum;
+    T* to = (T*)a.y + token * a.y_stride + col;
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) to[e] = (T)sum[e];
 }
 
 template <int TYPE, int NT, int V> void launch_rows(const Args& a, hipStream_t stream) {
@@ -70,6 +75,15 @@ template <int TYPE> void pick(const Args& a, int64_t x_rows, hipStream_t stream)
     }
 }
 
+template <int TYPE> void combine(const Args& a, const int32_t* chosen, const float* weights, int top, hipStream_t stream) {
+    const int cols = a.n % 4 == 0 ? 4 : 1;
+    const dim3 grid((unsigned)(a.routes / top), (unsigned)((a.n + 256 * cols - 1) / (256 * cols)));
+    if (cols == 4)
+        hipLaunchKernelGGL((w8_combine_kernel<TYPE, 4>), grid, dim3(256), 0, stream, a, chosen, weights, top);
+    else
+        hipLaunchKernelGGL((w8_combine_kernel<TYPE, 1>), grid, dim3(256), 0, stream, a, chosen, weights, top);
+}
+
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
 
@@ -110,11 +124,7 @@ extern "C" wino_status w8_experts_matmul(const int8_t* x, int64_t x_stride, cons
     }
     type == WINO_BF16 ? pick<WINO_BF16>(a, x_rows, stream) : pick<WINO_FP16>(a, x_rows, stream);
     if (weights && hipGetLastError() == hipSuccess) {
-        const dim3 grid((unsigned)y_rows, (unsigned)((n + 255) / 256));
-        if (type == WINO_BF16)
-            hipLaunchKernelGGL((w8_combine_kernel<WINO_BF16>), grid, dim3(256), 0, stream, a, chosen, weights, top);
-        else
-            hipLaunchKernelGGL((w8_combine_kernel<WINO_FP16>), grid, dim3(256), 0, stream, a, chosen, weights, top);
+        type == WINO_BF16 ? combine<WINO_BF16>(a, chosen, weights, top, stream) : combine<WINO_FP16>(a, chosen, weights, top, stream);
     }
     return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
 }

@@ -73,7 +73,8 @@ def test_route(t, e, top, score, name):
 @pytest.mark.parametrize("score", [W.SCORE_SOFTMAX, W.SCORE_SIGMOID])
 @pytest.mark.parametrize("t,groups,size,top_groups,best,top", [(50, 8, 32, 4, 2, 8), (20, 2, 2, 1, 2, 2), (9, 64, 2, 5, 2, 7),
                                                                (17, 8, 60, 3, 1, 8), (13, 3, 7, 2, 2, 14), (5, 64, 16, 63, 1, 32),
-                                                               (30, 16, 5, 1, 1, 5), (11, 4, 1, 2, 1, 2), (8, 4, 4, 4, 2, 6)])
+                                                               (30, 16, 5, 1, 1, 5), (11, 4, 1, 2, 1, 2), (8, 4, 4, 4, 2, 6),
+                                                               (130, 16, 64, 7, 2, 32), (64, 5, 100, 2, 2, 16), (65, 3, 33, 1, 1, 33 - 1)])
 def test_groups_and_bias(t, groups, size, top_groups, best, top, score):
     torch = torch_dev()
     rng = np.random.default_rng(t + groups * size)
@@ -200,7 +201,9 @@ def test_refused():
     for kw in (dict(groups=3), dict(score=2), dict(groups=8, top_groups=1), dict(scale=float("nan"))):
         with pytest.raises(W.WinoError):
             W.route_experts(logits, chosen, w, order, ends, workspace=room, **kw)
+    many = torch.zeros((65, 8), device="cuda")                  # more than one block: the order needs room
     with pytest.raises(W.WinoError):
-        W.route_experts(logits, chosen, w, order, ends)
+        W.route_experts(many, torch.zeros((65, 2), dtype=torch.int32, device="cuda"), torch.zeros((65, 2), device="cuda"),
+                        torch.zeros(130, dtype=torch.int32, device="cuda"), ends)
     with pytest.raises(ValueError):
         W.route_experts(logits, chosen, w, bias=logits[0].half())
