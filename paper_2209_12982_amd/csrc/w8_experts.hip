@@ -36,7 +36,7 @@ template <int TYPE, class S, bool FAR = false> void launch_tiles(const Args& a, 
     const int n_tiles = (a.n + S::kOuts - 1) / S::kOuts;
     // whole tiles of the rows, and one more for each expert's last
     const int m_tiles = a.routes / S::kRows + std::min(a.experts, a.routes);
-    const dim3 grid((unsigned)(((int64_t)n_tiles * m_tiles + 7) / 8 * 8));
+    const dim3 grid(workgroups<S>((int64_t)n_tiles * m_tiles));
     hipLaunchKernelGGL((w8_tiles_kernel<TYPE, S, true, FAR>), grid, dim3(S::kThreads), 0, stream, a, n_tiles, m_tiles);
 }
 

@@ -21,6 +21,11 @@ template <int WN_, int WM_, int GN_, int GM_, int GK_, int BK_, int STAGES_> str
     static constexpr int kRowPieces = BK / 16;
     static constexpr int kPiecesW = kOuts * kRowPieces / kThreads, kPiecesX = kRows * kRowPieces / kThreads;    // of a thread
     static constexpr int kBytesW = kOuts * BK, kBytes = kBytesW + kRows * BK;
+    // The largest tiles leave a compute unit room for one workgroup: it takes tile after tile, and the next one's first stage
+    // is on its way while results are stored.
+    static constexpr bool kLoop = kOuts * kRows >= 65536;
+    static_assert(WN == 1 || WN == 2 || WN == 4, "rows of results are turned in whole sets of banks");
+    static_assert(!kLoop || (STAGES == 2 && GK == 1), "results are turned in the second stage");
     static_assert(kOuts * kRowPieces % kThreads == 0 && kRows * kRowPieces % kThreads == 0, "whole copies");
     static __device__ int swap(int row) { return BK >= 256 ? row & 15 : (BK == 128 ? (row >> 1) & 7 : (row >> 2) & 3); }
 };
@@ -31,14 +36,27 @@ template <int WN_, int WM_, int GN_, int GM_, int GK_, int BK_, int STAGES_> str
 __device__ inline void copy16(const void* base, uint32_t off, uint32_t dst) {
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(dst) : "memory");
 }
+// An address that all lanes have alike, in scalar registers.
+__device__ inline const int8_t* uniform(const int8_t* p) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)p), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)p >> 32));
+    return (const int8_t*)((uintptr_t)hi << 32 | lo);
+}
 __device__ inline void copy16_from(const void* from, uint32_t dst) {
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(dst) : "memory");
 }
 
+// The same value, which the compiler does not know to be so: what follows from it is worked out here, not kept in registers
+// over the whole kernel.
+__device__ inline int anew(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // The experts' tile that a workgroup takes, or false where it has none: its expert, where its rows begin and end in the
 // order, and which of n_tiles outputs.  An expert's tiles stand together, those of the same outputs next to each other, and
-// each XCD takes a piece of that list (workgroup i runs on XCD i % 8): weights stay in its L2 for all rows that need them.
-template <int ROWS> __device__ inline bool find(const Args& a, int n_tiles, int& expert, int& begin, int& end, int& n_tile) {
+// each XCD takes a piece of that list (workgroup i runs on XCD i % 8), `own` counts in it: weights stay in its L2 for all rows
+// that need them.
+template <int ROWS> __device__ inline bool find(const Args& a, int n_tiles, int own, int& expert, int& begin, int& end, int& n_tile) {
     const int lane = threadIdx.x & 63;
     // the tiles of rows of 64 experts: where their rows are, how many, and how many up to each lane
     int b, e, count, upto;
@@ -58,8 +76,8 @@ template <int ROWS> __device__ inline bool find(const Args& a, int n_tiles, int&
         set(e0);
         all += __builtin_amdgcn_readlane(upto, 63);
     }
-    const int each = (all * n_tiles + 7) / 8, index = (int)(blockIdx.x % 8) * each + (int)(blockIdx.x / 8);
-    if ((int)(blockIdx.x / 8) >= each || index >= all * n_tiles) return false;
+    const int each = (all * n_tiles + 7) / 8, index = (int)(blockIdx.x % 8) * each + own;
+    if (own >= each || index >= all * n_tiles) return false;
     int before = 0;
     for (int e0 = 0; e0 < a.experts; e0 += 64) {
         if (a.experts > 64) set(e0);
@@ -82,64 +100,81 @@ template <int ROWS> __device__ inline bool find(const Args& a, int n_tiles, int&
 template <int TYPE, class S, bool EXPERTS, bool FAR = false>
 __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_tiles, int m_tiles) {
     typedef typename Half<TYPE>::type T;
-    typedef __attribute__((ext_vector_type(2))) T T2;
+    typedef __attribute__((ext_vector_type(8))) T T8;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[S::STAGES][S::kBytes];
-    __shared__ __attribute__((aligned(16))) float w_scale[S::kOuts], bias[S::kOuts], x_scale[S::kRows];
-    __shared__ int out_row[S::kRows];
+    constexpr int kSets = S::kLoop ? 2 : 1;
+    __shared__ __attribute__((aligned(16))) float w_scale[kSets][S::kOuts], bias[kSets][S::kOuts], x_scale[kSets][S::kRows];
+    __shared__ int out_row[kSets][S::kRows];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 31, half = lane >> 5;
 
-    int m0, m1, n0, expert = 0;
-    if (EXPERTS) {
-        if (!find<S::kRows>(a, n_tiles, expert, m0, m1, n0)) return;
-        n0 *= S::kOuts;
-    } else {
-        // workgroup i runs on XCD i % 8: each gets neighbouring tiles, eight rows of them at a time
-        const int tiles = n_tiles * m_tiles, each = (tiles + 7) / 8;
-        const int t = (int)(blockIdx.x % 8) * each + (int)(blockIdx.x / 8);
-        if ((int)(blockIdx.x / 8) >= each || t >= tiles) return;
-        const int set = 8 * n_tiles, g = t / set, high = min(8, m_tiles - 8 * g), in = t - g * set;
-        m0 = (8 * g + in % high) * S::kRows;
-        n0 = in / high * S::kOuts;
-        m1 = a.m;
-    }
+    struct Where {
+        int m0, m1, n0, expert;                             // rows (experts: places in the order), outputs
+    };
+    auto where = [&](int turn, Where& t) {
+        const int own = (int)(blockIdx.x / 8) + turn * (int)(gridDim.x / 8);
+        t.expert = 0;
+        if constexpr (EXPERTS) {
+            int n_tile;
+            if (!find<S::kRows>(a, n_tiles, own, t.expert, t.m0, t.m1, n_tile)) return false;
+            t.n0 = n_tile * S::kOuts;
+        } else {
+            // workgroup i runs on XCD i % 8: each gets neighbouring tiles, eight rows of them at a time
+            const int tiles = n_tiles * m_tiles, each = (tiles + 7) / 8, index = (int)(blockIdx.x % 8) * each + own;
+            if (own >= each || index >= tiles) return false;
+            const int set = 8 * n_tiles, g = index / set, high = min(8, m_tiles - 8 * g), in = index - g * set;
+            t.m0 = (8 * g + in % high) * S::kRows;
+            t.n0 = in / high * S::kOuts;
+            t.m1 = a.m;
+        }
+        return true;
+    };
     const int all = (a.k + S::BK - 1) / S::BK;
     const int first = EXPERTS ? 0 : (int)blockIdx.y * a.steps, last = EXPERTS ? all : min(first + a.steps, all);
+    Where t;
+    if (!where(0, t)) return;
 
-    for (int o = threadIdx.x; o < S::kOuts; o += S::kThreads) {
-        const int col = min(n0 + o, a.n - 1);
-        w_scale[o] = a.w_scales[(int64_t)expert * a.n + col];
-        bias[o] = !EXPERTS && a.bias ? (float)((const T*)a.bias)[col] : 0.f;
-    }
-    for (int o = threadIdx.x; o < S::kRows; o += S::kThreads) {
-        const int at = min(m0 + o, m1 - 1), route = EXPERTS ? a.order[at] : at;
-        x_scale[o] = a.x_scales[EXPERTS ? x_row(a, route) : route];
-        out_row[o] = m0 + o < m1 && (!EXPERTS || (uint32_t)route < (uint32_t)a.routes) ? route : -1;
-    }
+    auto load_scales = [&](const Where& t, int set) {
+        for (int o = threadIdx.x; o < S::kOuts; o += S::kThreads) {
+            const int col = min(t.n0 + o, a.n - 1);
+            w_scale[set][o] = a.w_scales[(int64_t)t.expert * a.n + col];
+            bias[set][o] = !EXPERTS && a.bias ? (float)((const T*)a.bias)[col] : 0.f;
+        }
+        for (int o = threadIdx.x; o < S::kRows; o += S::kThreads) {
+            const int at = min(t.m0 + o, t.m1 - 1), route = EXPERTS ? a.order[at] : at;
+            x_scale[set][o] = a.x_scales[EXPERTS ? x_row(a, route) : route];
+            out_row[set][o] = t.m0 + o < t.m1 && (!EXPERTS || (uint32_t)route < (uint32_t)a.routes) ? route : -1;
+        }
+    };
 
     // pieces that this thread copies: where they come from, relative to the tile's weights and to x
     uint32_t from_w[S::kPiecesW], from_x[S::kPiecesX];
+    int lane_s = lane;
     auto place = [&](int p, int& row, int& piece) {
         row = p / S::kRowPieces;
         piece = (p % S::kRowPieces) ^ S::swap(row);
     };
+    const int8_t *w_base, *x_base;
+    auto prepare = [&](const Where& t) {
+        const int lane = anew(threadIdx.x & 63);
 #pragma unroll
-    for (int i = 0; i < S::kPiecesW; ++i) {
-        int row, piece;
-        place((i * S::kWaves + wave) * 64 + lane, row, piece);
-        const int w_row = (row & ~31) | (row >> 2 & 1) << 4 | (row >> 3 & 3) << 2 | (row & 3);
-        from_w[i] = (uint32_t)(min(n0 + w_row, a.n - 1) - n0) * (uint32_t)a.k + 16 * piece;
-    }
+        for (int i = 0; i < S::kPiecesW; ++i) {
+            int row, piece;
+            place((i * S::kWaves + wave) * 64 + lane, row, piece);
+            const int w_row = (row & ~31) | (row >> 2 & 1) << 4 | (row >> 3 & 3) << 2 | (row & 3);
+            from_w[i] = (uint32_t)(min(t.n0 + w_row, a.n - 1) - t.n0) * (uint32_t)a.k + 16 * piece;
+        }
 #pragma unroll
-    for (int i = 0; i < S::kPiecesX; ++i) {
-        int row, piece;
-        place((i * S::kWaves + wave) * 64 + lane, row, piece);
-        const int at = min(m0 + row, m1 - 1);
-        const int64_t row_x = EXPERTS ? x_row(a, a.order[at]) : at - m0;
-        from_x[i] = FAR ? (uint32_t)row_x : (uint32_t)(row_x * a.x_stride) + 16 * piece;
-    }
-    const int8_t* w_base = a.w + ((int64_t)expert * a.n + n0) * a.k;
-    const int8_t* x_base = a.x + (EXPERTS ? 0 : m0 * a.x_stride);
+        for (int i = 0; i < S::kPiecesX; ++i) {
+            int row, piece;
+            place((i * S::kWaves + wave) * 64 + lane, row, piece);
+            const int at = min(t.m0 + row, t.m1 - 1);
+            const int64_t row_x = EXPERTS ? x_row(a, a.order[at]) : at - t.m0;
+            from_x[i] = FAR ? (uint32_t)row_x : (uint32_t)(row_x * a.x_stride) + 16 * piece;
+        }
+        w_base = uniform(a.w + ((int64_t)t.expert * a.n + t.n0) * a.k);
+        x_base = uniform(a.x + (EXPERTS ? 0 : t.m0 * a.x_stride));
+    };
     const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&lds[0][0] + wave * 1024;
     // Piece i of stage s on its way.  cut: the end of k lies inside the stage, what is behind it becomes 0.
     auto copy_piece = [&](int s, int buf, int i, bool cut) {
@@ -175,13 +210,6 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
     };
 
     i32x16 acc[S::WN][S::WM];
-#pragma unroll
-    for (int i = 0; i < S::WN; ++i)
-#pragma unroll
-        for (int j = 0; j < S::WM; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
-
     const int wn = wave % S::GN, wm = wave / S::GN % S::GM, wk = wave / (S::GN * S::GM);
     constexpr int kSteps = S::BK / 32 / S::GK;              // of a wave
     i32x4 w[2][S::WN], x[2][S::WM];                         // operands of a step of 32 of k, and of the next one
@@ -194,12 +222,12 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
 #pragma unroll
         for (int j = 0; j < S::WM; ++j) x[to][j] = *(const i32x4*)(lx + j * (32 * S::BK) + at);
     };
-    const bool busy = m0 + 32 * S::WM * wm < m1 && n0 + 32 * S::WN * wn < a.n;      // else the wave only copies
+    bool busy;                                              // whether the wave has results; else it only copies
     auto multiply = [&](int from, int i) {
 #pragma unroll
         for (int j = 0; j < S::WM; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[from][i], x[from][j], acc[i][j], 0, 0, 0);
     };
-    int buf = 0, s = first;
+    int buf, s;
     // Takes stage s.  Before its last step the next one has to have arrived, for all waves, with no more than `later` stages
     // on their way; all reads of this stage are done by then, so its buffer is filled again (FILL 1; 2: with the end of k).
     auto stage = [&](auto fill, auto later) {
@@ -233,11 +261,21 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
         buf = after;
         ++s;
     };
+    // All stages of a tile, whose first ones are on their way.
+    auto run = [&](const Where& t) {
 #pragma unroll
-    for (int i = 0; i < S::STAGES; ++i)
-        if (first + i < last) copy(first + i, i);
-    if (first < last) {
-        WINO_WAIT_VM_LDS(0);
+        for (int i = 0; i < S::WN; ++i)
+#pragma unroll
+            for (int j = 0; j < S::WM; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+        busy = t.m0 + 32 * S::WM * wm < t.m1 && t.n0 + 32 * S::WN * wn < a.n;
+        buf = 0, s = first;
+        if (first >= last) return;
+        if (last - first >= S::STAGES)
+            WINO_WAIT_VM_LDS((S::STAGES - 1) * kPieces);
+        else
+            WINO_WAIT_VM_LDS(0);
         winof4::ring_barrier();
         read(0, 0, 0);
         const int whole = min(last, a.k / S::BK);           // stages without the end of k
@@ -245,53 +283,41 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
         if (s + S::STAGES < last) stage(Int<2>(), Int<S::STAGES - 2>());
         while (s + 1 < last) stage(Int<0>(), Int<0>());
         stage(Int<0>(), Int<-1>());
-    }
-    __syncthreads();                                        // nobody reads a stage any more
-
-    if constexpr (S::GK > 1) {                              // the parts of k meet
-        typedef __attribute__((ext_vector_type(4))) int Sum;
-        constexpr int kSums = S::WN * S::WM * 4;            // pieces of 16 bytes a lane
-        static_assert((S::GK - 1) * S::GN * S::GM * kSums * 1024 <= S::STAGES * S::kBytes, "room for the parts");
-        uint8_t* parts = &lds[0][0] + 16 * lane;
-        if (wk > 0) {
-#pragma unroll
-            for (int p = 0; p < kSums; ++p) {
-                const i32x16& z = acc[p / 4 / S::WM][p / 4 % S::WM];
-                *(Sum*)(parts + ((wave - S::GN * S::GM) * kSums + p) * 1024) = Sum{z[p % 4 * 4], z[p % 4 * 4 + 1], z[p % 4 * 4 + 2], z[p % 4 * 4 + 3]};
-            }
-        }
-        __syncthreads();
-        if (wk > 0) return;
-#pragma unroll
-        for (int k = 0; k < S::GK - 1; ++k)
-#pragma unroll
-            for (int p = 0; p < kSums; ++p) {
-                const Sum v = *(const Sum*)(parts + ((wave + k * S::GN * S::GM) * kSums + p) * 1024);
-                i32x16& z = acc[p / 4 / S::WM][p / 4 % S::WM];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) z[p % 4 * 4 + e] += v[e];
-            }
-    }
-
-    // 32 rows at a time, each wave turns its own results in LDS, so that sixteen lanes store 256 neighbouring bytes.  The
-    // 16-byte pieces of a row are exchanged by the row's number: both ways sixteen lanes meet sixteen columns of the banks.
-    uint8_t* mine = &lds[0][0] + (S::GK > 1 ? (S::GK - 1) * S::GN * S::GM * S::WN * S::WM * 4096 : 0) + wave * (S::WN * 4096);
-    static_assert((S::GK > 1 ? (S::GK - 1) * S::GN * S::GM * S::WN * S::WM * 4096 : 0) + S::GN * S::GM * S::WN * 4096 <= S::STAGES * S::kBytes, "room to turn");
-    const int col0 = n0 + 32 * S::WN * wn;
-    auto at = [&](int row, int byte) {
-        const int swap = S::WN == 1 ? (row >> 1) & 7 : row & 15;    // a row has 8 S::WN pieces
-        return mine + row * (128 * S::WN) + 16 * ((byte >> 4) ^ swap) + (byte & 15);
     };
-    auto put = [&](int piece, u32x4 v) { *(u32x4*)at(c, 16 * piece) = v; };
-    auto turned = [&](int j, auto* out, int64_t stride) {
+    // All waves have done what they do in LDS; copies and stores stay on their way.
+    auto meet = [&]() {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        winof4::ring_barrier();
+    };
+
+    // 32 rows at a time, each wave turns its own results in LDS, so that neighbouring lanes store neighbouring bytes: up to 256
+    // of a row.  The 16-byte pieces of a row are exchanged by the row's number: both ways sixteen lanes meet sixteen columns of
+    // the banks.
+    constexpr int kParts = S::GK > 1 ? (S::GK - 1) * S::GN * S::GM * S::WN * S::WM * 4096 : 0;
+    constexpr int kTurn = 32 * (S::WN == 1 ? 128 : 256);    // bytes of a wave
+    static_assert((S::kLoop ? S::kBytes : kParts) + S::GN * S::GM * kTurn <= S::STAGES * S::kBytes, "room to turn");
+    uint8_t* mine = &lds[0][0] + (S::kLoop ? S::kBytes : kParts) + wave * kTurn;
+    // Stores rows of BLOCKS times 32 results of type E; put(block, piece) gives the 16-byte pieces of this lane's half of them.
+    auto turned = [&](const Where& t, int set, int j, int i0, auto blocks, auto* out, int64_t stride, auto put) {
         typedef std::remove_reference_t<decltype(*out)> E;
-        constexpr int kRowBytes = 32 * S::WN * (int)sizeof(E);
-        const int* to_row = out_row + 32 * (S::WM * wm + j);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (col0 + 32 * S::WN <= a.n && (((uintptr_t)out | (uintptr_t)stride * sizeof(E)) & 15) == 0) {
+        const int lane = lane_s, c = lane & 31, half = lane >> 5;
+        constexpr int BLOCKS = decltype(blocks)::value, kBlock = 32 * (int)sizeof(E), kRow = BLOCKS * kBlock;
+        static_assert(32 * kRow <= kTurn, "room");
+        auto at = [&](int row, int byte) {
+            const int swap = kRow == 256 ? row & 15 : (kRow == 128 ? (row >> 1) & 7 : (row >> 2) & 3);
+            return mine + row * kRow + 16 * ((byte >> 4) ^ swap) + (byte & 15);
+        };
 #pragma unroll
-            for (int i = 0; i < 32 * kRowBytes / 1024; ++i) {
-                const int p = 16 * (64 * i + lane), row = p / kRowBytes, byte = p % kRowBytes;
+        for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+            for (int p = 0; p < kBlock / 32; ++p) *(u32x4*)at(c, i * kBlock + half * (kBlock / 2) + 16 * p) = put(i0 + i, p);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int* to_row = out_row[set] + 32 * (S::WM * wm + j);
+        const int col0 = t.n0 + 32 * (S::WN * wn + i0);
+        if (col0 + 32 * BLOCKS <= a.n && (((uintptr_t)out | (uintptr_t)stride * sizeof(E)) & 15) == 0) {
+#pragma unroll
+            for (int i = 0; i < 32 * kRow / 1024; ++i) {
+                const int p = 16 * (64 * i + lane), row = p / kRow, byte = p % kRow;
                 const u32x4 v = *(const u32x4*)at(row, byte);
                 if (to_row[row] >= 0) *(u32x4*)((uint8_t*)(out + to_row[row] * stride + col0) + byte) = v;
             }
@@ -299,52 +325,97 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
             // rows that do not begin at multiples of 16 bytes, or end inside: 64 neighbours one by one (a lane's own eight,
             // each lane at another line, took 2.9 us longer for 333 x 5003)
 #pragma unroll 4
-            for (int i = 0; i < 16 * S::WN; ++i) {
-                const int p = 64 * i + lane, row = p / (32 * S::WN), col = p % (32 * S::WN);
+            for (int i = 0; i < 16 * BLOCKS; ++i) {
+                const int p = 64 * i + lane, row = p / (32 * BLOCKS), col = p % (32 * BLOCKS);
                 const E v = *(const E*)at(row, col * (int)sizeof(E));
                 if (to_row[row] >= 0 && col0 + col < a.n) out[to_row[row] * stride + col0 + col] = v;
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     };
+    auto store = [&](const Where& t, int set) {
+        lane_s = anew(threadIdx.x & 63);
 #pragma unroll
-    for (int j = 0; j < S::WM; ++j) {
-        const bool whole = !EXPERTS && a.part, single = EXPERTS && a.products;
-        const float xs = x_scale[32 * (S::WM * wm + j) + c];
-#pragma unroll
-        for (int i = 0; i < S::WN; ++i) {
-            float y[16];
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
+        for (int j = 0; j < S::WM; ++j) {
+            const int c = lane_s & 31, half = lane_s >> 5;
+            const float xs = x_scale[set][32 * (S::WM * wm + j) + c];
+            auto results = [&](int i, int e, float (&y)[4]) {       // four neighbouring ones of block i
                 const int o = 32 * (S::WN * wn + i) + 16 * half + e;
-                const f32x4 sc = *(const f32x4*)(w_scale + o), bi = *(const f32x4*)(bias + o);
+                const f32x4 sc = *(const f32x4*)(w_scale[set] + o), bi = *(const f32x4*)(bias[set] + o);
 #pragma unroll
-                for (int f = 0; f < 4; ++f) y[e + f] = finish(acc[i][j][e + f], xs, sc[f], bi[f]);
-            }
-            if (whole) {
+                for (int f = 0; f < 4; ++f) y[f] = finish(acc[i][j][e + f], xs, sc[f], bi[f]);
+            };
+            auto wide = [&](auto* out, int64_t stride, auto put) {  // 4 bytes each, 256 of a row at a time
+                constexpr int kBlocks = S::WN < 2 ? S::WN : 2;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    put(8 * i + 4 * half + e, u32x4{(uint32_t)acc[i][j][4 * e], (uint32_t)acc[i][j][4 * e + 1], (uint32_t)acc[i][j][4 * e + 2], (uint32_t)acc[i][j][4 * e + 3]});
-            } else if (single) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    put(8 * i + 4 * half + e, __builtin_bit_cast(u32x4, f32x4{y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]}));
+                for (int i = 0; i < S::WN; i += kBlocks) turned(t, set, j, i, Int<kBlocks>(), out, stride, put);
+            };
+            if (!EXPERTS && a.part) {
+                wide(a.part + (int64_t)blockIdx.y * a.m * a.n, (int64_t)a.n, [&](int i, int p) {
+                    const i32x16& z = acc[i][j];
+                    return u32x4{(uint32_t)z[4 * p], (uint32_t)z[4 * p + 1], (uint32_t)z[4 * p + 2], (uint32_t)z[4 * p + 3]};
+                });
+            } else if (EXPERTS && a.products) {
+                wide(a.products, (int64_t)a.n, [&](int i, int p) {
+                    float y[4];
+                    results(i, 4 * p, y);
+                    return __builtin_bit_cast(u32x4, f32x4{y[0], y[1], y[2], y[3]});
+                });
             } else {
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    u32x4 v;
-#pragma unroll
-                    for (int f = 0; f < 4; ++f) v[f] = __builtin_bit_cast(uint32_t, T2{(T)y[8 * e + 2 * f], (T)y[8 * e + 2 * f + 1]});
-                    put(4 * i + 2 * half + e, v);
-                }
+                turned(t, set, j, 0, Int<S::WN>(), (T*)a.y, a.y_stride, [&](int i, int p) {
+                    float y[4], z[4];
+                    results(i, 8 * p, y);
+                    results(i, 8 * p + 4, z);
+                    return __builtin_bit_cast(u32x4, T8{(T)y[0], (T)y[1], (T)y[2], (T)y[3], (T)z[0], (T)z[1], (T)z[2], (T)z[3]});
+                });
             }
         }
-        if (whole)
-            turned(j, a.part + (int64_t)blockIdx.y * a.m * a.n, (int64_t)a.n);
-        else if (single)
-            turned(j, a.products, (int64_t)a.n);
-        else
-            turned(j, (T*)a.y, a.y_stride);
+    };
+
+    prepare(t);
+#pragma unroll
+    for (int i = 0; i < S::STAGES; ++i)
+        if (first + i < last) copy(first + i, i);
+    load_scales(t, 0);
+    for (int turn = 0, set = 0;; ++turn, set ^= 1) {
+        run(t);
+        meet();                                             // nobody reads a stage any more, and the scales are there
+        if constexpr (S::GK > 1) {                              // the parts of k meet
+            typedef __attribute__((ext_vector_type(4))) int Sum;
+            constexpr int kSums = S::WN * S::WM * 4;            // pieces of 16 bytes a lane
+            static_assert((S::GK - 1) * S::GN * S::GM * kSums * 1024 <= S::STAGES * S::kBytes, "room for the parts");
+            uint8_t* parts = &lds[0][0] + 16 * lane;
+            if (wk > 0) {
+#pragma unroll
+                for (int p = 0; p < kSums; ++p) {
+                    const i32x16& z = acc[p / 4 / S::WM][p / 4 % S::WM];
+                    *(Sum*)(parts + ((wave - S::GN * S::GM) * kSums + p) * 1024) = Sum{z[p % 4 * 4], z[p % 4 * 4 + 1], z[p % 4 * 4 + 2], z[p % 4 * 4 + 3]};
+                }
+            }
+            __syncthreads();
+            if (wk > 0) return;
+#pragma unroll
+            for (int k = 0; k < S::GK - 1; ++k)
+#pragma unroll
+                for (int p = 0; p < kSums; ++p) {
+                    const Sum v = *(const Sum*)(parts + ((wave + k * S::GN * S::GM) * kSums + p) * 1024);
+                    i32x16& z = acc[p / 4 / S::WM][p / 4 % S::WM];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[p % 4 * 4 + e] += v[e];
+                }
+        }
+        Where next;
+        const bool more = S::kLoop && where(turn + 1, next);
+        if (more) {
+            prepare(next);
+            if (first < last) copy(first, 0);
+            load_scales(next, set ^ 1);
+        }
+        store(t, set);
+        if (!more) return;
+        meet();                                             // results are turned, the second stage is free
+        if (first + 1 < last) copy(first + 1, 1);
+        t = next;
     }
 }
 
@@ -355,6 +426,12 @@ typedef Tile<2, 1, 2, 4, 1, 128, 4> Tile128x128;
 typedef Tile<1, 1, 2, 4, 1, 128, 4> Tile64x128;
 typedef Tile<1, 1, 2, 2, 1, 128, 4> Tile64x64;
 typedef Tile<1, 1, 1, 1, 4, 256, 4> Tile32x32;
+// Workgroups for so many tiles: as many for each XCD, one for each of 256 compute units where they go on.
+template <class S> inline unsigned workgroups(int64_t tiles) {
+    const int64_t n = (tiles + 7) / 8 * 8;
+    return (unsigned)(S::kLoop && n > 256 ? 256 : n);
+}
+
 enum Kernel { kTile256x256, kTile256x128, kTile128x128, kTile64x128, kTile64x64, kTile32x32, kRows16, kRows32, kKernels };
 
 // Whether rows that far apart need the kernel for that, Tile64x128 with FAR.
