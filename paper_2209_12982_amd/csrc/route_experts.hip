@@ -25,9 +25,10 @@ namespace {
 using namespace mx4;
 
 constexpr int kMostExperts = 1024, kMostTop = 32, kMostGroups = 64;
-constexpr int kTokens = 32;             // of a block
+constexpr int kTokens = 32;             // of a block at most
 constexpr int kAlone = 64;              // that one block takes by itself
 constexpr int kWaveRoutes = 128;        // that a wave places
+constexpr int kFewBlocks = 16;          // whose counts each block adds up by itself: shorter than a launch between
 
 struct RouteArgs {
     const void* logits;
@@ -42,7 +43,7 @@ struct RouteArgs {
     winof4::FastDiv by_size;
     // the order, or null; counts: [experts][blocks], later what comes before a block; totals: [experts]
     int32_t *order, *ends, *counts, *totals;
-    int32_t blocks;
+    int32_t blocks, block_tokens;
 };
 
 template <int TYPE> __device__ inline float load(const void* p, int64_t at) {
@@ -257,13 +258,12 @@ __device__ inline void route(const RouteArgs& a, const float (&z)[J], const floa
 }
 
 // Places the routes of a block in the order: WAVES waves with kWaveRoutes each.  next: [WAVES][experts], scan: [WAVES].
-// first(e): where a block's routes of expert e begin, counting from the expert's own beginning; totals come from `total`.
-template <int WAVES, class E, class F, class G>
+// first(e): where a block's routes of expert e begin, counting from the expert's own beginning; total(e): all of them.  EARLY:
+// these are in memory, and asked for together with the routes; else they come from the counts in next.
+template <int WAVES, bool EARLY, class E, class F, class G>
 __device__ inline void place(const RouteArgs& a, int r0, int r1, int32_t* next, int32_t* scan, E expert, F total, G first, bool writes_ends) {
     constexpr int kThreads = 64 * WAVES, kEach = kMostExperts / kThreads;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int e = threadIdx.x; e < WAVES * a.experts; e += kThreads) next[e] = 0;
-    __syncthreads();
     int32_t* own = next + wave * a.experts;
     const int w0 = r0 + wave * kWaveRoutes;
     int mine[kWaveRoutes / 64];
@@ -271,17 +271,28 @@ __device__ inline void place(const RouteArgs& a, int r0, int r1, int32_t* next, 
     for (int i = 0; i < kWaveRoutes / 64; ++i) {
         const int r = w0 + 64 * i + lane;
         mine[i] = r < r1 ? expert(r) : -1;
-        if ((uint32_t)mine[i] < (uint32_t)a.experts) atomicAdd(&own[mine[i]], 1);
     }
-    __syncthreads();
-    // neighbouring experts a thread: where an expert begins
+    // neighbouring experts a thread
     const int e0 = kEach * (int)threadIdx.x;
-    int count[kEach], sum = 0;
+    int count[kEach], from[kEach];
+    auto ask = [&]() {
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-        count[j] = e0 + j < a.experts ? total(e0 + j) : 0;
-        sum += count[j];
-    }
+        for (int j = 0; j < kEach; ++j) {
+            count[j] = e0 + j < a.experts ? total(e0 + j) : 0;
+            from[j] = e0 + j < a.experts ? first(e0 + j) : 0;
+        }
+    };
+    if constexpr (EARLY) ask();
+    for (int e = threadIdx.x; e < WAVES * a.experts; e += kThreads) next[e] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWaveRoutes / 64; ++i)
+        if ((uint32_t)mine[i] < (uint32_t)a.experts) atomicAdd(&own[mine[i]], 1);
+    __syncthreads();
+    if constexpr (!EARLY) ask();
+    int sum = 0;                                            // where an expert begins
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) sum += count[j];
     int upto = sum;
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) {
@@ -297,7 +308,7 @@ __device__ inline void place(const RouteArgs& a, int r0, int r1, int32_t* next, 
         const int e = e0 + j;
         if (e >= a.experts) break;
         if (writes_ends) a.ends[e] = at;
-        int begin = at + first(e);
+        int begin = at + from[j];
         for (int w = 0; w < WAVES; ++w) {
             const int n = next[w * a.experts + e];
             next[w * a.experts + e] = begin;
@@ -346,7 +357,7 @@ template <int TYPE, int J, bool ALONE> __global__ __launch_bounds__(64 * waves_o
         for (int e = threadIdx.x; e < a.experts; e += 64 * kWaves) count[e] = 0;
         __syncthreads();
     }
-    const int64_t t0 = ALONE ? 0 : (int64_t)blockIdx.x * kTokens, t1 = ALONE || t0 + kTokens > a.tokens ? a.tokens : t0 + kTokens;
+    const int64_t t0 = ALONE ? 0 : (int64_t)blockIdx.x * a.block_tokens, t1 = ALONE || t0 + a.block_tokens > a.tokens ? a.tokens : t0 + a.block_tokens;
     const int64_t live = a.live ? *a.live : a.tokens;
     float z[J], ahead[J], bias[J];
     auto fetch = [&](int64_t token, float (&to)[J]) {
@@ -377,7 +388,7 @@ template <int TYPE, int J, bool ALONE> __global__ __launch_bounds__(64 * waves_o
     if (!a.ends) return;
     __syncthreads();
     if constexpr (ALONE) {
-        place<kWaves>(a, 0, (int)t1 * a.top, count, scan, [&](int r) { return (int)picked[r]; },
+        place<kWaves, false>(a, 0, (int)t1 * a.top, count, scan, [&](int r) { return (int)picked[r]; },
                       [&](int e) {
                           int n = 0;
                           for (int w = 0; w < kWaves; ++w) n += count[w * a.experts + e];
@@ -423,10 +434,33 @@ __global__ __launch_bounds__(64) void route_sum_kernel(RouteArgs a) {
 template <int WAVES> __global__ __launch_bounds__(64 * WAVES) void route_place_kernel(RouteArgs a) {
     extern __shared__ int32_t next[];
     __shared__ int32_t scan[WAVES];
-    const int64_t t0 = (int64_t)blockIdx.x * kTokens, t1 = t0 + kTokens < a.tokens ? t0 + kTokens : a.tokens;
-    place<WAVES>(a, (int)t0 * a.top, (int)t1 * a.top, next, scan, [&](int r) { return a.chosen[r]; },
-                 [&](int e) { return a.totals ? a.totals[e] : 0; },
-                 [&](int e) { return a.totals ? a.counts[(int64_t)e * a.blocks + blockIdx.x] : 0; }, blockIdx.x == 0);
+    const int64_t t0 = (int64_t)blockIdx.x * a.block_tokens, t1 = t0 + a.block_tokens < a.tokens ? t0 + a.block_tokens : a.tokens;
+    // few blocks: each adds up the counts of all of them, without the launch between
+    constexpr int kEach = kMostExperts / (64 * WAVES);
+    int all[kEach] = {}, before[kEach] = {};
+    if (a.counts && !a.totals) {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int e = kEach * (int)threadIdx.x + j;
+            if (e >= a.experts) break;
+            const int32_t* p = a.counts + (int64_t)e * a.blocks;
+#pragma unroll 8
+            for (int b = 0; b < a.blocks; ++b) {
+                const int n = p[b];
+                all[j] += n;
+                before[j] += b < (int)blockIdx.x ? n : 0;
+            }
+        }
+    }
+    auto mine = [&](const int (&v)[kEach], int e) {
+        int n = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) n = e % kEach == j ? v[j] : n;
+        return n;
+    };
+    place<WAVES, true>(a, (int)t0 * a.top, (int)t1 * a.top, next, scan, [&](int r) { return a.chosen[r]; },
+                 [&](int e) { return a.totals ? a.totals[e] : mine(all, e); },
+                 [&](int e) { return a.totals ? a.counts[(int64_t)e * a.blocks + blockIdx.x] : mine(before, e); }, blockIdx.x == 0);
 }
 
 template <int TYPE, int J> void launch(const RouteArgs& a, hipStream_t stream) {
@@ -452,23 +486,29 @@ template <int TYPE> void launch(const RouteArgs& a, hipStream_t stream) {
 }
 void launch_place(const RouteArgs& a, hipStream_t stream) {
     const int blocks = std::max(a.blocks, 1);
-    if (kTokens * a.top <= 4 * kWaveRoutes)
+    if (a.block_tokens * a.top <= 4 * kWaveRoutes)
         hipLaunchKernelGGL((route_place_kernel<4>), dim3((unsigned)blocks), dim3(256), 4 * a.experts * sizeof(int32_t), stream, a);
     else
         hipLaunchKernelGGL((route_place_kernel<16>), dim3((unsigned)blocks), dim3(1024), 16 * a.experts * sizeof(int32_t), stream, a);
 }
 
 bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
-int64_t blocks_of(int64_t tokens, int experts, int top) {
-    const bool alone = tokens <= kAlone && tokens * top <= kWaveRoutes * waves_of(lane_experts(experts));
-    return alone ? (tokens > 0 ? 1 : 0) : (tokens + kTokens - 1) / kTokens;
+// Tokens of a block: few are taken one by a wave (512 tokens to 8 of 256: 16 us with four one after the other), many as the
+// launches after it would have them.
+int block_tokens(int64_t tokens, int experts, int top) {
+    const int waves = waves_of(lane_experts(experts));
+    if (tokens <= kAlone && tokens * top <= kWaveRoutes * waves) return kAlone;
+    int n = waves;
+    while (n < kTokens && tokens > 256 * n) n *= 2;
+    return n;
 }
 
 }  // namespace
 
 extern "C" size_t route_experts_workspace_bytes(int32_t tokens, int32_t experts, int32_t top) {
     if (tokens < 1 || experts < 1 || top < 1 || experts > kMostExperts || top > kMostTop || (int64_t)tokens * top > 1 << 22) return 0;
-    const int64_t blocks = blocks_of(tokens, experts, top);
+    const int n = block_tokens(tokens, experts, top);
+    const int64_t blocks = (tokens + (int64_t)n - 1) / n;
     return blocks == 1 ? 0 : (size_t)(blocks + 1) * experts * sizeof(int32_t);
 }
 
@@ -494,15 +534,16 @@ extern "C" wino_status route_experts(const void* logits, int64_t stride, const f
     const size_t need = route_experts_workspace_bytes(tokens, experts, top);
     if (ends && need > 0 && (!workspace || workspace_bytes < need)) return WINO_EINVAL;
     if (tokens == 0 && !ends) return WINO_OK;
-    const int32_t blocks = (int32_t)blocks_of(tokens, experts, top);
+    const int32_t n = block_tokens(tokens, experts, top), blocks = (int32_t)((tokens + (int64_t)n - 1) / n);
     RouteArgs a = {logits, bias, live, chosen, weights, stride, tokens, experts, top, groups, experts / groups, top_groups,
                    group_best, score == WINO_SCORE_SIGMOID, normalise, 1, scale, winof4::make_fastdiv((uint32_t)(experts / groups)),
-                   order, ends, nullptr, nullptr, blocks};
+                   order, ends, nullptr, nullptr, blocks, n};
     while (2 * a.group_lanes * groups <= 64) a.group_lanes *= 2;
-    if (blocks > 1 && ends) a.counts = (int32_t*)workspace, a.totals = a.counts + (int64_t)blocks * experts;
+    if (blocks > 1 && ends) a.counts = (int32_t*)workspace;
+    if (blocks > kFewBlocks && ends) a.totals = a.counts + (int64_t)blocks * experts;
     if (blocks > 0) type == WINO_BF16 ? launch<WINO_BF16>(a, stream) : type == WINO_FP16 ? launch<WINO_FP16>(a, stream) : launch<WINO_FP32>(a, stream);
     if (ends && blocks != 1) {
-        if (blocks > 1) hipLaunchKernelGGL(route_sum_kernel, dim3((unsigned)experts), dim3(64), 0, stream, a);
+        if (a.totals) hipLaunchKernelGGL(route_sum_kernel, dim3((unsigned)experts), dim3(64), 0, stream, a);
         launch_place(a, stream);
     }
     return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;

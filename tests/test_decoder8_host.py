@@ -59,19 +59,20 @@ def test_route_refusals():
         return lib.route_experts(logits, stride, bias, t, e, top, score, g, tg, best, norm, scale, live, chosen, weights, order,
                                  ends, kind, ws, wb, None)
 
+    need = W.route_experts_workspace_bytes(65, 8, 2)
+    assert need > 0 and W.route_experts_workspace_bytes(64, 8, 2) == 0
     for kw, want in (({"kind": 3}, -1), ({"kind": -1}, -1), ({"score": 2}, -1), ({"t": -1}, -1), ({"e": 0}, -1), ({"top": 0}, -1),
                      ({"top": 9}, -1), ({"g": 0}, -1), ({"g": 3}, -1), ({"g": 4, "tg": 5}, -1), ({"tg": 0}, -1),
                      ({"g": 4, "tg": 2, "top": 5}, -1), ({"best": 0}, -1), ({"best": 3}, -1), ({"g": 8, "tg": 2, "best": 2}, -1),
                      ({"norm": 2}, -1), ({"scale": float("nan")}, -1), ({"scale": float("inf")}, -1), ({"order": None}, -1),
                      ({"ends": None}, -1), ({"logits": None}, -1), ({"chosen": None}, -1), ({"weights": None}, -1),
-                     ({"stride": 7}, -1), ({"t": 65, "ws": None}, -1), ({"t": 65, "wb": 95}, -1), ({"e": 1025, "stride": 1025}, -2),
+                     ({"stride": 7}, -1), ({"t": 65, "ws": None}, -1), ({"t": 65, "wb": need - 1}, -1), ({"e": 1025, "stride": 1025}, -2),
                      ({"e": 128, "stride": 128, "top": 33}, -2), ({"e": 130, "stride": 130, "g": 65}, -2),
                      ({"t": 1 << 22}, -2), ({"logits": p + 1}, -2), ({"kind": 2, "logits": p + 2}, -2), ({"bias": p + 2}, -2),
                      ({"live": p + 2}, -2), ({"chosen": p + 2}, -2), ({"weights": p + 1}, -2), ({"order": p + 2}, -2),
                      ({"ends": p + 2}, -2), ({"ws": p + 2}, -2), ({"t": 0, "order": None, "ends": None}, 0)):
         assert call(**kw) == want, kw
     assert W.route_experts_workspace_bytes(-1, 8, 2) == 0
-    assert W.route_experts_workspace_bytes(64, 8, 2) == 0 and W.route_experts_workspace_bytes(65, 8, 2) == 96
     assert W.route_experts_workspace_bytes(4, 2000, 2) == 0
 
 
