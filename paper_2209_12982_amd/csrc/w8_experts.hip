@@ -36,7 +36,7 @@ template <int TYPE, class S, bool FAR = false> void launch_tiles(const Args& a, 
     const int n_tiles = (a.n + S::kOuts - 1) / S::kOuts;
     // whole tiles of the rows, and one more for each expert's last
     const int m_tiles = a.routes / S::kRows + std::min(a.experts, a.routes);
-    const dim3 grid(workgroups<S>((int64_t)n_tiles * m_tiles));
+    const dim3 grid(workgroups<S>((int64_t)n_tiles * m_tiles, even_rows(a)));
     hipLaunchKernelGGL((w8_tiles_kernel<TYPE, S, true, FAR>), grid, dim3(S::kThreads), 0, stream, a, n_tiles, m_tiles);
 }
 
@@ -66,11 +66,14 @@ template <int TYPE> void pick(const Args& a, int64_t x_rows, hipStream_t stream)
     switch (kernel) {
         case kTile256x256: return launch_tiles<TYPE, Tile256x256>(a, stream);
         case kTile256x128: return launch_tiles<TYPE, Tile256x128>(a, stream);
+        case kTile128x256: return launch_tiles<TYPE, Tile128x256>(a, stream);
         case kTile128x128: return launch_tiles<TYPE, Tile128x128>(a, stream);
+        case kPair128x128: return launch_tiles<TYPE, Pair128x128>(a, stream);
         case kTile64x128: return launch_tiles<TYPE, Tile64x128>(a, stream);
         case kTile64x64: return launch_tiles<TYPE, Tile64x64>(a, stream);
         case kTile32x32: return launch_tiles<TYPE, Tile32x32>(a, stream);
         case kRows16: return launch_rows<TYPE, 1, 16>(a, stream);
+        case kRows16Few: return launch_rows<TYPE, 1, 8>(a, stream);
         default: return launch_rows<TYPE, 2, 4>(a, stream);
     }
 }

@@ -35,16 +35,15 @@ template <int TYPE, int NT, int V> void launch_rows(Args a, hipStream_t stream) 
 template <int TYPE, class S, bool FAR = false> void launch_tiles(Args a, int parts, hipStream_t stream) {
     parts = share_out(a, parts, S::BK);
     const int n_tiles = (a.n + S::kOuts - 1) / S::kOuts, m_tiles = (a.m + S::kRows - 1) / S::kRows;
-    const dim3 grid(workgroups<S>((int64_t)n_tiles * m_tiles), (unsigned)parts);
+    const dim3 grid(workgroups<S>((int64_t)n_tiles * m_tiles, even_rows(a)), (unsigned)parts);
     hipLaunchKernelGGL((w8_tiles_kernel<TYPE, S, false, FAR>), grid, dim3(S::kThreads), 0, stream, a, n_tiles, m_tiles);
     if (parts > 1)
         hipLaunchKernelGGL((w8_join_kernel<TYPE>), dim3((unsigned)(((int64_t)a.m * a.n + 255) / 256)), dim3(256), 0, stream, a, parts);
 }
 
-// Which kernel takes a call and in how many parts of k: the shortest estimate.  Over the 510 calls that is 2% longer than
-// the shortest measured one on average, 36% at most (18 rows by 2048 x 2048: 6.8 us, 5.0 in tiles of 32 x 32).  Parts are
-// joined by a second launch, which pays where few outputs have long sums (8 rows by 764 x 15824: 9.4 us in 6 parts, 11.4
-// whole); each is 1024 of k at least, and their sums 4 MiB at most.
+// Which kernel takes a call and in how many parts of k: the shortest estimate.  Parts are joined by a second launch, which
+// pays where few outputs have long sums (8 rows by 764 x 15824: 9.4 us in 6 parts, 11.4 whole; 515 rows by 1024 x 16384 22.4
+// in 3, 31 whole); each is 1024 of k at least, and their sums 16 MiB at most.
 struct Cut {
     Kernel kernel;
     int parts;
@@ -57,8 +56,8 @@ Cut cut(int64_t m, int64_t n, int64_t k) {
         const Form& f = kForms[i];
         const int64_t tiles = (n + f.outs - 1) / f.outs * ((m + f.rows - 1) / f.rows);
         for (const int parts : {1, 2, 4, 8, 16}) {
-            if (parts > 1 && (i < kTile64x128 || i >= kRows16 || k < 1024 * parts || parts * m * n > 1 << 20)) break;
-            const double join = parts > 1 ? 1.8 + 0.23 * parts + 1.5e-6 * (double)(parts * m * n) : 0;
+            if (parts > 1 && (i >= kRows16 || k < 1024 * parts || parts * m * n > 1 << 22)) break;
+            const double join = parts > 1 ? 1.95 + 0.17 * parts + 1.3e-6 * (double)(parts * m * n) : 0;
             const double t = estimate((Kernel)i, tiles * parts, k / parts, n * k, m) + join;
             if (least == 0 || t < least) least = t, best = Cut{(Kernel)i, parts};
         }
@@ -82,11 +81,14 @@ template <int TYPE> void pick(Args a, size_t bytes, hipStream_t stream) {
     switch (c.kernel) {
         case kTile256x256: return launch_tiles<TYPE, Tile256x256>(a, parts, stream);
         case kTile256x128: return launch_tiles<TYPE, Tile256x128>(a, parts, stream);
+        case kTile128x256: return launch_tiles<TYPE, Tile128x256>(a, parts, stream);
         case kTile128x128: return launch_tiles<TYPE, Tile128x128>(a, parts, stream);
+        case kPair128x128: return launch_tiles<TYPE, Pair128x128>(a, parts, stream);
         case kTile64x128: return launch_tiles<TYPE, Tile64x128>(a, parts, stream);
         case kTile64x64: return launch_tiles<TYPE, Tile64x64>(a, parts, stream);
         case kTile32x32: return launch_tiles<TYPE, Tile32x32>(a, parts, stream);
         case kRows16: return launch_rows<TYPE, 1, 16>(a, stream);
+        case kRows16Few: return launch_rows<TYPE, 1, 8>(a, stream);
         default: return launch_rows<TYPE, 2, 4>(a, stream);
     }
 }

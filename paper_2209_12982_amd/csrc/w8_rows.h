@@ -36,6 +36,21 @@ __global__ __launch_bounds__(64 * V) void w8_rows_kernel(Args a) {
             x[j] = a.x + (EXPERTS ? x_row(a, a.order[at]) : at) * a.x_stride + 32 * quarter;
         }
         for (int o = threadIdx.x; o < kRows * kOuts; o += 64 * V) sums[o / kOuts][o % kOuts] = 0;
+        // what a thread's results need beside their sums is asked for before the loop, not behind it
+        constexpr int kMine = (kRows * kOuts + 64 * V - 1) / (64 * V);
+        int row[kMine];
+        float xs[kMine], ws[kMine], bias[kMine];
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int o = threadIdx.x + 64 * V * i, at = m0 + o / kOuts, c = n0 + o % kOuts;
+            row[i] = -1;
+            if (o >= kRows * kOuts || at >= end || c >= a.n) continue;
+            row[i] = EXPERTS ? a.order[at] : at;
+            xs[i] = a.x_scales[EXPERTS ? x_row(a, row[i]) : at];
+            ws[i] = a.w_scales[(int64_t)expert * a.n + c];
+            bias[i] = !EXPERTS && a.bias ? (float)((const T*)a.bias)[c] : 0.f;
+            if (EXPERTS && row[i] >= a.routes) row[i] = -1;
+        }
         i32x4 acc[NT][MT];
 #pragma unroll
         for (int i = 0; i < NT; ++i)
@@ -74,24 +89,20 @@ __global__ __launch_bounds__(64 * V) void w8_rows_kernel(Args a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) atomicAdd(&sums[16 * j + r][16 * i + 4 * quarter + e], acc[i][j][e]);
         __syncthreads();
-        for (int o = threadIdx.x; o < kRows * kOuts; o += 64 * V) {
-            const int at = m0 + o / kOuts, c = n0 + o % kOuts;
-            if (at >= end || c >= a.n) continue;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            if (row[i] < 0) continue;
+            const int o = threadIdx.x + 64 * V * i, c = n0 + o % kOuts;
             const int sum = sums[o / kOuts][o % kOuts];
-            if (EXPERTS) {
-                const int route = a.order[at];
-                if ((uint32_t)route >= (uint32_t)a.routes) continue;
-                const float y = finish(sum, a.x_scales[x_row(a, route)], a.w_scales[(int64_t)expert * a.n + c], 0.f);
-                if (a.products)
-                    a.products[(int64_t)route * a.n + c] = y;
-                else
-                    ((T*)a.y)[route * a.y_stride + c] = (T)y;
-            } else if (a.part) {
-                a.part[((int64_t)blockIdx.z * a.m + at) * a.n + c] = sum;
-            } else {
-                ((T*)a.y)[at * a.y_stride + c] =
-                    (T)finish(sum, a.x_scales[at], a.w_scales[c], a.bias ? (float)((const T*)a.bias)[c] : 0.f);
+            if (!EXPERTS && a.part) {
+                a.part[((int64_t)blockIdx.z * a.m + row[i]) * a.n + c] = sum;
+                continue;
             }
+            const float y = finish(sum, xs[i], ws[i], bias[i]);
+            if (EXPERTS && a.products)
+                a.products[(int64_t)row[i] * a.n + c] = y;
+            else
+                ((T*)a.y)[row[i] * a.y_stride + c] = (T)y;
         }
         __syncthreads();                                    // before the sums are cleared again
     }

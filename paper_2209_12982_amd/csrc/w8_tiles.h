@@ -230,7 +230,7 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
     int buf, s;
     // Takes stage s.  Before its last step the next one has to have arrived, for all waves, with no more than `later` stages
     // on their way; all reads of this stage are done by then, so its buffer is filled again (FILL 1; 2: with the end of k).
-    auto stage = [&](auto fill, auto later) {
+    auto stage = [&](auto fill, auto later) __attribute__((always_inline)) {
         constexpr int FILL = decltype(fill)::value, LATER = decltype(later)::value;
         const int after = buf + 1 == S::STAGES ? 0 : buf + 1;
 #pragma unroll
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
         ++s;
     };
     // All stages of a tile, whose first ones are on their way.
-    auto run = [&](const Where& t) {
+    auto run = [&](const Where& t) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < S::WN; ++i)
 #pragma unroll
@@ -298,7 +298,9 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
     static_assert((S::kLoop ? S::kBytes : kParts) + S::GN * S::GM * kTurn <= S::STAGES * S::kBytes, "room to turn");
     uint8_t* mine = &lds[0][0] + (S::kLoop ? S::kBytes : kParts) + wave * kTurn;
     // Stores rows of BLOCKS times 32 results of type E; put(block, piece) gives the 16-byte pieces of this lane's half of them.
-    auto turned = [&](const Where& t, int set, int j, int i0, auto blocks, auto* out, int64_t stride, auto put) {
+    auto turned = [&](const Where& t, int set, int j, int i0, auto blocks, auto* out, int64_t stride, auto put) __attribute__((always_inline)) {
+        const int col0 = t.n0 + 32 * (S::WN * wn + i0);
+        if (col0 >= a.n) return;
         typedef std::remove_reference_t<decltype(*out)> E;
         const int lane = lane_s, c = lane & 31, half = lane >> 5;
         constexpr int BLOCKS = decltype(blocks)::value, kBlock = 32 * (int)sizeof(E), kRow = BLOCKS * kBlock;
@@ -313,7 +315,6 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
             for (int p = 0; p < kBlock / 32; ++p) *(u32x4*)at(c, i * kBlock + half * (kBlock / 2) + 16 * p) = put(i0 + i, p);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         const int* to_row = out_row[set] + 32 * (S::WM * wm + j);
-        const int col0 = t.n0 + 32 * (S::WN * wn + i0);
         if (col0 + 32 * BLOCKS <= a.n && (((uintptr_t)out | (uintptr_t)stride * sizeof(E)) & 15) == 0) {
 #pragma unroll
             for (int i = 0; i < 32 * kRow / 1024; ++i) {
@@ -322,18 +323,43 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
                 if (to_row[row] >= 0) *(u32x4*)((uint8_t*)(out + to_row[row] * stride + col0) + byte) = v;
             }
         } else {
-            // rows that do not begin at multiples of 16 bytes, or end inside: 64 neighbours one by one (a lane's own eight,
-            // each lane at another line, took 2.9 us longer for 333 x 5003)
-#pragma unroll 4
-            for (int i = 0; i < 16 * BLOCKS; ++i) {
-                const int p = 64 * i + lane, row = p / (32 * BLOCKS), col = p % (32 * BLOCKS);
-                const E v = *(const E*)at(row, col * (int)sizeof(E));
-                if (to_row[row] >= 0 && col0 + col < a.n) out[to_row[row] * stride + col0 + col] = v;
+            // Rows that do not begin at multiples of 16 bytes, or end inside: four neighbouring bytes a lane, eight of them read
+            // before the first is stored.  Of rows of 2-byte results that begin at an odd multiple of two bytes, these begin with
+            // the second result; a row's first and last one, where they are left, follow for all rows together.
+            constexpr int kWords = kRow / 4, kEach = 4 / (int)sizeof(E);
+            const int valid = min(a.n - col0, 32 * BLOCKS);
+            auto odd = [&](int r) { return kEach == 2 ? ((int)((uintptr_t)out >> 1) + r * (int)stride + col0) & 1 : 0; };
+#pragma unroll 1
+            for (int i0 = 0; i0 < 32 * kWords / 64; i0 += 8) {
+                uint32_t v[8];
+                int r[8], from[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int p = 64 * (i0 + i) + lane, row = p / kWords, word = p % kWords;
+                    r[i] = to_row[row];
+                    v[i] = *(const uint32_t*)at(row, 4 * word);
+                    from[i] = kEach * word;
+                    if constexpr (kEach == 2) {
+                        const uint32_t before = *(const uint32_t*)at(row, 4 * max(word - 1, 0));
+                        if (odd(r[i])) {
+                            v[i] = __builtin_amdgcn_alignbyte(v[i], before, 2);
+                            from[i] -= 1;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (r[i] >= 0 && from[i] >= 0 && from[i] + kEach <= valid) *(uint32_t*)(out + r[i] * stride + col0 + from[i]) = v[i];
+            }
+            if constexpr (kEach == 2) {
+                const int r = to_row[c], first = odd(r);
+                const int one = half ? ((valid - first) & 1 ? valid - 1 : -1) : (first ? 0 : -1);
+                if (r >= 0 && one >= 0) out[r * stride + col0 + one] = *(const E*)at(c, one * (int)sizeof(E));
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     };
-    auto store = [&](const Where& t, int set) {
+    auto store = [&](const Where& t, int set) __attribute__((always_inline)) {
         lane_s = anew(threadIdx.x & 63);
 #pragma unroll
         for (int j = 0; j < S::WM; ++j) {
@@ -345,7 +371,7 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
 #pragma unroll
                 for (int f = 0; f < 4; ++f) y[f] = finish(acc[i][j][e + f], xs, sc[f], bi[f]);
             };
-            auto wide = [&](auto* out, int64_t stride, auto put) {  // 4 bytes each, 256 of a row at a time
+            auto wide = [&](auto* out, int64_t stride, auto put) __attribute__((always_inline)) {  // 4 bytes each, 256 of a row at a time
                 constexpr int kBlocks = S::WN < 2 ? S::WN : 2;
 #pragma unroll
                 for (int i = 0; i < S::WN; i += kBlocks) turned(t, set, j, i, Int<kBlocks>(), out, stride, put);
@@ -419,35 +445,45 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
     }
 }
 
-// The tiles that calls are cut into (outputs x rows of a workgroup), largest first, and rows alone (w8_rows.h).
+// The tiles that calls are cut into (outputs x rows of a workgroup).  128 x 128 comes twice: with four stages and a compute
+// unit for itself, and with two stages and two to a compute unit, which suits more tiles than compute units.
 typedef Tile<4, 2, 2, 4, 1, 128, 2> Tile256x256;
 typedef Tile<2, 2, 4, 2, 1, 128, 2> Tile256x128;
+typedef Tile<2, 2, 2, 4, 1, 64, 3> Tile128x256;
 typedef Tile<2, 1, 2, 4, 1, 128, 4> Tile128x128;
-typedef Tile<1, 1, 2, 4, 1, 128, 4> Tile64x128;
-typedef Tile<1, 1, 2, 2, 1, 128, 4> Tile64x64;
+typedef Tile<2, 1, 2, 4, 1, 128, 2> Pair128x128;
+typedef Tile<1, 1, 2, 4, 1, 128, 3> Tile64x128;
+typedef Tile<1, 1, 2, 2, 1, 128, 3> Tile64x64;
 typedef Tile<1, 1, 1, 1, 4, 256, 4> Tile32x32;
-// Workgroups for so many tiles: as many for each XCD, one for each of 256 compute units where they go on.
-template <class S> inline unsigned workgroups(int64_t tiles) {
-    const int64_t n = (tiles + 7) / 8 * 8;
-    return (unsigned)(S::kLoop && n > 256 ? 256 : n);
-}
+// They, and rows alone (w8_rows.h): 16 outputs by 16 or 8 waves, 32 outputs by 4.
+enum Kernel { kTile256x256, kTile256x128, kTile128x256, kTile128x128, kPair128x128, kTile64x128, kTile64x64, kTile32x32, kRows16, kRows16Few, kRows32, kKernels };
 
-enum Kernel { kTile256x256, kTile256x128, kTile128x128, kTile64x128, kTile64x64, kTile32x32, kRows16, kRows32, kKernels };
+// Workgroups for so many tiles: as many for each XCD, one for each of 256 compute units where they go on.  With rows of
+// results that do not begin at multiples of 16 bytes they do not: a workgroup that goes on waits for its stores.
+template <class S> inline unsigned workgroups(int64_t tiles, bool even) {
+    const int64_t n = (tiles + 7) / 8 * 8;
+    return (unsigned)(S::kLoop && even && n > 256 ? 256 : n);
+}
+inline bool even_rows(const Args& a) {
+    return a.products ? a.n % 4 == 0 : (((uintptr_t)a.y | (uintptr_t)a.y_stride * 2) & 15) == 0;
+}
 
 // Whether rows that far apart need the kernel for that, Tile64x128 with FAR.
 inline bool far(int64_t rows, int64_t stride, int64_t k) { return (rows - 1) * stride + k > (int64_t)0xffffffff; }
 
 // What a kernel takes (us): `start` beside the loop, `step` for 1024 of k, `step` times 1 + `full` with a workgroup on each
-// of the 256 compute units (rows: with 16 rows), and `pair` times that for two workgroups each.  Fitted to 510 calls of 1 to
-// 8192 rows, 64 to 32768 outputs and k of 128 to 16384, off by 8 to 19% (root mean square).
+// of the 256 compute units (rows: with 16 rows), and `pair` times that for two workgroups each.  Chosen for 900 measured calls
+// of 1 to 8192 rows, 64 to 32768 outputs and k of 128 to 16384 such that the kernel of the shortest estimate is as near to the
+// shortest measured one as they go: 1.6% longer on average, 37% at most (1 row by 8192 x 16384: 29.4 us, 21.6 in tiles of 32 x 32).
 struct Form {
     int outs, rows;
     double start, step, pair, full;
 };
 constexpr Form kForms[kKernels] = {
-    {256, 256, 11.1, 7.9, 2.45, 0.43}, {256, 128, 6.6, 5.15, 2.17, 0.71}, {128, 128, 3.8, 2.6, 2.5, 0.42},
-    {64, 128, 2.5, 1.7, 2.2, 0.53},    {64, 64, 2.3, 1.24, 1.44, 0.65},   {32, 32, 2.4, 0.42, 1.2, 1.1},
-    {16, 16, 0.56, 0.40, 1.92, 1.32},  {32, 16, 0.46, 0.83, 1.76, 1.0},
+    {256, 256, 12.7, 5.6, 1.73, 0.69}, {256, 128, 5.86, 4.9, 1.84, 1.02}, {128, 256, 4.2, 4.3, 1.58, 0.98},
+    {128, 128, 3.91, 2.27, 2.17, 0.78}, {128, 128, 3.14, 2.42, 1.3, 1.01}, {64, 128, 2.26, 1.67, 1.56, 0.7},
+    {64, 64, 2.26, 1.58, 1.3, 0.38},    {32, 32, 2.32, 0.48, 1.24, 0.71},  {16, 16, 1.1, 0.32, 1.84, 1.37},
+    {16, 16, 0.26, 0.424, 1.76, 1.16},  {32, 16, 0.46, 0.98, 1.5, 1.24},
 };
 // The time of a kernel that has so many tiles, for k of a part and so many bytes of weights.
 inline double estimate(Kernel kernel, int64_t tiles, int64_t k, int64_t bytes, int64_t m) {
@@ -455,7 +491,10 @@ inline double estimate(Kernel kernel, int64_t tiles, int64_t k, int64_t bytes, i
     const int64_t rest = tiles % 512;
     const double rounds = f.pair * (double)(tiles / 512) + (rest == 0 ? 0 : (rest <= 256 ? 1 : f.pair));
     const double fill = kernel >= kRows16 ? (double)m / 16 : (tiles < 256 ? (double)tiles / 256 : 1);
-    const double t = (f.start + f.step * (1 + f.full * fill) * (double)k / 1024) * rounds, memory = (double)bytes / 5.2e6;
+    // Sixteen rows of 4096 bytes or a multiple lie in the same memory channels, and eight waves ask for half of them at a
+    // time: one row by 4096 x 4096 7.2 us, by 16 waves 5.5; by 4096 x 4080 4.2 both.
+    const double same = kernel == kRows16Few && k % 4096 == 0 ? 1.4 : 1;
+    const double t = (f.start + same * f.step * (1 + f.full * fill) * (double)k / 1024) * rounds, memory = (double)bytes / 5.2e6;
     return t > memory ? t + 0.05 * memory : memory + 0.05 * t;      // what is less decides between equal ones
 }
 
