@@ -773,7 +773,9 @@ wino_status route_experts(const void* logits, int64_t stride, const float* bias,
  *   a launch holds 2^23 workgroups: (routes / 128 + experts) n / 128, experts
  *   n / 16, and with weights (routes / top) n / 256 stay below that.
  *   workspace w8_experts_matmul_workspace_bytes(routes, n, weights != NULL)
- *             bytes or more, 16-byte aligned, scratch: needed with weights.
+ *             bytes or more, 16-byte aligned, scratch.  With weights, routes * n
+ *             floats of it are needed; with less than the rest, or NULL, the
+ *             same result comes more slowly.
  */
 size_t w8_experts_matmul_workspace_bytes(int32_t routes, int32_t n, int32_t combine);
 wino_status w8_experts_matmul(const int8_t* x, int64_t x_stride, const float* x_scales, int32_t x_rows, const int8_t* w,

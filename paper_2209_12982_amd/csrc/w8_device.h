@@ -26,12 +26,15 @@ struct Args {
     int32_t m, n, k;        // m: rows of x (dense)
     int32_t* part;          // dense: sums of parts of k, [parts][m][n], or null
     int32_t steps;          // of k in a part
+    int32_t* tail;          // sums of the last tiles' parts of k, or null
     // experts: routes in the order of their experts, where each expert's begin; x has a row for `share` routes
     const int32_t *order, *ends;
     int32_t experts, routes;
     winof4::FastDiv share;
     float* products;        // [routes][n] where they are added up with weights, or null
 };
+
+constexpr int kMostParts = 8;           // of k, of the last tiles
 
 __device__ const uint32_t kZeros[4] = {0, 0, 0, 0};     // what lies behind the end of k
 

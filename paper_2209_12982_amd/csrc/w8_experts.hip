@@ -36,15 +36,17 @@ template <int TYPE, class S, bool FAR = false> void launch_tiles(const Args& a, 
     const int n_tiles = (a.n + S::kOuts - 1) / S::kOuts;
     // whole tiles of the rows, and one more for each expert's last
     const int m_tiles = a.routes / S::kRows + std::min(a.experts, a.routes);
-    const dim3 grid(workgroups<S>((int64_t)n_tiles * m_tiles, even_rows(a)));
+    const dim3 grid(workgroups<S>(a, (int64_t)n_tiles * m_tiles, even_rows(a)));
     hipLaunchKernelGGL((w8_tiles_kernel<TYPE, S, true, FAR>), grid, dim3(S::kThreads), 0, stream, a, n_tiles, m_tiles);
+    launch_tail<TYPE, S, true>(a, n_tiles, m_tiles, stream);
 }
 
 // The shortest estimate for routes that are spread evenly: the host does not know how they are.  An expert with r rows on
 // average has r / rows tiles and half a one more, or one.  Measured (us): 4096 tokens to 8 of 64 experts, n 2816, k 2048:
-// 256 x 256 257, 256 x 128 328, 128 x 128 337; 2000 to 2 of 8, 4096 x 8192: 218, 260, 212; 256 to 6 of 64: 102, 87, 91,
-// 64 x 64 79; 32 to 6 of 64: rows of 32 outputs 62, 64 x 64 67; one to 2 of 8, 1024 x 2048: rows of 16 outputs 4.5.
-Kernel choose(int64_t routes, int64_t experts, int64_t n, int64_t k) {
+// 256 x 256 249, two 128 x 128 297, 128 x 256 337; 2000 to 2 of 8, 4096 x 8192: 187 with the last tiles in parts and 220
+// without, 210, 218; 256 to 6 of 64: 102, 87, 91, 64 x 64 79; 32 to 6 of 64: rows of 32 outputs 62, 64 x 64 67; one to 2 of 8,
+// 1024 x 2048: rows of 16 outputs 4.5.
+Kernel choose(int64_t routes, int64_t experts, int64_t n, int64_t k, bool tail) {
     const int64_t used = std::min(routes, experts);
     const double each = (double)routes / (double)used;
     Kernel best = kTile256x256;
@@ -53,19 +55,22 @@ Kernel choose(int64_t routes, int64_t experts, int64_t n, int64_t k) {
         const Form& f = kForms[i];
         if (i >= kRows16 && each > 16) break;
         const double tiles = each > f.rows ? each / f.rows + 0.5 : 1;
-        const double t = estimate((Kernel)i, (int64_t)(tiles * (double)(used * ((n + f.outs - 1) / f.outs))), k, used * n * k,
-                                  (int64_t)std::min(each, 16.0));
+        const int64_t all = (int64_t)(tiles * (double)(used * ((n + f.outs - 1) / f.outs)));
+        double t = estimate((Kernel)i, all, k, used * n * k, (int64_t)std::min(each, 16.0));
+        // tiles whose last ones are cut in parts of k take a part of the last round, and their join 20 us
+        if (i == kTile256x256 && tail)
+            t = std::min(t, std::max((f.start + f.step * (1 + f.full) * (double)k / 1024) * ((double)all / 256 + 0.1) + 20,
+                                     (double)(used * n * k) / 5.2e6));
         if (least == 0 || t < least) least = t, best = (Kernel)i;
     }
     return best;
 }
 
 template <int TYPE> void pick(const Args& a, int64_t x_rows, hipStream_t stream) {
-    const Kernel kernel = choose(a.routes, a.experts, a.n, a.k);
+    const Kernel kernel = choose(a.routes, a.experts, a.n, a.k, a.tail != nullptr);
     if (kernel < kRows16 && far(x_rows, a.x_stride, a.k)) return launch_tiles<TYPE, Tile64x128, true>(a, stream);
     switch (kernel) {
         case kTile256x256: return launch_tiles<TYPE, Tile256x256>(a, stream);
-        case kTile256x128: return launch_tiles<TYPE, Tile256x128>(a, stream);
         case kTile128x256: return launch_tiles<TYPE, Tile128x256>(a, stream);
         case kTile128x128: return launch_tiles<TYPE, Tile128x128>(a, stream);
         case kPair128x128: return launch_tiles<TYPE, Pair128x128>(a, stream);
@@ -87,14 +92,18 @@ template <int TYPE> void combine(const Args& a, const int32_t* chosen, const flo
         hipLaunchKernelGGL((w8_combine_kernel<TYPE, 1>), grid, dim3(256), 0, stream, a, chosen, weights, top);
 }
 
+size_t product_bytes(int64_t routes, int64_t n) { return ((size_t)routes * n * sizeof(float) + 15) / 16 * 16; }
+// Results for which tiles of 256 x 256, the last ones cut in parts of k, may be the fastest.
+bool many(int64_t routes, int64_t n) { return routes * n >= 1 << 22; }
+
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
 
 }  // namespace
 
 extern "C" size_t w8_experts_matmul_workspace_bytes(int32_t routes, int32_t n, int32_t combine) {
-    if (routes < 1 || n < 1 || !combine) return 0;
-    return (size_t)routes * n * sizeof(float);
+    if (routes < 1 || n < 1) return 0;
+    return (combine ? product_bytes(routes, n) : 0) + (many(routes, n) ? kTailBytes : 0);
 }
 
 extern "C" wino_status w8_experts_matmul(const int8_t* x, int64_t x_stride, const float* x_scales, int32_t x_rows, const int8_t* w,
@@ -121,10 +130,14 @@ extern "C" wino_status w8_experts_matmul(const int8_t* x, int64_t x_stride, cons
     a.x = x, a.w = w, a.x_scales = x_scales, a.w_scales = w_scales, a.y = y, a.x_stride = x_stride, a.y_stride = y_stride;
     a.n = n, a.k = k, a.order = order, a.ends = ends, a.experts = experts, a.routes = routes;
     a.share = winof4::make_fastdiv((uint32_t)(routes / x_rows));
+    const size_t products = weights ? product_bytes(routes, n) : 0;
     if (weights) {
-        if (!workspace || workspace_bytes < w8_experts_matmul_workspace_bytes(routes, n, 1)) return WINO_EINVAL;
+        if (!workspace || workspace_bytes < (size_t)routes * n * sizeof(float)) return WINO_EINVAL;
         a.products = (float*)workspace;
     }
+    // Shorter sums gain less than the join of their parts takes: 3000 tokens to 4 of 16, 2048 x 4096, 121 us without parts and
+    // 124 with them.
+    if (many(routes, n) && k > 4096 && workspace && workspace_bytes >= products + kTailBytes) a.tail = (int32_t*)((char*)workspace + products);
     type == WINO_BF16 ? pick<WINO_BF16>(a, x_rows, stream) : pick<WINO_FP16>(a, x_rows, stream);
     if (weights && hipGetLastError() == hipSuccess) {
         type == WINO_BF16 ? combine<WINO_BF16>(a, chosen, weights, top, stream) : combine<WINO_FP16>(a, chosen, weights, top, stream);

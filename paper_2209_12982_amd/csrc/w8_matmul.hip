@@ -35,8 +35,9 @@ template <int TYPE, int NT, int V> void launch_rows(Args a, hipStream_t stream) 
 template <int TYPE, class S, bool FAR = false> void launch_tiles(Args a, int parts, hipStream_t stream) {
     parts = share_out(a, parts, S::BK);
     const int n_tiles = (a.n + S::kOuts - 1) / S::kOuts, m_tiles = (a.m + S::kRows - 1) / S::kRows;
-    const dim3 grid(workgroups<S>((int64_t)n_tiles * m_tiles, even_rows(a)), (unsigned)parts);
+    const dim3 grid(workgroups<S>(a, (int64_t)n_tiles * m_tiles, even_rows(a)), (unsigned)parts);
     hipLaunchKernelGGL((w8_tiles_kernel<TYPE, S, false, FAR>), grid, dim3(S::kThreads), 0, stream, a, n_tiles, m_tiles);
+    launch_tail<TYPE, S, false>(a, n_tiles, m_tiles, stream);
     if (parts > 1)
         hipLaunchKernelGGL((w8_join_kernel<TYPE>), dim3((unsigned)(((int64_t)a.m * a.n + 255) / 256)), dim3(256), 0, stream, a, parts);
 }
@@ -58,7 +59,8 @@ Cut cut(int64_t m, int64_t n, int64_t k) {
         for (const int parts : {1, 2, 4, 8, 16}) {
             if (parts > 1 && (i >= kRows16 || k < 1024 * parts || parts * m * n > 1 << 22)) break;
             const double join = parts > 1 ? 1.95 + 0.17 * parts + 1.3e-6 * (double)(parts * m * n) : 0;
-            const double t = estimate((Kernel)i, tiles * parts, k / parts, n * k, m) + join;
+            double t = estimate((Kernel)i, tiles * parts, k / parts, n * k, m) + join;
+            if (i == kTile256x256 && parts == 1) t -= std::max(tail_gain(tiles, k), 0.0);
             if (least == 0 || t < least) least = t, best = Cut{(Kernel)i, parts};
         }
     }
@@ -70,6 +72,9 @@ bool beyond(int64_t m, int64_t n, int64_t k) {
 }
 
 size_t part_bytes(const Cut& c, int64_t m, int64_t n) { return c.parts > 1 ? (size_t)(c.parts * m * n) * sizeof(int32_t) : 0; }
+bool cuts_tail(const Cut& c, int64_t m, int64_t n, int64_t k) {
+    return c.kernel == kTile256x256 && c.parts == 1 && tail_gain((m + 255) / 256 * ((n + 255) / 256), k) > 0;
+}
 
 template <int TYPE> void pick(Args a, size_t bytes, hipStream_t stream) {
     const Cut c = cut(a.m, a.n, a.k);
@@ -78,9 +83,9 @@ template <int TYPE> void pick(Args a, size_t bytes, hipStream_t stream) {
         return launch_tiles<TYPE, Tile64x128, true>(a, 1, stream);
     }
     const int parts = a.part && bytes >= part_bytes(c, a.m, a.n) ? c.parts : 1;
+    if (cuts_tail(c, a.m, a.n, a.k) && bytes >= kTailBytes) a.tail = a.part;
     switch (c.kernel) {
         case kTile256x256: return launch_tiles<TYPE, Tile256x256>(a, parts, stream);
-        case kTile256x128: return launch_tiles<TYPE, Tile256x128>(a, parts, stream);
         case kTile128x256: return launch_tiles<TYPE, Tile128x256>(a, parts, stream);
         case kTile128x128: return launch_tiles<TYPE, Tile128x128>(a, parts, stream);
         case kPair128x128: return launch_tiles<TYPE, Pair128x128>(a, parts, stream);
@@ -100,7 +105,8 @@ bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
 
 extern "C" size_t w8_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k) {
     if (m < 1 || n < 1 || k < 1 || beyond(m, n, k)) return 0;
-    return part_bytes(cut(m, n, k), m, n);
+    const Cut c = cut(m, n, k);
+    return cuts_tail(c, m, n, k) ? kTailBytes : part_bytes(c, m, n);
 }
 
 extern "C" wino_status w8_matmul(const int8_t* x, int64_t x_stride, const float* x_scales, const int8_t* w, const float* w_scales,

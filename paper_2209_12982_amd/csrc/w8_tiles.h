@@ -24,6 +24,7 @@ template <int WN_, int WM_, int GN_, int GM_, int GK_, int BK_, int STAGES_> str
     // The largest tiles leave a compute unit room for one workgroup: it takes tile after tile, and the next one's first stage
     // is on its way while results are stored.
     static constexpr bool kLoop = kOuts * kRows >= 65536;
+    static constexpr int kSlots = 32;                       // compute units of an XCD
     static_assert(WN == 1 || WN == 2 || WN == 4, "rows of results are turned in whole sets of banks");
     static_assert(!kLoop || (STAGES == 2 && GK == 1), "results are turned in the second stage");
     static_assert(kOuts * kRowPieces % kThreads == 0 && kRows * kRowPieces % kThreads == 0, "whole copies");
@@ -52,48 +53,87 @@ __device__ inline int anew(int v) {
     return v;
 }
 
-// The experts' tile that a workgroup takes, or false where it has none: its expert, where its rows begin and end in the
-// order, and which of n_tiles outputs.  An expert's tiles stand together, those of the same outputs next to each other, and
-// each XCD takes a piece of that list (workgroup i runs on XCD i % 8), `own` counts in it: weights stay in its L2 for all rows
-// that need them.
-template <int ROWS> __device__ inline bool find(const Args& a, int n_tiles, int own, int& expert, int& begin, int& end, int& n_tile) {
+// A tile: its rows (experts: places in the order), outputs, expert, stages of k, and the place of its sums in a.tail, or -1.
+struct Where {
+    int m0, m1, n0, expert, first, last, slot;
+};
+
+// The tiles of rows of 64 experts from e0 on: where a lane's expert has its rows, how many tiles, and how many up to it.
+template <int ROWS> __device__ inline void count_tiles(const Args& a, int e0, int& begin, int& end, int& count, int& upto) {
     const int lane = threadIdx.x & 63;
-    // the tiles of rows of 64 experts: where their rows are, how many, and how many up to each lane
-    int b, e, count, upto;
-    auto set = [&](int e0) {
-        b = 0, e = 0;
-        if (e0 + lane < a.experts) rows_of(a, e0 + lane, b, e);
-        count = (e - b + ROWS - 1) / ROWS;
-        upto = count;
+    begin = 0, end = 0;
+    if (e0 + lane < a.experts) rows_of(a, e0 + lane, begin, end);
+    count = (end - begin + ROWS - 1) / ROWS;
+    upto = count;
 #pragma unroll
-        for (int s = 1; s < 64; s <<= 1) {
-            const int other = __shfl_up(upto, s);
-            if (lane >= s) upto += other;
-        }
-    };
-    int all = 0;
-    for (int e0 = 0; e0 < a.experts; e0 += 64) {
-        set(e0);
-        all += __builtin_amdgcn_readlane(upto, 63);
+    for (int s = 1; s < 64; s <<= 1) {
+        const int other = __shfl_up(upto, s);
+        if (lane >= s) upto += other;
     }
-    const int each = (all * n_tiles + 7) / 8, index = (int)(blockIdx.x % 8) * each + own;
-    if (own >= each || index >= all * n_tiles) return false;
+}
+
+// The tiles of one XCD (workgroup i runs on XCD i % 8): a piece of the list of all.  An expert's tiles stand together there,
+// those of the same outputs next to each other, so that weights stay in the XCD's L2 for all rows that need them; dense ones
+// eight rows of tiles at a time.  Items are what workgroups take: the whole tiles, and parts of the last ones.
+struct List {
+    int begin, length, whole, parts, items;     // whole: tiles that are not cut
+};
+// In how many parts of k the last `rest` tiles of an XCD are cut, where these would leave half of its compute units idle.
+__host__ __device__ inline int tail_parts(int rest, int stages) {
+    int parts = rest > 0 ? 32 / rest : 1;
+    parts = parts > kMostParts ? kMostParts : parts;
+    return parts > stages / 4 ? stages / 4 : parts;
+}
+template <class S, bool EXPERTS> __device__ inline List list_of(const Args& a, int xcd, int n_tiles, int m_tiles) {
+    int tiles = n_tiles * m_tiles;
+    if (EXPERTS) {
+        tiles = 0;
+        for (int e0 = 0; e0 < a.experts; e0 += 64) {
+            int begin, end, count, upto;
+            count_tiles<S::kRows>(a, e0, begin, end, count, upto);
+            tiles += __builtin_amdgcn_readlane(upto, 63);
+        }
+        tiles *= n_tiles;
+    }
+    const int each = (tiles + 7) / 8;
+    List l;
+    l.begin = xcd * each;
+    l.length = max(0, min(each, tiles - l.begin));
+    l.whole = l.length, l.parts = 1;
+    if (S::kLoop && a.tail) {
+        const int rest = l.length % S::kSlots, parts = tail_parts(rest, (a.k + S::BK - 1) / S::BK);
+        if (parts > 1) l.whole -= rest, l.parts = parts;
+    }
+    l.items = l.whole + (l.length - l.whole) * l.parts;
+    return l;
+}
+// Tile `index` of all.
+template <class S, bool EXPERTS> __device__ inline void locate(const Args& a, int index, int n_tiles, int m_tiles, Where& t) {
+    t.expert = 0;
+    if (!EXPERTS) {
+        const int set = 8 * n_tiles, g = index / set, high = min(8, m_tiles - 8 * g), in = index - g * set;
+        t.m0 = (8 * g + in % high) * S::kRows;
+        t.n0 = in / high * S::kOuts;
+        t.m1 = a.m;
+        return;
+    }
+    t.m0 = t.m1 = t.n0 = 0;
     int before = 0;
     for (int e0 = 0; e0 < a.experts; e0 += 64) {
-        if (a.experts > 64) set(e0);
+        int begin, end, count, upto;
+        count_tiles<S::kRows>(a, e0, begin, end, count, upto);
         const uint64_t here = __ballot(index < (before + upto) * n_tiles);
         if (here) {
-            const int l = __builtin_ctzll(here);
-            const int tiles = __builtin_amdgcn_readlane(count, l), in = index - (before + __builtin_amdgcn_readlane(upto, l) - tiles) * n_tiles;
-            expert = e0 + l;
-            begin = __builtin_amdgcn_readlane(b, l) + in % tiles * ROWS;
-            end = __builtin_amdgcn_readlane(e, l);
-            n_tile = in / tiles;
-            return true;
+            const int l = __builtin_ctzll(here), tiles = __builtin_amdgcn_readlane(count, l);
+            const int in = index - (before + __builtin_amdgcn_readlane(upto, l) - tiles) * n_tiles;
+            t.expert = e0 + l;
+            t.m0 = __builtin_amdgcn_readlane(begin, l) + in % tiles * S::kRows;
+            t.m1 = __builtin_amdgcn_readlane(end, l);
+            t.n0 = in / tiles * S::kOuts;
+            return;
         }
         before += __builtin_amdgcn_readlane(upto, 63);
     }
-    return false;
 }
 
 // FAR: rows of x whose distance from the first of a tile (experts: of x) does not fit 32 bits.
@@ -108,29 +148,26 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 31, half = lane >> 5;
 
-    struct Where {
-        int m0, m1, n0, expert;                             // rows (experts: places in the order), outputs
-    };
+    const List list = list_of<S, EXPERTS>(a, blockIdx.x % 8, n_tiles, m_tiles);
+    const int all = (a.k + S::BK - 1) / S::BK;
     auto where = [&](int turn, Where& t) {
-        const int own = (int)(blockIdx.x / 8) + turn * (int)(gridDim.x / 8);
-        t.expert = 0;
-        if constexpr (EXPERTS) {
-            int n_tile;
-            if (!find<S::kRows>(a, n_tiles, own, t.expert, t.m0, t.m1, n_tile)) return false;
-            t.n0 = n_tile * S::kOuts;
-        } else {
-            // workgroup i runs on XCD i % 8: each gets neighbouring tiles, eight rows of them at a time
-            const int tiles = n_tiles * m_tiles, each = (tiles + 7) / 8, index = (int)(blockIdx.x % 8) * each + own;
-            if (own >= each || index >= tiles) return false;
-            const int set = 8 * n_tiles, g = index / set, high = min(8, m_tiles - 8 * g), in = index - g * set;
-            t.m0 = (8 * g + in % high) * S::kRows;
-            t.n0 = in / high * S::kOuts;
-            t.m1 = a.m;
+        const int item = (int)(blockIdx.x / 8) + turn * (int)(gridDim.x / 8);
+        if (item >= list.items) return false;
+        const int cut = list.length - list.whole, part = item < list.whole ? 0 : (item - list.whole) / cut;
+        locate<S, EXPERTS>(a, list.begin + item - part * cut, n_tiles, m_tiles, t);
+        t.first = 0, t.last = all, t.slot = -1;
+        if (item >= list.whole) {
+            const int steps = (all + list.parts - 1) / list.parts;
+            t.first = min(part * steps, all);
+            t.last = min(t.first + steps, all);
+            t.slot = (int)(blockIdx.x % 8) * S::kSlots + item - list.whole;
+        } else if (!EXPERTS && a.part) {
+            t.first = (int)blockIdx.y * a.steps;
+            t.last = min(t.first + a.steps, all);
         }
+        for (int* v : {&t.m0, &t.m1, &t.n0, &t.expert, &t.first, &t.last, &t.slot}) *v = __builtin_amdgcn_readfirstlane(*v);
         return true;
     };
-    const int all = (a.k + S::BK - 1) / S::BK;
-    const int first = EXPERTS ? 0 : (int)blockIdx.y * a.steps, last = EXPERTS ? all : min(first + a.steps, all);
     Where t;
     if (!where(0, t)) return;
 
@@ -270,9 +307,10 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
         busy = t.m0 + 32 * S::WM * wm < t.m1 && t.n0 + 32 * S::WN * wn < a.n;
-        buf = 0, s = first;
-        if (first >= last) return;
-        if (last - first >= S::STAGES)
+        const int last = t.last;
+        buf = 0, s = t.first;
+        if (s >= last) return;
+        if (last - s >= S::STAGES)
             WINO_WAIT_VM_LDS((S::STAGES - 1) * kPieces);
         else
             WINO_WAIT_VM_LDS(0);
@@ -361,6 +399,17 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
     };
     auto store = [&](const Where& t, int set) __attribute__((always_inline)) {
         lane_s = anew(threadIdx.x & 63);
+        if (S::kLoop && t.slot >= 0) {                      // sums of a part of k, as the lanes have them
+            int32_t* to = a.tail + (int64_t)t.slot * (S::kOuts * S::kRows) + (wave * (S::WN * S::WM * 4) * 64 + lane_s) * 4;
+#pragma unroll
+            for (int i = 0; i < S::WN; ++i)
+#pragma unroll
+                for (int j = 0; j < S::WM; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        *(i32x4*)(to + ((j * S::WN + i) * 4 + e) * 256) = i32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < S::WM; ++j) {
             const int c = lane_s & 31, half = lane_s >> 5;
@@ -401,7 +450,7 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
     prepare(t);
 #pragma unroll
     for (int i = 0; i < S::STAGES; ++i)
-        if (first + i < last) copy(first + i, i);
+        if (t.first + i < t.last) copy(t.first + i, i);
     load_scales(t, 0);
     for (int turn = 0, set = 0;; ++turn, set ^= 1) {
         run(t);
@@ -434,21 +483,75 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
         const bool more = S::kLoop && where(turn + 1, next);
         if (more) {
             prepare(next);
-            if (first < last) copy(first, 0);
+            if (next.first < next.last) copy(next.first, 0);
             load_scales(next, set ^ 1);
         }
         store(t, set);
         if (!more) return;
         meet();                                             // results are turned, the second stage is free
-        if (first + 1 < last) copy(first + 1, 1);
         t = next;
+        if (t.first + 1 < t.last) copy(t.first + 1, 1);
+    }
+}
+
+// The results of tiles that were cut in parts of k: a wave for each block of 32 x 32, of a workgroup of four.  Memory bounds it:
+// 4 bytes of each part a result.
+template <int TYPE, class S, bool EXPERTS> __global__ __launch_bounds__(256) void w8_tail_kernel(Args a, int n_tiles, int m_tiles) {
+    typedef typename Half<TYPE>::type T;
+    typedef __attribute__((ext_vector_type(8))) T T8;
+    constexpr int kUnits = S::kWaves * S::WM * S::WN;
+    const int xcd = blockIdx.x % 8, own = blockIdx.x / 8 * 4 + (threadIdx.x >> 6), unit = own % kUnits, tile = own / kUnits;
+    const List list = list_of<S, EXPERTS>(a, xcd, n_tiles, m_tiles);
+    const int cut = list.length - list.whole;
+    if (tile >= cut) return;
+    Where t;
+    locate<S, EXPERTS>(a, list.begin + list.whole + tile, n_tiles, m_tiles, t);
+    const int lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5;
+    const int wave = unit / (S::WM * S::WN), j = unit / S::WN % S::WM, i = unit % S::WN;
+    const int at = t.m0 + 32 * (S::WM * (wave / S::GN) + j) + c, col = t.n0 + 32 * (S::WN * (wave % S::GN) + i) + 16 * half;
+    const int32_t* from = a.tail + (int64_t)(xcd * S::kSlots + tile) * (S::kOuts * S::kRows) + (unit * 4 * 64 + lane) * 4;
+    const int row = at >= t.m1 ? -1 : (EXPERTS ? a.order[at] : at);
+    i32x4 sum[4] = {};
+    for (int p = 0; p < list.parts; ++p, from += (int64_t)cut * (S::kOuts * S::kRows))
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += *(const i32x4*)(from + e * 256);
+    if (row < 0 || col >= a.n || (EXPERTS && row >= a.routes)) return;
+    const float xs = a.x_scales[EXPERTS ? x_row(a, row) : row];
+    const float* ws = a.w_scales + (int64_t)t.expert * a.n + col;
+    const bool whole = col + 16 <= a.n;
+    float y[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const bool there = whole || col + e < a.n;
+        const float bias = !EXPERTS && a.bias && there ? (float)((const T*)a.bias)[col + e] : 0.f;
+        y[e] = finish(sum[e / 4][e % 4], xs, there ? ws[e] : 0.f, bias);
+    }
+    if (EXPERTS && a.products) {
+        float* to = a.products + (int64_t)row * a.n + col;
+        if (whole && ((uintptr_t)to & 15) == 0) {
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) *(f32x4*)(to + e) = f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]};
+        } else {
+            for (int e = 0; e < 16; ++e)
+                if (col + e < a.n) to[e] = y[e];
+        }
+        return;
+    }
+    T* to = (T*)a.y + row * a.y_stride + col;
+    if (whole && ((uintptr_t)to & 15) == 0) {
+#pragma unroll
+        for (int e = 0; e < 16; e += 8)
+            *(u32x4*)(to + e) = __builtin_bit_cast(u32x4, T8{(T)y[e], (T)y[e + 1], (T)y[e + 2], (T)y[e + 3], (T)y[e + 4], (T)y[e + 5], (T)y[e + 6], (T)y[e + 7]});
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (col + e < a.n) to[e] = (T)y[e];
     }
 }
 
 // The tiles that calls are cut into (outputs x rows of a workgroup).  128 x 128 comes twice: with four stages and a compute
 // unit for itself, and with two stages and two to a compute unit, which suits more tiles than compute units.
 typedef Tile<4, 2, 2, 4, 1, 128, 2> Tile256x256;
-typedef Tile<2, 2, 4, 2, 1, 128, 2> Tile256x128;
 typedef Tile<2, 2, 2, 4, 1, 64, 3> Tile128x256;
 typedef Tile<2, 1, 2, 4, 1, 128, 4> Tile128x128;
 typedef Tile<2, 1, 2, 4, 1, 128, 2> Pair128x128;
@@ -456,13 +559,22 @@ typedef Tile<1, 1, 2, 4, 1, 128, 3> Tile64x128;
 typedef Tile<1, 1, 2, 2, 1, 128, 3> Tile64x64;
 typedef Tile<1, 1, 1, 1, 4, 256, 4> Tile32x32;
 // They, and rows alone (w8_rows.h): 16 outputs by 16 or 8 waves, 32 outputs by 4.
-enum Kernel { kTile256x256, kTile256x128, kTile128x256, kTile128x128, kPair128x128, kTile64x128, kTile64x64, kTile32x32, kRows16, kRows16Few, kRows32, kKernels };
+enum Kernel { kTile256x256, kTile128x256, kTile128x128, kPair128x128, kTile64x128, kTile64x64, kTile32x32, kRows16, kRows16Few, kRows32, kKernels };
 
 // Workgroups for so many tiles: as many for each XCD, one for each of 256 compute units where they go on.  With rows of
 // results that do not begin at multiples of 16 bytes they do not: a workgroup that goes on waits for its stores.
-template <class S> inline unsigned workgroups(int64_t tiles, bool even) {
-    const int64_t n = (tiles + 7) / 8 * 8;
-    return (unsigned)(S::kLoop && even && n > 256 ? 256 : n);
+template <class S> inline unsigned workgroups(const Args& a, int64_t tiles, bool even) {
+    int64_t each = (tiles + 7) / 8;
+    if (S::kLoop && a.tail) each = (each + S::kSlots - 1) / S::kSlots * S::kSlots;      // parts fill the last round at most
+    return (unsigned)(8 * (S::kLoop && even && each > 32 ? 32 : each));
+}
+// Sums of the tiles that are cut: a tile for each compute unit at most.
+constexpr size_t kTailBytes = (size_t)256 * 256 * 256 * sizeof(int32_t);
+template <int TYPE, class S, bool EXPERTS> void launch_tail(const Args& a, int n_tiles, int m_tiles, hipStream_t stream) {
+    if constexpr (S::kLoop)
+        if (a.tail)
+            hipLaunchKernelGGL((w8_tail_kernel<TYPE, S, EXPERTS>), dim3(8u * (S::kSlots / 2) * S::kWaves * S::WM * S::WN / 4), dim3(256), 0,
+                               stream, a, n_tiles, m_tiles);
 }
 inline bool even_rows(const Args& a) {
     return a.products ? a.n % 4 == 0 : (((uintptr_t)a.y | (uintptr_t)a.y_stride * 2) & 15) == 0;
@@ -480,7 +592,7 @@ struct Form {
     double start, step, pair, full;
 };
 constexpr Form kForms[kKernels] = {
-    {256, 256, 12.7, 5.6, 1.73, 0.69}, {256, 128, 5.86, 4.9, 1.84, 1.02}, {128, 256, 4.2, 4.3, 1.58, 0.98},
+    {256, 256, 12.7, 5.6, 1.73, 0.69}, {128, 256, 4.2, 4.3, 1.58, 0.98},
     {128, 128, 3.91, 2.27, 2.17, 0.78}, {128, 128, 3.14, 2.42, 1.3, 1.01}, {64, 128, 2.26, 1.67, 1.56, 0.7},
     {64, 64, 2.26, 1.58, 1.3, 0.38},    {32, 32, 2.32, 0.48, 1.24, 0.71},  {16, 16, 1.1, 0.32, 1.84, 1.37},
     {16, 16, 0.26, 0.424, 1.76, 1.16},  {32, 16, 0.46, 0.98, 1.5, 1.24},
@@ -496,6 +608,16 @@ inline double estimate(Kernel kernel, int64_t tiles, int64_t k, int64_t bytes, i
     const double same = kernel == kRows16Few && k % 4096 == 0 ? 1.4 : 1;
     const double t = (f.start + same * f.step * (1 + f.full * fill) * (double)k / 1024) * rounds, memory = (double)bytes / 5.2e6;
     return t > memory ? t + 0.05 * memory : memory + 0.05 * t;      // what is less decides between equal ones
+}
+// What it gains (us) to cut the last of so many tiles of 256 x 256 in parts of k: a part of a round instead of a whole one, for
+// a launch that reads their sums, 256 KB a part.  Measured without and with it: 4096 rows by 4608 x 14336 308 and 240 us, 2048
+// by 2048 x 16384 148 and 80, 6144 by 4096 x 8192 191 and 189, 4096 by 5120 x 4096 99 both.
+inline double tail_gain(int64_t tiles, int64_t k) {
+    const Form& f = kForms[kTile256x256];
+    const int rest = (int)((tiles + 7) / 8 % 32), parts = tail_parts(rest, (int)((k + 127) / 128));
+    if (parts <= 1) return 0;
+    const double whole = 1 + f.full * rest / 32, part = 1 + f.full * rest * parts / 32;
+    return f.step * (whole - part / parts) * (double)k / 1024 - (4 + 0.5 * rest * parts);
 }
 
 }  // namespace w8

@@ -91,6 +91,41 @@ def test_against_the_oracle():
     assert (np.abs(host(y) - ref) <= err + ROUND["fp16"] * (np.abs(ref) + err) + TINY["fp16"]).all()
 
 
+@pytest.mark.parametrize("t,e,top,n,k", [(2100, 2, 2, 2052, 8208), (2100, 2, 1, 2050, 6160), (4500, 3, 2, 1000, 6160),
+                                         (4100, 70, 2, 600, 6160), (9000, 2, 1, 4100, 528)])
+def test_more_tiles_than_compute_units(t, e, top, n, k):
+    """Workgroups that go on from tile to tile, and last tiles in parts of k, with routes that are nobody's."""
+    torch = torch_dev()
+    rng = np.random.default_rng(t + n + k)
+    x, xs, w, ws, chosen = layer(torch, rng, t, e, top, n, k, True, skew=0.5)
+    chosen[rng.integers(0, t, 50)] = -1
+    order, ends, routes, begin = grouped(torch, chosen, e)
+    ref = products(x, xs, w, ws, routes, begin, t * top)
+    there = torch.from_numpy((chosen >= 0).reshape(-1)).cuda()
+    chosen = torch.from_numpy(chosen).cuda()
+    weights = torch.from_numpy(rng.uniform(0, 1, (t, top)).astype(np.float32)).cuda()
+    parts = torch.where(there[:, None], ref, 0.0).view(t, top, n) * weights.double()[..., None]
+    products_bytes = t * top * n * 4
+    first = None
+    for more in (True, False):
+        need = W.w8_experts_matmul_workspace_bytes(t * top, n, False)
+        room = torch.full((need + 16,), 255, dtype=torch.uint8, device="cuda") if more else None
+        y = torch.full((t * top + 1, n), 77.0, dtype=torch.bfloat16, device="cuda")
+        W.w8_experts_matmul(x, xs, w, ws, order, ends, y[:-1], workspace=room)
+        close(y[:-1][there], ref[there], ref[there].abs(), 3, "bf16")
+        assert (y[:-1][~there] == 77).all() and (y[-1] == 77).all()
+        assert room is None or (room[need:] == 255).all()
+        need = W.w8_experts_matmul_workspace_bytes(t * top, n, True) if more else products_bytes
+        room = torch.full((need + 16,), 255, dtype=torch.uint8, device="cuda")
+        out = torch.full((t + 1, n), 77.0, dtype=torch.bfloat16, device="cuda")
+        W.w8_experts_matmul(x, xs, w, ws, order, ends, out[:-1], chosen=chosen, weights=weights, workspace=room[:need])
+        close(out[:-1], parts.sum(1), parts.abs().sum(1), 4 + top, "bf16")
+        assert (out[-1] == 77).all() and (room[need:] == 255).all()
+        if first is None:
+            first = y, out
+        assert torch.equal(first[0], y) and torch.equal(first[1], out), "another workspace gives another result"
+
+
 @pytest.mark.parametrize("t,e", [(5, 3), (90, 2), (400, 5)])
 def test_missing_routes(t, e):
     """Padding tokens, single routes without an expert, and experts without routes."""

@@ -70,6 +70,34 @@ def test_large_tiles(m, n, k):
     check(y, x, xs, w, ws, None, "bf16")
 
 
+@pytest.mark.parametrize("m,n,k,tail", [(2048, 2050, 8192, True), (4050, 4352, 8192, True), (4000, 4300, 6160, True),
+                                        (7000, 6000, 2064, False), (5000, 9000, 1040, False), (7003, 6003, 1040, False)])
+def test_more_tiles_than_compute_units(m, n, k, tail):
+    """Workgroups that go on from tile to tile, and last tiles in parts of k: with rows of results at multiples of 16 bytes
+    and without, in a workspace, without one, and in one that is a byte too small."""
+    torch = torch_dev()
+    rng = np.random.default_rng(m * n + k)
+    x, xs, w, ws = operands(torch, rng, m, n, k)
+    xs *= (1024 / k) ** 0.5
+    bias = half(torch, rng.normal(0, 1, n), "fp16")[0]
+    need = W.w8_matmul_workspace_bytes(m, n, k)
+    assert bool(need) == tail
+    room = torch.full((need + 16,), 255, dtype=torch.uint8, device="cuda")
+    wide = torch.full((m + 2, n + 16), 7.0, dtype=torch.float16, device="cuda")
+    first = None
+    for space in (room[:need], None, room[:max(need - 1, 0)]):
+        wide.fill_(7.0)
+        y = wide[1:m + 1, 8:n + 8]
+        y.fill_(float("nan"))
+        W.w8_matmul(x, xs, w, ws, y, bias=bias, workspace=space)
+        if first is None:
+            check(y, x, xs, w, ws, bias, "fp16")
+            first = y.clone()
+        assert torch.equal(first, y), "another workspace gives another result"
+        assert (wide[0] == 7).all() and (wide[m + 1] == 7).all() and (wide[:, :8] == 7).all() and (wide[:, n + 8:] == 7).all()
+        assert (room[need:] == 255).all()
+
+
 @pytest.mark.parametrize("m", [1, 20, 64, 65, 200])
 def test_against_the_oracle(m):
     torch = torch_dev()
