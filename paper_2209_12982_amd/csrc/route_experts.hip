@@ -54,8 +54,9 @@ template <int TYPE> __device__ inline float load(const void* p, int64_t at) {
 
 // Order of doubles as whole numbers; every number is above 0.
 __device__ inline uint64_t ordered(double v) {
-    const uint64_t b = __builtin_bit_cast(uint64_t, v + 0.0);      // -0 is 0
-    return b >> 63 ? ~b : b | (uint64_t)1 << 63;
+    const u32x2 b = __builtin_bit_cast(u32x2, v + 0.0);             // -0 is 0
+    const uint32_t sign = (uint32_t)((int)b[1] >> 31);
+    return (uint64_t)(b[1] ^ (sign | 0x80000000u)) << 32 | (b[0] ^ sign);
 }
 // The largest of a wave, by moves inside the registers (a shuffle through LDS for each of six steps takes twice as long).
 __device__ inline uint32_t wave_max(uint32_t v) {
@@ -96,9 +97,9 @@ __device__ inline uint32_t ordered(float v) {
 }
 __device__ inline float unordered(uint32_t b) { return __builtin_bit_cast(float, b >> 31 ? b ^ 0x80000000u : ~b); }
 // e^x to 2^-47 of itself: x = n ln 2 + r with |r| <= ln 2 / 2, and the series of e^r to r^11 (the rest is below r^12 / 12! =
-// 6.3e-15).  Half the instructions of the library's function, whose last six bits no choice and no weight needs.
+// 6.3e-15).  Half the instructions of the library's function, whose last six bits no choice and no weight needs.  For |x| up to
+// 800, where e^x is 0 or infinity, and a NaN.
 __device__ inline double exponential(double x) {
-    x = x < -800.0 ? -800.0 : (x > 800.0 ? 800.0 : x);     // 0 and infinity there; a NaN stays
     const double n = __builtin_rint(x * 1.4426950408889634);
     double r = __builtin_fma(n, -0.6931471805599453, x);
     r = __builtin_fma(n, -2.3190468138462996e-17, r);       // ln 2 - 0.6931471805599453
@@ -117,6 +118,17 @@ __device__ inline double exponential(double x) {
     return __builtin_ldexp(p, (int)n);
 }
 
+// 1 / (1 + e^-z): a reciprocal made exact by two steps of Newton's, which need no scaling as the divisor is 1 or more (half the
+// instructions of a division; what is below 2^-1022 may become 0).
+__device__ inline double sigmoid(float z) {
+    const float x = z == z ? __builtin_amdgcn_fmed3f(-z, -800.f, 800.f) : z;
+    const double d = 1.0 + exponential((double)x);
+    double r = __builtin_amdgcn_rcp(d);
+    r = __builtin_fma(r, __builtin_fma(-d, r, 1.0), r);
+    r = __builtin_fma(r, __builtin_fma(-d, r, 1.0), r);
+    return __builtin_amdgcn_div_fixup(r, d, 1.0);           // infinity and NaN
+}
+
 // What is not a number counts as minus infinity.
 __device__ inline double number(double v) { return v == v ? v : -__builtin_inf(); }
 
@@ -131,7 +143,7 @@ __device__ inline void route(const RouteArgs& a, const float (&z)[J], const floa
     double s[J];
     if (a.sigmoid) {
 #pragma unroll
-        for (int j = 0; j < J; ++j) s[j] = 1.0 / (1.0 + exponential(-(double)z[j]));
+        for (int j = 0; j < J; ++j) s[j] = sigmoid(z[j]);
     } else {
         // a NaN is left out of the maximum, and makes the sum and with it all scores NaN
         uint32_t most = 0;
@@ -142,7 +154,8 @@ __device__ inline void route(const RouteArgs& a, const float (&z)[J], const floa
         double sum = 0.0;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            s[j] = lane * J + j < a.experts ? exponential((double)z[j] - top) : 0.0;
+            const double x = (double)z[j] - top;
+            s[j] = lane * J + j < a.experts ? exponential(x < -800.0 ? -800.0 : x) : 0.0;
             sum += s[j];
         }
         const double part = 1.0 / wave_sum(sum);
