@@ -10,7 +10,8 @@
 // is a half is no less than it: R takes halves up.
 //
 // Memory bounds it: 2 bytes read and 1 written a value.  A workgroup takes a
-// row and holds it in registers between the maximum and the codes.
+// row and holds it in registers between the maximum and the codes.  2048 rows
+// of 16384: 24 us, 4.2 TB/s.
 #include <hip/hip_runtime.h>
 
 #include "mx4.h"

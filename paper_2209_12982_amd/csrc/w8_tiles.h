@@ -5,6 +5,9 @@
 // ahead; the copies fill LDS densely, so the 16-byte pieces of a row are exchanged (swap) such that sixteen rows' reads of
 // the same piece fall into the sixteen columns of the 256-byte banks.  Within 32 rows of weights the copy puts row
 // 16 h + 4 q + e where operand row 8 q + 4 h + e is read: a lane's sixteen sums are then neighbouring outputs of one row.
+//
+// Measured: 8192 rows by 16384 x 4096 482 to 490 us, 2.25 to 2.28 POP/s, at the 1.6 to 1.7 GHz that the load leaves of the
+// clock; 2048 by 4096 x 16384 132 us, 2.08 POP/s; 48 by 16384 x 4096 13.2 us, bound by the weights' bytes.
 #pragma once
 #include <type_traits>
 
