@@ -691,7 +691,7 @@ wino_status prompt_attention(const void* q, int64_t q_stride, const void* k, int
  * its products are NaN.  Weights are quantized by the same call, a row an
  * output.
  *   x        [m][k], row stride x_stride >= k;  codes: int8 [m][k], dense;
- *   scales   fp32 [m].  k a multiple of 16.
+ *   scales   fp32 [m].  k a multiple of 16, m below 2^24.
  */
 wino_status w8_quantize(const void* x, int64_t x_stride, int8_t* codes, float* scales, int32_t m, int32_t k,
                         wino_float_type type, hipStream_t stream);

@@ -134,6 +134,7 @@ extern "C" wino_status w8_quantize(const void* x, int64_t x_stride, int8_t* code
     if (m == 0) return WINO_OK;
     if (!scales || (k > 0 && (!x || !codes))) return WINO_EINVAL;
     if (m > 1 && x_stride < k) return WINO_EINVAL;
+    if (m >= 1 << 24) return WINO_EUNSUPPORTED;             // a launch counts its threads in 32 bits
     if (!aligned16(x) || !aligned16(codes) || ((uintptr_t)scales & 3) || (k > 0 && m > 1 && (x_stride & 7))) return WINO_EUNSUPPORTED;
     const QuantizeArgs a = {x, codes, scales, x_stride, k};
     type == WINO_BF16 ? launch<WINO_BF16>(a, m, stream) : launch<WINO_FP16>(a, m, stream);

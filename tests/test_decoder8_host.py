@@ -28,7 +28,7 @@ def test_quantize_refusals():
 
     for kw, want in (({"kind": 2}, -1), ({"kind": -1}, -1), ({"m": -1}, -1), ({"k": -16}, -1), ({"k": 40}, -1), ({"x": None}, -1),
                      ({"codes": None}, -1), ({"scales": None}, -1), ({"xs": 48}, -1), ({"xs": 68}, -2), ({"x": p + 8}, -2),
-                     ({"codes": p + 8}, -2), ({"scales": p + 2}, -2), ({"m": 0}, 0), ({"m": 0, "x": None}, 0)):
+                     ({"codes": p + 8}, -2), ({"scales": p + 2}, -2), ({"m": 1 << 24}, -2), ({"m": 0}, 0), ({"m": 0, "x": None}, 0)):
         assert call(**kw) == want, kw
 
 
