@@ -96,7 +96,7 @@ template <class S, bool EXPERTS> __device__ inline List list_of(const Args& a, i
             count_tiles<S::kRows>(a, e0, begin, end, count, upto);
             tiles += __builtin_amdgcn_readlane(upto, 63);
         }
-        tiles *= n_tiles;
+        tiles = min(tiles, m_tiles) * n_tiles;              // more only where ends are not in order
     }
     const int each = (tiles + 7) / 8;
     List l;
@@ -125,7 +125,7 @@ template <class S, bool EXPERTS> __device__ inline void locate(const Args& a, in
     for (int e0 = 0; e0 < a.experts; e0 += 64) {
         int begin, end, count, upto;
         count_tiles<S::kRows>(a, e0, begin, end, count, upto);
-        const uint64_t here = __ballot(index < (before + upto) * n_tiles);
+        const uint64_t here = __ballot(index < min(before + upto, m_tiles) * n_tiles);
         if (here) {
             const int l = __builtin_ctzll(here), tiles = __builtin_amdgcn_readlane(count, l);
             const int in = index - (before + __builtin_amdgcn_readlane(upto, l) - tiles) * n_tiles;
@@ -369,7 +369,7 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
             // the second result; a row's first and last one, where they are left, follow for all rows together.
             constexpr int kWords = kRow / 4, kEach = 4 / (int)sizeof(E);
             const int valid = min(a.n - col0, 32 * BLOCKS);
-            auto odd = [&](int r) { return kEach == 2 ? ((int)((uintptr_t)out >> 1) + r * (int)stride + col0) & 1 : 0; };
+            auto odd = [&](int r) { return kEach == 2 ? (int)(((uint32_t)((uintptr_t)out >> 1) + (uint32_t)r * (uint32_t)stride + (uint32_t)col0) & 1) : 0; };
 #pragma unroll 1
             for (int i0 = 0; i0 < 32 * kWords / 64; i0 += 8) {
                 uint32_t v[8];

@@ -177,6 +177,25 @@ def test_orders_out_of_range(t):
         assert (memory[0] == 77).all() and (memory[t + 1] == 77).all()
 
 
+@pytest.mark.parametrize("t,e,n,k", [(40, 9, 70, 96), (700, 70, 130, 64), (4200, 5, 1000, 6160), (4200, 2, 2052, 8208)])
+def test_ends_that_go_back(t, e, n, k):
+    """Every other expert claims all routes: more tiles than routes can have, in the lists of the XCDs and in the parts of the
+    last ones.  Nothing outside is read or written."""
+    torch = torch_dev()
+    rng = np.random.default_rng(t + n)
+    x, xs, w, ws, chosen = layer(torch, rng, t, e, 1, n, k, True)
+    order, ends, routes, begin = grouped(torch, chosen, e)
+    bad = torch.tensor([0, t] * (e // 2 + 1), dtype=torch.int32, device="cuda")[:e + 1].contiguous()
+    need = W.w8_experts_matmul_workspace_bytes(t, n, False)
+    room = torch.full((need + 16,), 255, dtype=torch.uint8, device="cuda")
+    memory = torch.full((t + 2, n), 77.0, dtype=torch.float16, device="cuda")
+    W.w8_experts_matmul(x, xs, w, ws, order, bad, memory[1:t + 1], workspace=room[:need])
+    assert (memory[0] == 77).all() and (memory[t + 1] == 77).all() and (room[need:] == 255).all()
+    W.w8_experts_matmul(x, xs, w, ws, order, ends, memory[1:t + 1], workspace=room[:need])
+    ref = products(x, xs, w, ws, routes, begin, t)
+    close(memory[1:t + 1], ref, ref.abs(), 3, "fp16")
+
+
 @pytest.mark.parametrize("t", [8, 500])
 def test_strided_rows_and_neighbours(t):
     torch = torch_dev()
