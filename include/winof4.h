@@ -729,7 +729,7 @@ typedef enum wino_score { WINO_SCORE_SOFTMAX = 0, WINO_SCORE_SIGMOID = 1 } wino_
  *   chosen s with `normalise` (0 where that is 0), times scale.  A NaN among
  *   the s that a weight is made of makes it NaN; the choice is valid all the same.
  * Everything up to the weights is held in 64 bits, because a choice hangs on
- * the difference of two values.
+ * the difference of two values; a sigmoid below 2^-1022 may count as 0.
  *   logits   [tokens][experts] bf16, fp16 or fp32, row stride `stride`, any
  *            alignment of whole numbers
  *   bias     fp32 [experts] or NULL

@@ -29,7 +29,7 @@ using namespace mx4;
 
 constexpr int kMostExperts = 1024, kMostTop = 32, kMostGroups = 64;
 constexpr int kTokens = 32;             // of a block at most
-constexpr int kAlone = 64;              // that one block takes by itself
+constexpr int kAlone = 32;              // that one block takes by itself at most
 constexpr int kWaveRoutes = 128;        // that a wave places
 constexpr int kFewBlocks = 16;          // whose counts each block adds up by itself: shorter than a launch between
 
@@ -44,9 +44,9 @@ struct RouteArgs {
     int32_t group_lanes;    // that a group has: the largest power of two, all groups in a wave
     float scale;
     winof4::FastDiv by_size;
-    // the order, or null; counts: [experts][blocks], later what comes before a block; totals: [experts]
+    // the order, or null; counts: [experts][row_blocks], later what comes before a block; totals: [experts]
     int32_t *order, *ends, *counts, *totals;
-    int32_t blocks, block_tokens;
+    int32_t blocks, block_tokens, row_blocks;
 };
 
 template <int TYPE> __device__ inline float load(const void* p, int64_t at) {
@@ -361,16 +361,17 @@ constexpr int waves_of(int j) { return j <= 2 ? 16 : (j <= 8 ? 8 : 4); }
 
 // A block of tokens.  ALONE: it is the only one, and its order follows at once; else its counts.
 template <int TYPE, int J, bool ALONE> __global__ __launch_bounds__(64 * waves_of(J)) void route_experts_kernel(RouteArgs a) {
-    constexpr int kWaves = waves_of(J);
+    constexpr int kMost = waves_of(J);
+    const int waves = ALONE ? kMost : (int)blockDim.x / 64;
     extern __shared__ __attribute__((aligned(16))) double room[];                        // of each wave; the order's counts
-    __shared__ int32_t scan[kWaves];
+    __shared__ int32_t scan[kMost];
     __shared__ int16_t picked[ALONE ? kAlone * kMostTop : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int own = J * 64 * (a.top_groups < a.groups ? 2 : 1);
-    int32_t* count = (int32_t*)(room + (ALONE ? 0 : kWaves * own));
+    int32_t* count = (int32_t*)(room + (ALONE ? 0 : waves * own));
     const bool counts = !ALONE && a.ends;
     if (counts) {
-        for (int e = threadIdx.x; e < a.experts; e += 64 * kWaves) count[e] = 0;
+        for (int e = threadIdx.x; e < a.experts; e += 64 * waves) count[e] = 0;
         __syncthreads();
     }
     const int64_t t0 = ALONE ? 0 : (int64_t)blockIdx.x * a.block_tokens, t1 = ALONE || t0 + a.block_tokens > a.tokens ? a.tokens : t0 + a.block_tokens;
@@ -387,10 +388,10 @@ template <int TYPE, int J, bool ALONE> __global__ __launch_bounds__(64 * waves_o
     fetch(t0 + wave, ahead);
 #pragma unroll
     for (int j = 0; j < J; ++j) bias[j] = a.bias && lane * J + j < a.experts ? a.bias[lane * J + j] : 0.f;
-    for (int64_t token = t0 + wave; token < t1; token += kWaves) {
+    for (int64_t token = t0 + wave; token < t1; token += waves) {
 #pragma unroll
         for (int j = 0; j < J; ++j) z[j] = ahead[j];
-        fetch(token + kWaves, ahead);
+        fetch(token + waves, ahead);
         int mine = -1;
         float weight = 0.f;
         if (token < live) route<TYPE, J>(a, z, bias, room + wave * own, mine, weight);
@@ -404,15 +405,15 @@ template <int TYPE, int J, bool ALONE> __global__ __launch_bounds__(64 * waves_o
     if (!a.ends) return;
     __syncthreads();
     if constexpr (ALONE) {
-        place<kWaves, false>(a, 0, (int)t1 * a.top, count, scan, [&](int r) { return (int)picked[r]; },
+        place<kMost, false>(a, 0, (int)t1 * a.top, count, scan, [&](int r) { return (int)picked[r]; },
                       [&](int e) {
                           int n = 0;
-                          for (int w = 0; w < kWaves; ++w) n += count[w * a.experts + e];
+                          for (int w = 0; w < kMost; ++w) n += count[w * a.experts + e];
                           return n;
                       },
                       [](int) { return 0; }, true);
     } else {
-        for (int e = threadIdx.x; e < a.experts; e += 64 * kWaves) a.counts[(int64_t)e * a.blocks + blockIdx.x] = count[e];
+        for (int e = threadIdx.x; e < a.experts; e += 64 * waves) a.counts[(int64_t)e * a.row_blocks + blockIdx.x] = count[e];
     }
 }
 
@@ -459,11 +460,11 @@ template <int WAVES> __global__ __launch_bounds__(64 * WAVES) void route_place_k
         for (int j = 0; j < kEach; ++j) {
             const int e = kEach * (int)threadIdx.x + j;
             if (e >= a.experts) break;
-            const int32_t* p = a.counts + (int64_t)e * a.blocks;
-#pragma unroll 8
-            for (int b = 0; b < a.blocks; ++b) {
+            const int32_t* p = a.counts + (int64_t)e * kFewBlocks;
+#pragma unroll
+            for (int b = 0; b < kFewBlocks; ++b) {          // read whole, in wide loads; what no block wrote counts nothing
                 const int n = p[b];
-                all[j] += n;
+                all[j] += b < a.blocks ? n : 0;
                 before[j] += b < (int)blockIdx.x ? n : 0;
             }
         }
@@ -480,13 +481,14 @@ template <int WAVES> __global__ __launch_bounds__(64 * WAVES) void route_place_k
 }
 
 template <int TYPE, int J> void launch(const RouteArgs& a, hipStream_t stream) {
-    const size_t room = (size_t)waves_of(J) * (J * 64) * (a.top_groups < a.groups ? 2 : 1) * sizeof(double);
-    const dim3 block(64 * waves_of(J));
-    if (a.blocks == 1)
-        hipLaunchKernelGGL((route_experts_kernel<TYPE, J, true>), dim3(1), block,
-                           std::max(room, waves_of(J) * a.experts * sizeof(int32_t)), stream, a);
+    const bool alone = a.blocks == 1 && a.ends;
+    const int waves = alone ? waves_of(J) : std::min(waves_of(J), a.block_tokens);
+    const size_t room = (size_t)waves * (J * 64) * (a.top_groups < a.groups ? 2 : 1) * sizeof(double);
+    if (alone)
+        hipLaunchKernelGGL((route_experts_kernel<TYPE, J, true>), dim3(1), dim3(64 * waves),
+                           std::max(room, waves * a.experts * sizeof(int32_t)), stream, a);
     else
-        hipLaunchKernelGGL((route_experts_kernel<TYPE, J, false>), dim3((unsigned)a.blocks), block,
+        hipLaunchKernelGGL((route_experts_kernel<TYPE, J, false>), dim3((unsigned)a.blocks), dim3(64 * waves),
                            room + (a.ends ? a.experts * sizeof(int32_t) : 0), stream, a);
 }
 // Experts that a lane holds.
@@ -509,12 +511,15 @@ void launch_place(const RouteArgs& a, hipStream_t stream) {
 }
 
 bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
-// Tokens of a block: few are taken one by a wave (512 tokens to 8 of 256: 16 us with four one after the other), many as the
-// launches after it would have them.
-int block_tokens(int64_t tokens, int experts, int top) {
-    const int waves = waves_of(lane_experts(experts));
-    if (tokens <= kAlone && tokens * top <= kWaveRoutes * waves) return kAlone;
-    int n = waves;
+// Tokens of a block.  Few are routed and put in order by one block: one to a wave, or two where a lane has one expert (us, one
+// launch and two: 24 tokens to 6 of 64 6.7 and 8.7, 64 to 4 of 64 11.3 and 7.9, 32 to 8 of 256 16.3 and 9.4).  More are spread
+// over as many blocks as need no launch for their sums, then taken one by a wave (512 tokens to 8 of 256: 16 us with four one
+// after the other), and many as the launches after it would have them.
+int block_tokens(int64_t tokens, int experts) {
+    const int each = lane_experts(experts), waves = waves_of(each);
+    if (tokens <= waves * (each == 1 ? 2 : 1)) return kAlone;
+    int n = 4;
+    while (n < waves && tokens > kFewBlocks * n) n *= 2;
     while (n < kTokens && tokens > 256 * n) n *= 2;
     return n;
 }
@@ -523,9 +528,9 @@ int block_tokens(int64_t tokens, int experts, int top) {
 
 extern "C" size_t route_experts_workspace_bytes(int32_t tokens, int32_t experts, int32_t top) {
     if (tokens < 1 || experts < 1 || top < 1 || experts > kMostExperts || top > kMostTop || (int64_t)tokens * top > 1 << 22) return 0;
-    const int n = block_tokens(tokens, experts, top);
+    const int n = block_tokens(tokens, experts);
     const int64_t blocks = (tokens + (int64_t)n - 1) / n;
-    return blocks == 1 ? 0 : (size_t)(blocks + 1) * experts * sizeof(int32_t);
+    return blocks == 1 ? 0 : (size_t)(blocks <= kFewBlocks ? kFewBlocks : blocks + 1) * experts * sizeof(int32_t);
 }
 
 extern "C" wino_status route_experts(const void* logits, int64_t stride, const float* bias, int32_t tokens, int32_t experts,
@@ -550,10 +555,11 @@ extern "C" wino_status route_experts(const void* logits, int64_t stride, const f
     const size_t need = route_experts_workspace_bytes(tokens, experts, top);
     if (ends && need > 0 && (!workspace || workspace_bytes < need)) return WINO_EINVAL;
     if (tokens == 0 && !ends) return WINO_OK;
-    const int32_t n = block_tokens(tokens, experts, top), blocks = (int32_t)((tokens + (int64_t)n - 1) / n);
+    // without an order few tokens are spread as far as they go (32 tokens to 8 of 256: 4.8 us, by one block 14.5)
+    const int32_t n = ends || tokens > 4096 ? block_tokens(tokens, experts) : 4, blocks = (int32_t)((tokens + (int64_t)n - 1) / n);
     RouteArgs a = {logits, bias, live, chosen, weights, stride, tokens, experts, top, groups, experts / groups, top_groups,
                    group_best, score == WINO_SCORE_SIGMOID, normalise, 1, scale, winof4::make_fastdiv((uint32_t)(experts / groups)),
-                   order, ends, nullptr, nullptr, blocks, n};
+                   order, ends, nullptr, nullptr, blocks, n, std::max(blocks, kFewBlocks)};
     while (2 * a.group_lanes * groups <= 64) a.group_lanes *= 2;
     if (blocks > 1 && ends) a.counts = (int32_t*)workspace;
     if (blocks > kFewBlocks && ends) a.totals = a.counts + (int64_t)blocks * experts;

@@ -60,7 +60,7 @@ def test_route_refusals():
                                  ends, kind, ws, wb, None)
 
     need = W.route_experts_workspace_bytes(65, 8, 2)
-    assert need > 0 and W.route_experts_workspace_bytes(64, 8, 2) == 0
+    assert need > 0 and W.route_experts_workspace_bytes(32, 8, 2) == 0
     for kw, want in (({"kind": 3}, -1), ({"kind": -1}, -1), ({"score": 2}, -1), ({"t": -1}, -1), ({"e": 0}, -1), ({"top": 0}, -1),
                      ({"top": 9}, -1), ({"g": 0}, -1), ({"g": 3}, -1), ({"g": 4, "tg": 5}, -1), ({"tg": 0}, -1),
                      ({"g": 4, "tg": 2, "top": 5}, -1), ({"best": 0}, -1), ({"best": 3}, -1), ({"g": 8, "tg": 2, "best": 2}, -1),

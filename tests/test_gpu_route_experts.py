@@ -70,6 +70,20 @@ def test_route(t, e, top, score, name):
     check(values, run(torch, logits, top, **how), top, **how)
 
 
+@pytest.mark.parametrize("t", [2, 4, 5, 8, 9, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 300])
+@pytest.mark.parametrize("e,top", [(60, 6), (128, 3), (250, 8), (400, 2), (1000, 5)])
+def test_numbers_of_tokens(t, e, top):
+    """One block or several, with and without their sums in a launch of their own, a last block that is not full, padding."""
+    torch = torch_dev()
+    rng = np.random.default_rng(t * 31 + e + top)
+    logits, values = logits_of(torch, rng, t, e, "fp16")
+    live = t - t // 5
+    got = run(torch, logits, top, live=live)
+    check(values, got, top, live=live)
+    alone = run(torch, logits, top, live=live, ordered=False)
+    assert (alone[0] == got[0]).all() and (alone[1] == got[1]).all()
+
+
 @pytest.mark.parametrize("score", [W.SCORE_SOFTMAX, W.SCORE_SIGMOID])
 @pytest.mark.parametrize("t,groups,size,top_groups,best,top", [(50, 8, 32, 4, 2, 8), (20, 2, 2, 1, 2, 2), (9, 64, 2, 5, 2, 7),
                                                                (17, 8, 60, 3, 1, 8), (13, 3, 7, 2, 2, 14), (5, 64, 16, 63, 1, 32),
