@@ -57,6 +57,8 @@ Kernel choose(int64_t routes, int64_t experts, int64_t n, int64_t k, bool tail) 
         if (i >= kRows16 && each > 16) break;
         const double tiles = each > f.rows ? each / f.rows + 0.5 : 1;
         const int64_t all = (int64_t)(tiles * (double)(used * ((n + f.outs - 1) / f.outs)));
+        // uneven routes have more tiles than that, and one more than 256 would cost these a second round
+        if (f.pair == 0 && all > 200) continue;
         double t = estimate((Kernel)i, all, k, used * n * k, (int64_t)std::min(each, 16.0));
         // tiles whose last ones are cut in parts of k take a part of the last round, and their join 20 us
         if (i == kTile256x256 && tail)
@@ -78,6 +80,9 @@ template <int TYPE> void pick(const Args& a, int64_t x_rows, hipStream_t stream)
         case kTile64x128: return launch_tiles<TYPE, Tile64x128>(a, stream);
         case kTile64x64: return launch_tiles<TYPE, Tile64x64>(a, stream);
         case kTile32x32: return launch_tiles<TYPE, Tile32x32>(a, stream);
+        case kShared64x128: return launch_tiles<TYPE, Shared64x128>(a, stream);
+        case kShared64x64: return launch_tiles<TYPE, Shared64x64>(a, stream);
+        case kShared64x32: return launch_tiles<TYPE, Shared64x32>(a, stream);
         case kRows16: return launch_rows<TYPE, 1, 16>(a, stream);
         case kRows16Few: return launch_rows<TYPE, 1, 8>(a, stream);
         default: return launch_rows<TYPE, 2, 4>(a, stream);

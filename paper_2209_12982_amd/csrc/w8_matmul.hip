@@ -58,6 +58,7 @@ Cut cut(int64_t m, int64_t n, int64_t k) {
         const int64_t tiles = (n + f.outs - 1) / f.outs * ((m + f.rows - 1) / f.rows);
         for (const int parts : {1, 2, 4, 8, 16}) {
             if (parts > 1 && (i >= kRows16 || k < 1024 * parts || parts * m * n > 1 << 22)) break;
+            if (f.pair == 0 && tiles * parts > 256) break;
             const double join = parts > 1 ? 1.95 + 0.17 * parts + 1.3e-6 * (double)(parts * m * n) : 0;
             double t = estimate((Kernel)i, tiles * parts, k / parts, n * k, m) + join;
             if (i == kTile256x256 && parts == 1) t -= std::max(tail_gain(tiles, k), 0.0);
@@ -92,6 +93,9 @@ template <int TYPE> void pick(Args a, size_t bytes, hipStream_t stream) {
         case kTile64x128: return launch_tiles<TYPE, Tile64x128>(a, parts, stream);
         case kTile64x64: return launch_tiles<TYPE, Tile64x64>(a, parts, stream);
         case kTile32x32: return launch_tiles<TYPE, Tile32x32>(a, parts, stream);
+        case kShared64x128: return launch_tiles<TYPE, Shared64x128>(a, parts, stream);
+        case kShared64x64: return launch_tiles<TYPE, Shared64x64>(a, parts, stream);
+        case kShared64x32: return launch_tiles<TYPE, Shared64x32>(a, parts, stream);
         case kRows16: return launch_rows<TYPE, 1, 16>(a, stream);
         case kRows16Few: return launch_rows<TYPE, 1, 8>(a, stream);
         default: return launch_rows<TYPE, 2, 4>(a, stream);

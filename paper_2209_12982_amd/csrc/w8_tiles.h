@@ -561,8 +561,13 @@ typedef Tile<2, 1, 2, 4, 1, 128, 2> Pair128x128;
 typedef Tile<1, 1, 2, 4, 1, 128, 3> Tile64x128;
 typedef Tile<1, 1, 2, 2, 1, 128, 3> Tile64x64;
 typedef Tile<1, 1, 1, 1, 4, 256, 4> Tile32x32;
+// Sums shared out to two or four waves: a compute unit that has one tile needs more waves than its blocks of 32 x 32 give (200
+// rows by 4096 x 4096: 64 x 64 11.1 us, by twice the waves 9.2; 128 by 4096 x 8192, 64 x 32 by four times 12.1).
+typedef Tile<1, 1, 2, 4, 2, 256, 3> Shared64x128;
+typedef Tile<1, 1, 2, 2, 2, 256, 3> Shared64x64;
+typedef Tile<1, 1, 2, 1, 4, 256, 4> Shared64x32;
 // They, and rows alone (w8_rows.h): 16 outputs by 16 or 8 waves, 32 outputs by 4.
-enum Kernel { kTile256x256, kTile128x256, kTile128x128, kPair128x128, kTile64x128, kTile64x64, kTile32x32, kRows16, kRows16Few, kRows32, kKernels };
+enum Kernel { kTile256x256, kTile128x256, kTile128x128, kPair128x128, kTile64x128, kTile64x64, kTile32x32, kShared64x128, kShared64x64, kShared64x32, kRows16, kRows16Few, kRows32, kKernels };
 
 // Workgroups for so many tiles: as many for each XCD, one for each of 256 compute units where they go on.  With rows of
 // results that do not begin at multiples of 16 bytes they do not: a workgroup that goes on waits for its stores.
@@ -587,9 +592,11 @@ inline bool even_rows(const Args& a) {
 inline bool far(int64_t rows, int64_t stride, int64_t k) { return (rows - 1) * stride + k > (int64_t)0xffffffff; }
 
 // What a kernel takes (us): `start` beside the loop, `step` for 1024 of k, `step` times 1 + `full` with a workgroup on each
-// of the 256 compute units (rows: with 16 rows), and `pair` times that for two workgroups each.  Chosen for 900 measured calls
-// of 1 to 8192 rows, 64 to 32768 outputs and k of 128 to 16384 such that the kernel of the shortest estimate is as near to the
-// shortest measured one as they go: 1.6% longer on average, 37% at most (1 row by 8192 x 16384: 29.4 us, 21.6 in tiles of 32 x 32).
+// of the 256 compute units (rows: with 16 rows), and `pair` times that for two workgroups each (0: not for so many).  Chosen
+// for 900 measured calls of 1 to 8192 rows, 64 to 32768 outputs and k of 128 to 16384 such that the kernel of the shortest
+// estimate is as near to the shortest measured one as they go: 1.6% longer on average, 37% at most (1 row by 8192 x 16384: 29.4
+// us, 21.6 in tiles of 32 x 32).  Those whose sums are shared out, for 330 more: of 400 others 122 take them then, in 0.94 of
+// the time without them on average, 0.77 to 1.17.
 struct Form {
     int outs, rows;
     double start, step, pair, full;
@@ -597,7 +604,8 @@ struct Form {
 constexpr Form kForms[kKernels] = {
     {256, 256, 12.7, 5.6, 1.73, 0.69}, {128, 256, 4.2, 4.3, 1.58, 0.98},
     {128, 128, 3.91, 2.27, 2.17, 0.78}, {128, 128, 3.14, 2.42, 1.3, 1.01}, {64, 128, 2.26, 1.67, 1.56, 0.7},
-    {64, 64, 2.26, 1.58, 1.3, 0.38},    {32, 32, 2.32, 0.48, 1.24, 0.71},  {16, 16, 1.1, 0.32, 1.84, 1.37},
+    {64, 64, 2.26, 1.58, 1.3, 0.38},    {32, 32, 2.32, 0.48, 1.24, 0.71},  {64, 128, 3.7, 1.13, 0, 0.62},
+    {64, 64, 2.8, 1.2, 0, 0.19},        {64, 32, 2.94, 0.716, 0, 0.2},     {16, 16, 1.1, 0.32, 1.84, 1.37},
     {16, 16, 0.26, 0.424, 1.76, 1.16},  {32, 16, 0.46, 0.98, 1.5, 1.24},
 };
 // The time of a kernel that has so many tiles, for k of a part and so many bytes of weights.

@@ -40,7 +40,8 @@ def check(y, x, xs, w, ws, bias, name):
 SIZES = [(1, 1, 16), (1, 17, 64), (1, 4096, 4096), (2, 16, 96), (3, 33, 160), (5, 203, 2080), (8, 64, 512), (15, 130, 1024),
          (16, 48, 4096), (17, 100, 544), (33, 31, 256), (48, 129, 1040), (64, 257, 2064), (1, 40, 16384), (31, 64, 131056),
          (65, 7, 48), (70, 20, 128), (100, 300, 1008), (128, 128, 128), (129, 127, 4096), (333, 1003, 2080), (257, 520, 144),
-         (300, 16, 16), (1000, 64, 8192), (90, 2500, 16400), (2050, 1030, 112)]
+         (300, 16, 16), (1000, 64, 8192), (90, 2500, 16400), (2050, 1030, 112), (200, 4090, 4112), (128, 4101, 8208), (333, 5003, 2080),
+         (340, 500, 16400), (150, 1001, 16384)]
 
 
 @pytest.mark.parametrize("name", ["bf16", "fp16"])
