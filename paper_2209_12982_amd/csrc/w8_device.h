@@ -34,6 +34,8 @@ struct Args {
     float* products;        // [routes][n] where they are added up with weights, or null
 };
 
+typedef u32x4 __attribute__((aligned(2))) Anywhere;      // 16 bytes that begin at any 16-bit number
+
 constexpr int kMostParts = 8;           // of k, of the last tiles
 
 __device__ const uint32_t kZeros[4] = {0, 0, 0, 0};     // what lies behind the end of k

@@ -356,46 +356,22 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
             for (int p = 0; p < kBlock / 32; ++p) *(u32x4*)at(c, i * kBlock + half * (kBlock / 2) + 16 * p) = put(i0 + i, p);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         const int* to_row = out_row[set] + 32 * (S::WM * wm + j);
-        if (col0 + 32 * BLOCKS <= a.n && (((uintptr_t)out | (uintptr_t)stride * sizeof(E)) & 15) == 0) {
+        // 16 bytes a lane at any alignment: a row of results may begin anywhere
+        const int valid = (a.n - col0) * (int)sizeof(E);    // bytes of a row
 #pragma unroll
-            for (int i = 0; i < 32 * kRow / 1024; ++i) {
-                const int p = 16 * (64 * i + lane), row = p / kRow, byte = p % kRow;
-                const u32x4 v = *(const u32x4*)at(row, byte);
-                if (to_row[row] >= 0) *(u32x4*)((uint8_t*)(out + to_row[row] * stride + col0) + byte) = v;
-            }
-        } else {
-            // Rows that do not begin at multiples of 16 bytes, or end inside: four neighbouring bytes a lane, eight of them read
-            // before the first is stored.  Of rows of 2-byte results that begin at an odd multiple of two bytes, these begin with
-            // the second result; a row's first and last one, where they are left, follow for all rows together.
-            constexpr int kWords = kRow / 4, kEach = 4 / (int)sizeof(E);
-            const int valid = min(a.n - col0, 32 * BLOCKS);
-            auto odd = [&](int r) { return kEach == 2 ? (int)(((uint32_t)((uintptr_t)out >> 1) + (uint32_t)r * (uint32_t)stride + (uint32_t)col0) & 1) : 0; };
-#pragma unroll 1
-            for (int i0 = 0; i0 < 32 * kWords / 64; i0 += 8) {
-                uint32_t v[8];
-                int r[8], from[8];
+        for (int i = 0; i < 32 * kRow / 1024; ++i) {
+            const int p = 16 * (64 * i + lane), row = p / kRow, byte = p % kRow, r = to_row[row];
+            const u32x4 v = *(const u32x4*)at(row, byte);
+            if (r < 0 || byte >= valid) continue;
+            uint8_t* to = (uint8_t*)(out + r * stride + col0) + byte;
+            if (byte + 16 <= valid) {
+                *(Anywhere*)to = v;
+            } else {                                        // the end of a row
+                typedef __attribute__((ext_vector_type(16 / sizeof(E)))) E Many;
+                const Many all = __builtin_bit_cast(Many, v);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int p = 64 * (i0 + i) + lane, row = p / kWords, word = p % kWords;
-                    r[i] = to_row[row];
-                    v[i] = *(const uint32_t*)at(row, 4 * word);
-                    from[i] = kEach * word;
-                    if constexpr (kEach == 2) {
-                        const uint32_t before = *(const uint32_t*)at(row, 4 * max(word - 1, 0));
-                        if (odd(r[i])) {
-                            v[i] = __builtin_amdgcn_alignbyte(v[i], before, 2);
-                            from[i] -= 1;
-                        }
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (r[i] >= 0 && from[i] >= 0 && from[i] + kEach <= valid) *(uint32_t*)(out + r[i] * stride + col0 + from[i]) = v[i];
-            }
-            if constexpr (kEach == 2) {
-                const int r = to_row[c], first = odd(r);
-                const int one = half ? ((valid - first) & 1 ? valid - 1 : -1) : (first ? 0 : -1);
-                if (r >= 0 && one >= 0) out[r * stride + col0 + one] = *(const E*)at(c, one * (int)sizeof(E));
+                for (int e = 0; e < 16 / (int)sizeof(E); ++e)
+                    if (byte + (e + 1) * (int)sizeof(E) <= valid) ((E*)to)[e] = all[e];
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
