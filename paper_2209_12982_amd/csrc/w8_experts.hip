@@ -9,24 +9,36 @@ namespace {
 using namespace w8;
 
 // out[t] = sum_j weights[t][j] products[t top + j], in the order of j; routes without an expert add nothing.  Memory bounds
-// it; COLS columns a thread, four where rows of products begin at multiples of 16 bytes (2000 tokens, two routes each, 4096
-// outputs: 14 us for 27 with one, 5.8 TB/s of products that are in the last-level cache).
-template <int TYPE, int COLS>
-__global__ __launch_bounds__(256) void w8_combine_kernel(Args a, const int32_t* chosen, const float* weights, int top) {
+// it: four columns a thread (2000 tokens, two routes each, 4096 outputs: 14 us for 27 with one, 5.8 TB/s of products that are
+// in the last-level cache).
+template <int TYPE> __global__ __launch_bounds__(256) void w8_combine_kernel(Args a, const int32_t* chosen, const float* weights, int top) {
     typedef typename Half<TYPE>::type T;
-    typedef __attribute__((ext_vector_type(COLS))) float Row;
-    const int col = ((int)blockIdx.y * 256 + (int)threadIdx.x) * COLS;
+    typedef __attribute__((ext_vector_type(4), aligned(4))) float Row;      // rows may begin at any number
+    typedef __attribute__((ext_vector_type(4), aligned(2))) T Out;
+    const int col = ((int)blockIdx.y * 256 + (int)threadIdx.x) * 4;
     const int64_t token = blockIdx.x;
     if (col >= a.n) return;
-    Row sum = {};
+    const bool whole = col + 4 <= a.n;
+    f32x4 sum = {};
 #pragma unroll 4
     for (int j = 0; j < top; ++j) {
         const int64_t route = token * top + j;
-        if ((uint32_t)chosen[route] < (uint32_t)a.experts) sum += weights[route] * *(const Row*)(a.products + route * a.n + col);
+        if ((uint32_t)chosen[route] >= (uint32_t)a.experts) continue;
+        const float* from = a.products + route * a.n + col;
+        f32x4 p = {};
+        if (whole)
+            p = *(const Row*)from;
+        else
+            for (int e = 0; e < 3; ++e)
+                if (col + e < a.n) p[e] = from[e];
+        sum += weights[route] * p;
     }
     T* to = (T*)a.y + token * a.y_stride + col;
-#pragma unroll
-    for (int e = 0; e < COLS; ++e) to[e] = (T)sum[e];
+    if (whole)
+        *(Out*)to = Out{(T)sum[0], (T)sum[1], (T)sum[2], (T)sum[3]};
+    else
+        for (int e = 0; e < 3; ++e)
+            if (col + e < a.n) to[e] = (T)sum[e];
 }
 
 template <int TYPE, int NT, int V> void launch_rows(const Args& a, hipStream_t stream) {
@@ -37,7 +49,7 @@ template <int TYPE, class S, bool FAR = false> void launch_tiles(const Args& a, 
     const int n_tiles = (a.n + S::kOuts - 1) / S::kOuts;
     // whole tiles of the rows, and one more for each expert's last
     const int m_tiles = a.routes / S::kRows + std::min(a.experts, a.routes);
-    const dim3 grid(workgroups<S>(a, (int64_t)n_tiles * m_tiles, even_rows(a)));
+    const dim3 grid(workgroups<S>(a, (int64_t)n_tiles * m_tiles));
     hipLaunchKernelGGL((w8_tiles_kernel<TYPE, S, true, FAR>), grid, dim3(S::kThreads), 0, stream, a, n_tiles, m_tiles);
     launch_tail<TYPE, S, true>(a, n_tiles, m_tiles, stream);
 }
@@ -90,12 +102,8 @@ template <int TYPE> void pick(const Args& a, int64_t x_rows, hipStream_t stream)
 }
 
 template <int TYPE> void combine(const Args& a, const int32_t* chosen, const float* weights, int top, hipStream_t stream) {
-    const int cols = a.n % 4 == 0 ? 4 : 1;
-    const dim3 grid((unsigned)(a.routes / top), (unsigned)((a.n + 256 * cols - 1) / (256 * cols)));
-    if (cols == 4)
-        hipLaunchKernelGGL((w8_combine_kernel<TYPE, 4>), grid, dim3(256), 0, stream, a, chosen, weights, top);
-    else
-        hipLaunchKernelGGL((w8_combine_kernel<TYPE, 1>), grid, dim3(256), 0, stream, a, chosen, weights, top);
+    const dim3 grid((unsigned)(a.routes / top), (unsigned)((a.n + 1023) / 1024));
+    hipLaunchKernelGGL((w8_combine_kernel<TYPE>), grid, dim3(256), 0, stream, a, chosen, weights, top);
 }
 
 size_t product_bytes(int64_t routes, int64_t n) { return ((size_t)routes * n * sizeof(float) + 15) / 16 * 16; }

@@ -35,7 +35,7 @@ template <int TYPE, int NT, int V> void launch_rows(Args a, hipStream_t stream) 
 template <int TYPE, class S, bool FAR = false> void launch_tiles(Args a, int parts, hipStream_t stream) {
     parts = share_out(a, parts, S::BK);
     const int n_tiles = (a.n + S::kOuts - 1) / S::kOuts, m_tiles = (a.m + S::kRows - 1) / S::kRows;
-    const dim3 grid(workgroups<S>(a, (int64_t)n_tiles * m_tiles, even_rows(a)), (unsigned)parts);
+    const dim3 grid(workgroups<S>(a, (int64_t)n_tiles * m_tiles), (unsigned)parts);
     hipLaunchKernelGGL((w8_tiles_kernel<TYPE, S, false, FAR>), grid, dim3(S::kThreads), 0, stream, a, n_tiles, m_tiles);
     launch_tail<TYPE, S, false>(a, n_tiles, m_tiles, stream);
     if (parts > 1)

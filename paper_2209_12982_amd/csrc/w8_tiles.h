@@ -507,9 +507,9 @@ template <int TYPE, class S, bool EXPERTS> __global__ __launch_bounds__(256) voi
     }
     if (EXPERTS && a.products) {
         float* to = a.products + (int64_t)row * a.n + col;
-        if (whole && ((uintptr_t)to & 15) == 0) {
+        if (whole) {
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) *(f32x4*)(to + e) = f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]};
+            for (int e = 0; e < 16; e += 4) *(Anywhere*)(to + e) = __builtin_bit_cast(u32x4, f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]});
         } else {
             for (int e = 0; e < 16; ++e)
                 if (col + e < a.n) to[e] = y[e];
@@ -517,10 +517,10 @@ template <int TYPE, class S, bool EXPERTS> __global__ __launch_bounds__(256) voi
         return;
     }
     T* to = (T*)a.y + row * a.y_stride + col;
-    if (whole && ((uintptr_t)to & 15) == 0) {
+    if (whole) {
 #pragma unroll
         for (int e = 0; e < 16; e += 8)
-            *(u32x4*)(to + e) = __builtin_bit_cast(u32x4, T8{(T)y[e], (T)y[e + 1], (T)y[e + 2], (T)y[e + 3], (T)y[e + 4], (T)y[e + 5], (T)y[e + 6], (T)y[e + 7]});
+            *(Anywhere*)(to + e) = __builtin_bit_cast(u32x4, T8{(T)y[e], (T)y[e + 1], (T)y[e + 2], (T)y[e + 3], (T)y[e + 4], (T)y[e + 5], (T)y[e + 6], (T)y[e + 7]});
     } else {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -545,12 +545,11 @@ typedef Tile<1, 1, 2, 1, 4, 256, 4> Shared64x32;
 // They, and rows alone (w8_rows.h): 16 outputs by 16 or 8 waves, 32 outputs by 4.
 enum Kernel { kTile256x256, kTile128x256, kTile128x128, kPair128x128, kTile64x128, kTile64x64, kTile32x32, kShared64x128, kShared64x64, kShared64x32, kRows16, kRows16Few, kRows32, kKernels };
 
-// Workgroups for so many tiles: as many for each XCD, one for each of 256 compute units where they go on.  With rows of
-// results that do not begin at multiples of 16 bytes they do not: a workgroup that goes on waits for its stores.
-template <class S> inline unsigned workgroups(const Args& a, int64_t tiles, bool even) {
+// Workgroups for so many tiles: as many for each XCD, one for each of 256 compute units where they go on.
+template <class S> inline unsigned workgroups(const Args& a, int64_t tiles) {
     int64_t each = (tiles + 7) / 8;
     if (S::kLoop && a.tail) each = (each + S::kSlots - 1) / S::kSlots * S::kSlots;      // parts fill the last round at most
-    return (unsigned)(8 * (S::kLoop && even && each > 32 ? 32 : each));
+    return (unsigned)(8 * (S::kLoop && each > 32 ? 32 : each));
 }
 // Sums of the tiles that are cut: a tile for each compute unit at most.
 constexpr size_t kTailBytes = (size_t)256 * 256 * 256 * sizeof(int32_t);
@@ -559,9 +558,6 @@ template <int TYPE, class S, bool EXPERTS> void launch_tail(const Args& a, int n
         if (a.tail)
             hipLaunchKernelGGL((w8_tail_kernel<TYPE, S, EXPERTS>), dim3(8u * (S::kSlots / 2) * S::kWaves * S::WM * S::WN / 4), dim3(256), 0,
                                stream, a, n_tiles, m_tiles);
-}
-inline bool even_rows(const Args& a) {
-    return a.products ? a.n % 4 == 0 : (((uintptr_t)a.y | (uintptr_t)a.y_stride * 2) & 15) == 0;
 }
 
 // Whether rows that far apart need the kernel for that, Tile64x128 with FAR.
