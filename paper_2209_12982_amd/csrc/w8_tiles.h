@@ -536,9 +536,10 @@ typedef Tile<2, 1, 2, 4, 1, 128, 4> Tile128x128;
 typedef Tile<2, 1, 2, 4, 1, 128, 2> Pair128x128;
 typedef Tile<1, 1, 2, 4, 1, 128, 3> Tile64x128;
 typedef Tile<1, 1, 2, 2, 1, 128, 3> Tile64x64;
-typedef Tile<1, 1, 1, 1, 4, 256, 4> Tile32x32;
+typedef Tile<1, 1, 1, 1, 8, 256, 4> Tile32x32;
 // Sums shared out to two or four waves: a compute unit that has one tile needs more waves than its blocks of 32 x 32 give (200
-// rows by 4096 x 4096: 64 x 64 11.1 us, by twice the waves 9.2; 128 by 4096 x 8192, 64 x 32 by four times 12.1).
+// rows by 4096 x 4096: 64 x 64 11.1 us, by twice the waves 9.2; 128 by 4096 x 8192, 64 x 32 by four times 12.1; 64 by 1024 x
+// 8192: 32 x 32 by four waves 8.1, by the eight that it has above 7.0).
 typedef Tile<1, 1, 2, 4, 2, 256, 3> Shared64x128;
 typedef Tile<1, 1, 2, 2, 2, 256, 3> Shared64x64;
 typedef Tile<1, 1, 2, 1, 4, 256, 4> Shared64x32;
