@@ -298,6 +298,12 @@ __global__ __launch_bounds__(S::kThreads) void w8_tiles_kernel(Args a, int n_til
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
+        if constexpr (kSteps & 1) {                         // the next stage begins with the first of the two sets
+#pragma unroll
+            for (int i = 0; i < S::WN; ++i) w[0][i] = w[1][i];
+#pragma unroll
+            for (int j = 0; j < S::WM; ++j) x[0][j] = x[1][j];
+        }
         buf = after;
         ++s;
     };
