@@ -770,8 +770,9 @@ wino_status route_experts(const void* logits, int64_t stride, const float* bias,
  *             hold exactly those routes.
  *   weights   fp32 [routes / top][top] or NULL;  chosen: int32, the same (with weights)
  *   routes <= 2^22, experts <= 1024, n <= 2^20, k a multiple of 16 below 2^17;
- *   a launch holds 2^23 workgroups: (routes / 128 + experts) n / 128, experts
- *   n / 16, and with weights (routes / top) n / 256 stay below that.
+ *   a launch holds 2^23 workgroups: (routes / 128 + experts) n / 128 (n / 64
+ *   where rows of x reach past 2^32 bytes), experts n / 16, and with weights
+ *   (routes / top) n / 256 stay below that.
  *   workspace w8_experts_matmul_workspace_bytes(routes, n, weights != NULL)
  *             bytes or more, 16-byte aligned, scratch.  With weights, routes * n
  *             floats of it are needed; with less than the rest, or NULL, the

@@ -67,6 +67,7 @@ Kernel choose(int64_t routes, int64_t experts, int64_t n, int64_t k, bool tail) 
     for (int i = 0; i < kKernels; ++i) {
         const Form& f = kForms[i];
         if (i >= kRows16 && each > 16) break;
+        if (i < kRows16 && !launch_holds((routes / f.rows + used) * ((n + f.outs - 1) / f.outs))) continue;
         const double tiles = each > f.rows ? each / f.rows + 0.5 : 1;
         const int64_t all = (int64_t)(tiles * (double)(used * ((n + f.outs - 1) / f.outs)));
         // uneven routes have more tiles than that, and one more than 256 would cost these a second round
@@ -138,6 +139,7 @@ extern "C" wino_status w8_experts_matmul(const int8_t* x, int64_t x_stride, cons
         !aligned4(ends) || !aligned4(chosen) || !aligned4(weights) || ((uintptr_t)y & 1) || (k > 0 && x_rows > 1 && (x_stride & 15)))
         return WINO_EUNSUPPORTED;
     if (!launch_holds((int64_t)(routes / 128 + experts) * ((n + 127) / 128)) || !launch_holds((int64_t)((n + 15) / 16) * experts) ||
+        (far(x_rows, x_stride, k) && !launch_holds((int64_t)(routes / 128 + experts) * ((n + 63) / 64))) ||
         (weights && !launch_holds((int64_t)y_rows * ((n + 255) / 256))))
         return WINO_EUNSUPPORTED;
     Args a = {};

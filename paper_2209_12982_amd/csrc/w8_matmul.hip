@@ -56,6 +56,7 @@ Cut cut(int64_t m, int64_t n, int64_t k) {
         if (i >= kRows16 && m > 32) break;
         const Form& f = kForms[i];
         const int64_t tiles = (n + f.outs - 1) / f.outs * ((m + f.rows - 1) / f.rows);
+        if (!launch_holds(tiles)) continue;
         for (const int parts : {1, 2, 4, 8, 16}) {
             if (parts > 1 && (i >= kRows16 || k < 1024 * parts || parts * m * n > 1 << 22)) break;
             if (f.pair == 0 && tiles * parts > 256) break;

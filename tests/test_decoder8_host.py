@@ -94,7 +94,9 @@ def test_experts_refusals():
                      ({"x": p + 8}, -2), ({"w": p + 8}, -2), ({"sx": p + 2}, -2), ({"sw": p + 2}, -2), ({"order": p + 2}, -2),
                      ({"ends": p + 2}, -2), ({"y": p + 1}, -2), ({"ws": p + 8}, -2), ({"e": 1025}, -2), ({"k": 1 << 17, "xs": 1 << 17}, -2),
                      ({"routes": (1 << 22) + 2}, -2), ({"n": (1 << 20) + 1, "ys": 1 << 21}, -2),
-                     ({"routes": 1 << 22, "rows": 1 << 22, "n": 1 << 20, "ys": 1 << 20}, -2), ({"routes": 0}, 0), ({"n": 0}, 0)):
+                     ({"routes": 1 << 22, "rows": 1 << 22, "n": 1 << 20, "ys": 1 << 20}, -2),
+                     ({"routes": 1 << 17, "rows": 1 << 17, "e": 100, "xs": 1 << 17, "n": 900000, "ys": 900000, "k": 16}, -2),
+                     ({"routes": 0}, 0), ({"n": 0}, 0)):
         assert call(**kw) == want, kw
     assert W.w8_experts_matmul_workspace_bytes(-1, 8, 1) == 0
     assert W.w8_experts_matmul_workspace_bytes(4, 8, 0) == 0
