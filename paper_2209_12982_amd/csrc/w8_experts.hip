@@ -15,30 +15,41 @@ template <int TYPE> __global__ __launch_bounds__(256) void w8_combine_kernel(Arg
     typedef typename Half<TYPE>::type T;
     typedef __attribute__((ext_vector_type(4), aligned(4))) float Row;      // rows may begin at any number
     typedef __attribute__((ext_vector_type(4), aligned(2))) T Out;
-    const int col = ((int)blockIdx.y * 256 + (int)threadIdx.x) * 4;
+    int col = ((int)blockIdx.y * 256 + (int)threadIdx.x) * 4;
     const int64_t token = blockIdx.x;
     if (col >= a.n) return;
-    const bool whole = col + 4 <= a.n;
+    col = max(min(col, a.n - 4), 0);        // the last four: two threads may have the same ones, and the same results
+    const bool whole = a.n >= 4;
+    // eight rows of products are asked for together, and those of routes without an expert dropped (one token with eight
+    // routes, 2048 outputs: 3.2 us, one row after the other 4.5)
     f32x4 sum = {};
-#pragma unroll 4
-    for (int j = 0; j < top; ++j) {
-        const int64_t route = token * top + j;
-        if ((uint32_t)chosen[route] >= (uint32_t)a.experts) continue;
-        const float* from = a.products + route * a.n + col;
-        f32x4 p = {};
-        if (whole)
-            p = *(const Row*)from;
-        else
-            for (int e = 0; e < 3; ++e)
-                if (col + e < a.n) p[e] = from[e];
-        sum += weights[route] * p;
+    for (int j0 = 0; j0 < top; j0 += 8) {
+        f32x4 p[8] = {};
+        float weight[8] = {};
+        int expert[8] = {};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (j0 + j >= top) break;
+            const int64_t route = token * top + j0 + j;
+            const float* from = a.products + route * a.n + col;
+            expert[j] = chosen[route];
+            weight[j] = weights[route];
+            if (whole)
+                p[j] = *(const Row*)from;
+            else
+                for (int e = 0; e < a.n; ++e) p[j][e] = from[e];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (j0 + j < top && (uint32_t)expert[j] < (uint32_t)a.experts) sum[e] = __builtin_fmaf(weight[j], p[j][e], sum[e]);
     }
     T* to = (T*)a.y + token * a.y_stride + col;
     if (whole)
         *(Out*)to = Out{(T)sum[0], (T)sum[1], (T)sum[2], (T)sum[3]};
     else
-        for (int e = 0; e < 3; ++e)
-            if (col + e < a.n) to[e] = (T)sum[e];
+        for (int e = 0; e < a.n; ++e) to[e] = (T)sum[e];
 }
 
 template <int TYPE, int NT, int V> void launch_rows(const Args& a, hipStream_t stream) {
