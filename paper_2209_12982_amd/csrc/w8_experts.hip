@@ -53,7 +53,11 @@ template <int TYPE> __global__ __launch_bounds__(256) void w8_combine_kernel(Arg
 }
 
 template <int TYPE, int NT, int V> void launch_rows(const Args& a, hipStream_t stream) {
-    const dim3 grid((unsigned)((a.n + 16 * NT - 1) / (16 * NT)), (unsigned)a.experts);
+    // Few routes: workgroups for as many experts as can have one, which then look for it (0.1 us), where that saves many: one
+    // token to 8 of 256, 1024 x 2048: 6.5 us, with workgroups for all experts 10.7.
+    const int n_tiles = (a.n + 16 * NT - 1) / (16 * NT);
+    const bool few = 2 * a.routes <= a.experts && (a.experts - a.routes) * n_tiles >= 512;
+    const dim3 grid((unsigned)n_tiles, (unsigned)(few ? a.routes : a.experts));
     hipLaunchKernelGGL((w8_rows_kernel<TYPE, 1, NT, V, true>), grid, dim3(64 * V), 0, stream, a);
 }
 template <int TYPE, class S, bool FAR = false> void launch_tiles(const Args& a, hipStream_t stream) {

@@ -12,6 +12,27 @@
 
 namespace w8 {
 
+// The expert that is number `which` of those that have rows, or false.
+__device__ inline bool expert_with_rows(const Args& a, int which, int& expert, int& begin, int& end) {
+    const int lane = threadIdx.x & 63;
+    for (int e0 = 0; e0 < a.experts; e0 += 64) {
+        int b = 0, e = 0;
+        if (e0 + lane < a.experts) rows_of(a, e0 + lane, b, e);
+        const uint64_t some = __ballot(b < e);
+        const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(some >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)some, 0));
+        const uint64_t here = __ballot(b < e && before == which);
+        if (here) {
+            const int l = __builtin_ctzll(here);
+            expert = e0 + l;
+            begin = __builtin_amdgcn_readlane(b, l);
+            end = __builtin_amdgcn_readlane(e, l);
+            return true;
+        }
+        which -= __builtin_popcountll(some);
+    }
+    return false;
+}
+
 template <int TYPE, int MT, int NT, int V, bool EXPERTS>
 __global__ __launch_bounds__(64 * V) void w8_rows_kernel(Args a) {
     typedef typename Half<TYPE>::type T;
@@ -23,7 +44,11 @@ __global__ __launch_bounds__(64 * V) void w8_rows_kernel(Args a) {
     int begin = 0, end = a.m, expert = 0;
     if (EXPERTS) {
         expert = blockIdx.y;
-        rows_of(a, expert, begin, end);
+        if ((int)gridDim.y < a.experts) {
+            if (!expert_with_rows(a, blockIdx.y, expert, begin, end)) return;
+        } else {
+            rows_of(a, expert, begin, end);
+        }
     }
     const int8_t* w[NT];
 #pragma unroll

@@ -57,7 +57,8 @@ def close(y, ref, size, roundings, name):
 SIZES = [(1, 1, 1, 1, 16), (1, 8, 2, 100, 64), (3, 5, 5, 33, 272), (7, 60, 6, 48, 144), (32, 64, 6, 130, 2064), (40, 4, 2, 257, 96),
          (200, 3, 1, 40, 512), (150, 8, 4, 129, 1040), (600, 16, 8, 72, 208), (333, 128, 8, 20, 64), (64, 1024, 2, 17, 32),
          (3, 2, 1, 4096, 4096), (1000, 2, 2, 300, 128), (2100, 6, 3, 260, 48),
-         (186, 4, 2, 1519, 7104), (78, 16, 2, 562, 4528), (1343, 4, 2, 367, 7568)]
+         (186, 4, 2, 1519, 7104), (78, 16, 2, 562, 4528), (1343, 4, 2, 367, 7568),
+         (1, 256, 8, 130, 272), (3, 1024, 4, 70, 144), (2, 65, 3, 257, 2064)]
 
 
 @pytest.mark.parametrize("name", ["bf16", "fp16"])
@@ -127,7 +128,7 @@ def test_more_tiles_than_compute_units(t, e, top, n, k):
         assert torch.equal(first[0], y) and torch.equal(first[1], out), "another workspace gives another result"
 
 
-@pytest.mark.parametrize("t,e", [(5, 3), (90, 2), (400, 5)])
+@pytest.mark.parametrize("t,e", [(5, 3), (90, 2), (400, 5), (4, 300), (30, 1000)])
 def test_missing_routes(t, e):
     """Padding tokens, single routes without an expert, and experts without routes."""
     torch = torch_dev()
