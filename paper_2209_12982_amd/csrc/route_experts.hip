@@ -84,11 +84,14 @@ __device__ inline double lane_value(double v, int lane) {
     const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)b[0], lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)b[1], lane);
     return __builtin_bit_cast(double, u32x2{lo, hi});
 }
-__device__ inline double wave_sum(double v) {
+// The sum over the first `lanes` lanes, the others have zeros: fewer steps for up to 4 or 16.
+__device__ inline double wave_sum(double v, int lanes = 64) {
     v += moved<0x111, 0xf>(v);
     v += moved<0x112, 0xf>(v);
+    if (lanes <= 4) return lane_value(v, 3);
     v += moved<0x114, 0xf>(v);
     v += moved<0x118, 0xf>(v);
+    if (lanes <= 16) return lane_value(v, 15);
     v += moved<0x142, 0xa>(v);
     v += moved<0x143, 0xc>(v);
     return lane_value(v, 63);
@@ -121,15 +124,18 @@ __device__ inline double exponential(double x) {
     return __builtin_ldexp(p, (int)n);
 }
 
-// 1 / (1 + e^-z): a reciprocal made exact by two steps of Newton's, which need no scaling as the divisor is 1 or more (half the
-// instructions of a division; what is below 2^-1022 may become 0).
-__device__ inline double sigmoid(float z) {
-    const float x = z == z ? __builtin_amdgcn_fmed3f(-z, -800.f, 800.f) : z;
-    const double d = 1.0 + exponential((double)x);
+// 1 / d for d of 1 or more: two steps of Newton's make it exact and need no scaling (half the instructions of a division; what
+// is below 2^-1022 may become 0).
+__device__ inline double reciprocal(double d) {
     double r = __builtin_amdgcn_rcp(d);
     r = __builtin_fma(r, __builtin_fma(-d, r, 1.0), r);
     r = __builtin_fma(r, __builtin_fma(-d, r, 1.0), r);
     return __builtin_amdgcn_div_fixup(r, d, 1.0);           // infinity and NaN
+}
+// 1 / (1 + e^-z).
+__device__ inline double sigmoid(float z) {
+    const float x = z == z ? __builtin_amdgcn_fmed3f(-z, -800.f, 800.f) : z;
+    return reciprocal(1.0 + exponential((double)x));
 }
 
 // What is not a number counts as minus infinity.
@@ -161,7 +167,7 @@ __device__ inline void route(const RouteArgs& a, const float (&z)[J], const floa
             s[j] = lane * J + j < a.experts ? exponential(x < -800.0 ? -800.0 : x) : 0.0;
             sum += s[j];
         }
-        const double part = 1.0 / wave_sum(sum);
+        const double part = reciprocal(wave_sum(sum));        // the largest one adds 1
 #pragma unroll
         for (int j = 0; j < J; ++j) s[j] *= part;
     }
@@ -266,7 +272,7 @@ __device__ inline void route(const RouteArgs& a, const float (&z)[J], const floa
     }
     double w = lane < a.top ? room[mine] : 0.0;
     if (a.normalise) {
-        const double all = wave_sum(w);
+        const double all = wave_sum(w, a.top);
         w = all == 0.0 ? 0.0 : w / all;
     }
     weight = (float)(w * (double)a.scale);
