@@ -170,7 +170,8 @@ extern "C" wino_status w8_experts_matmul(const int8_t* x, int64_t x_stride, cons
     // 124 with them.
     if (many(routes, n) && k > 4096 && workspace && workspace_bytes >= products + kTailBytes) a.tail = (int32_t*)((char*)workspace + products);
     type == WINO_BF16 ? pick<WINO_BF16>(a, x_rows, stream) : pick<WINO_FP16>(a, x_rows, stream);
-    if (weights && hipGetLastError() == hipSuccess) {
+    if (weights) {
+        if (hipGetLastError() != hipSuccess) return WINO_EHIP;      // asking for an error clears it
         type == WINO_BF16 ? combine<WINO_BF16>(a, chosen, weights, top, stream) : combine<WINO_FP16>(a, chosen, weights, top, stream);
     }
     return hipGetLastError() == hipSuccess ? WINO_OK : WINO_EHIP;
