@@ -702,7 +702,8 @@ wino_status w8_quantize(const void* x, int64_t x_stride, int8_t* codes, float* s
  *   w         int8 [n][k], dense;  w_scales: fp32 [n]
  *   bias      [n] in the type of y, or NULL
  *   y         [m][n], row stride y_stride >= n (any alignment)
- *   m <= 2^20, n <= 2^24, (m / 128)(n / 128), both rounded up, below 2^23, k a
+ *   m <= 2^20, n <= 2^24, (m / 128)(n / 128), both rounded up, below 2^23 (with
+ *   rows of x that reach past 2^32 bytes inside a tile (m / 128)(n / 64)), k a
  *   multiple of 16 below 2^17 (no sum of products of codes from -128 on
  *   passes int32 there).
  *   workspace w8_matmul_workspace_bytes(m, n, k) bytes or more, 16-byte

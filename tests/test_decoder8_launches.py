@@ -12,3 +12,26 @@ def test_launches_that_fail_are_reported(fail):
     (good, both), (status, made) = launches([("w8_experts_matmul", args, -1), ("w8_experts_matmul", args, fail)])
     assert good == 0 and [m["kernel"].split("<")[0] for m in both] == ["w8_rows_kernel", "w8_combine_kernel"]
     assert status == -6 and made == both[:fail + 1]
+
+
+def matmul(m, n, k, x_stride=None, room=1 << 40):
+    return ("w8_matmul", [P, k if x_stride is None else x_stride, P, P, P, None, P, n, m, n, k, 0, P, room, None], -1)
+
+
+def test_far_rows_that_a_launch_does_not_hold_are_refused():
+    """Rows of x 2^25 bytes apart take tiles of 64 x 128, of which there are twice as many as of 128 x 128."""
+    outs = 1 << 24
+    calls = [matmul(rows, outs, 16, 1 << 25) for rows in (4096, 3969, 3968)]
+    assert [status for status, made in launches(calls)] == [-2, -2, 0]
+
+
+def test_grids_that_are_accepted_fit_a_launch():
+    """A launch counts its threads in 32 bits, in each direction."""
+    sizes = [(m, n, k) for m in (1, 30, 70, 1000, 5000, 40000, 1 << 20) for n in (1, 300, 4096, 1 << 17, 1 << 24) for k in (16, 1040, 65536)]
+    calls = [matmul(m, n, k, stride) for m, n, k in sizes for stride in (k, 1 << 27)]
+    done = launches(calls)
+    assert sum(status == 0 for status, made in done) > 100
+    for call, (status, made) in zip(calls, done):
+        assert status in (0, -2) and bool(made) == (status == 0), call
+        for m in made:
+            assert m["grid"][0] * m["threads"] < 2 ** 32 and max(m["grid"][1:]) < 2 ** 16, (call, m)
