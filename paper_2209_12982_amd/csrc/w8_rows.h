@@ -12,6 +12,12 @@
 
 namespace w8 {
 
+// The rows that workgroup `set` of a dense product takes: each row falls to one.
+struct Span {
+    int begin, end;
+};
+constexpr Span rows_of_set(int set, int rows, int m) { return {set * rows, m - set * rows < rows ? m : set * rows + rows}; }
+
 // The expert that is number `which` of those that have rows, or false.
 __device__ inline bool expert_with_rows(const Args& a, int which, int& expert, int& begin, int& end) {
     const int lane = threadIdx.x & 63;
@@ -41,7 +47,7 @@ __global__ __launch_bounds__(64 * V) void w8_rows_kernel(Args a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, quarter = lane >> 4;
     const int n0 = blockIdx.x * kOuts;
-    int begin = 0, end = a.m, expert = 0;
+    int begin, end, expert = 0;
     if (EXPERTS) {
         expert = blockIdx.y;
         if ((int)gridDim.y < a.experts) {
@@ -49,6 +55,9 @@ __global__ __launch_bounds__(64 * V) void w8_rows_kernel(Args a) {
         } else {
             rows_of(a, expert, begin, end);
         }
+    } else {
+        const Span own = rows_of_set(blockIdx.y, kRows, a.m);
+        begin = own.begin, end = own.end;
     }
     const int8_t* w[NT];
 #pragma unroll
@@ -56,7 +65,7 @@ __global__ __launch_bounds__(64 * V) void w8_rows_kernel(Args a) {
         w[i] = a.w + ((int64_t)expert * a.n + min(n0 + 16 * i + r, a.n - 1)) * a.k + 32 * quarter;
     const int all = (a.k + 127) / 128;
     const int first = EXPERTS ? 0 : (int)blockIdx.z * a.steps, last = EXPERTS ? all : min(first + a.steps, all);
-    for (int m0 = begin + (EXPERTS ? 0 : (int)blockIdx.y * kRows); m0 < end; m0 += kRows) {
+    for (int m0 = begin; m0 < end; m0 += kRows) {               // once, where they are no expert's
         const int8_t* x[MT];
 #pragma unroll
         for (int j = 0; j < MT; ++j) {

@@ -1,5 +1,10 @@
 """What the 8-bit decoder operators launch, asked on the host without a GPU."""
+import os
+import subprocess
+
 import pytest
+
+from paper_2209_12982_amd import build as B
 
 from launch_util import ADDRESS as P
 from launch_util import launches
@@ -35,3 +40,32 @@ def test_grids_that_are_accepted_fit_a_launch():
         assert status in (0, -2) and bool(made) == (status == 0), call
         for m in made:
             assert m["grid"][0] * m["threads"] < 2 ** 32 and max(m["grid"][1:]) < 2 ** 16, (call, m)
+
+
+def test_few_rows_fall_to_one_workgroup_each(tmp_path):
+    """Up to 32 rows by the kernel for few: the sets that its workgroups take, over the grid that is launched, hold each row once."""
+    try:
+        hipcc = B.hipcc()
+    except RuntimeError:
+        pytest.skip("no hipcc")
+    sizes = [(m, n, k) for m in range(1, 33) for n, k in ((1407, 768), (8771, 112), (96, 16))]
+    grids = set()
+    for (m, n, k), (status, made) in zip(sizes, launches([matmul(*s) for s in sizes])):
+        if made[0]["kernel"].startswith("w8_rows_kernel"):
+            grids.add((m, made[0]["grid"][1]))
+    assert {m for m, sets in grids} == set(range(1, 33))
+    source = tmp_path / "sets.hip"
+    source.write_text("""
+#include "w8_rows.h"
+constexpr bool once(int m, int sets) {
+    for (int row = 0; row < m; ++row) {
+        int times = 0;
+        for (int s = 0; s < sets; ++s) times += w8::rows_of_set(s, 16, m).begin <= row && row < w8::rows_of_set(s, 16, m).end;
+        if (times != 1) return false;
+    }
+    return w8::rows_of_set(sets - 1, 16, m).end == m;
+}
+""" + "".join(f"static_assert(once({m}, {sets}), \"{m} rows\");\n" for m, sets in sorted(grids)))
+    r = subprocess.run([hipcc, "-std=c++17", "-fsyntax-only", "--offload-host-only", "-I", B.CSRC, "-I", os.path.join(B.ROOT, "include"),
+                        str(source)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
