@@ -82,10 +82,12 @@ bool cuts_tail(const Cut& c, int64_t m, int64_t n, int64_t k) {
 }
 
 // Rows of x too far apart for the offsets of a kernel of tiles: Tile64x128 takes them, which has some for that.
-bool far_rows(const Cut& c, int64_t x_stride, int64_t k) { return c.kernel < kRows16 && far(kForms[c.kernel].rows, x_stride, k); }
+bool far_rows(const Cut& c, int64_t m, int64_t x_stride, int64_t k) {
+    return c.kernel < kRows16 && far(std::min<int64_t>(kForms[c.kernel].rows, m), x_stride, k);
+}
 
 template <int TYPE> void pick(Args a, const Cut& c, size_t bytes, hipStream_t stream) {
-    if (far_rows(c, a.x_stride, a.k)) {
+    if (far_rows(c, a.m, a.x_stride, a.k)) {
         a.part = nullptr;
         return launch_tiles<TYPE, Tile64x128, true>(a, 1, stream);
     }
@@ -132,7 +134,7 @@ extern "C" wino_status w8_matmul(const int8_t* x, int64_t x_stride, const float*
         ((uintptr_t)y & 1) || ((uintptr_t)bias & 1) || (k > 0 && m > 1 && (x_stride & 15)))
         return WINO_EUNSUPPORTED;
     const Cut c = cut(m, n, k);
-    if (far_rows(c, x_stride, k) && !launch_holds((int64_t)((m + 127) / 128) * ((n + 63) / 64))) return WINO_EUNSUPPORTED;
+    if (far_rows(c, m, x_stride, k) && !launch_holds((int64_t)((m + 127) / 128) * ((n + 63) / 64))) return WINO_EUNSUPPORTED;
     Args a = {};
     a.x = x, a.w = w, a.x_scales = x_scales, a.w_scales = w_scales, a.bias = bias, a.y = y;
     a.x_stride = x_stride, a.y_stride = y_stride, a.m = m, a.n = n, a.k = k, a.part = (int32_t*)workspace;

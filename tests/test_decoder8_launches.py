@@ -69,3 +69,16 @@ constexpr bool once(int m, int sets) {
     r = subprocess.run([hipcc, "-std=c++17", "-fsyntax-only", "--offload-host-only", "-I", B.CSRC, "-I", os.path.join(B.ROOT, "include"),
                         str(source)], capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
+
+
+def test_rows_that_are_not_there_are_not_far():
+    """Fewer rows than a tile: how far the last of them lies decides, and the stride of a single one does not count."""
+    sizes = [(m, n, k) for m in (1, 2, 5, 33) for n in (64, 5000) for k in (2064, 16384, 65536)]
+    near, far = [], []
+    for m, n, k in sizes:
+        apart = ((1 << 32) - 1 - k) // (m - 1) // 16 * 16 if m > 1 else 1 << 62
+        near.append(matmul(m, n, k))
+        far.append(matmul(m, n, k, apart))
+    plain = launches(near)
+    assert any("w8_tiles" in made[0]["kernel"] for status, made in plain)
+    assert launches(far) == plain
