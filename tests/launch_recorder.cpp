@@ -60,6 +60,13 @@ int hipGetLastError() {
     last_error = 0;
     return error;
 }
+// The kernels of the library, one a line.
+const char* kernels_known() {
+    static std::string all;
+    all.clear();
+    for (const auto& k : kernels()) all += k.second + "\n";
+    return all.c_str();
+}
 // What was launched since the last call; the launch of that number from here on fails (-1: none).
 const char* launches_taken(int fail) {
     static std::string taken;

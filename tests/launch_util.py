@@ -19,7 +19,8 @@ ADDRESS = 1 << 20           # aligned, and nobody's
 _CHILD = """
 import ctypes, json, sys
 recorder = ctypes.CDLL(sys.argv[1], ctypes.RTLD_GLOBAL)
-recorder.launches_taken.restype = ctypes.c_char_p
+sys.modules["torch"] = None         # the library by itself
+recorder.launches_taken.restype = recorder.kernels_known.restype = ctypes.c_char_p
 import paper_2209_12982_amd as W
 lib = W.load_library()
 out = []
@@ -27,12 +28,15 @@ for name, args, fail in json.load(sys.stdin):
     recorder.launches_taken(fail)
     status = getattr(lib, name)(*args)
     out.append([status, recorder.launches_taken(-1).decode()])
-print(json.dumps(out))
+print(json.dumps([recorder.kernels_known().decode(), out]))
 """
 
 
-def launches(calls):
-    """[(name, arguments, number of the launch that fails or -1)] -> [(status, [dict of kernel, grid, threads, shared])]."""
+def _plain(kernel):
+    return re.sub(r"\bw8::|^void |\(.*\)$", "", kernel.replace("(anonymous namespace)::", ""))
+
+
+def _ask(calls):
     try:
         W.load_library()
     except W.LibraryNotBuilt:
@@ -47,12 +51,21 @@ def launches(calls):
         r = subprocess.run([sys.executable, "-c", _CHILD, recorder], input=json.dumps(calls), capture_output=True, text=True, cwd=ROOT,
                            timeout=300)
     assert r.returncode == 0, r.stderr
+    return json.loads(r.stdout)
+
+
+def kernels():
+    """The names of all kernels that the library holds."""
+    return [_plain(line) for line in _ask([])[0].splitlines()]
+
+
+def launches(calls):
+    """[(name, arguments, number of the launch that fails or -1)] -> [(status, [dict of kernel, grid, threads, shared])]."""
     out = []
-    for status, text in json.loads(r.stdout):
+    for status, text in _ask(calls)[1]:
         made = []
         for line in text.splitlines():
             grid, threads, shared, kernel = line.split("|", 3)
-            kernel = re.sub(r"\(anonymous namespace\)::|\bw8::|^void |\(.*\)$", "", re.sub(r"\(anonymous namespace\)::", "", kernel))
-            made.append(dict(kernel=kernel, grid=[int(v) for v in grid.split()], threads=int(threads), shared=int(shared)))
+            made.append(dict(kernel=_plain(kernel), grid=[int(v) for v in grid.split()], threads=int(threads), shared=int(shared)))
         out.append((status, made))
     return out

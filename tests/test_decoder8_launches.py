@@ -6,8 +6,9 @@ import pytest
 
 from paper_2209_12982_amd import build as B
 
+import decoder8_sizes as sizes
 from launch_util import ADDRESS as P
-from launch_util import launches
+from launch_util import kernels, launches
 
 
 @pytest.mark.parametrize("fail", [0, 1])
@@ -82,3 +83,49 @@ def test_rows_that_are_not_there_are_not_far():
     plain = launches(near)
     assert any("w8_tiles" in made[0]["kernel"] for status, made in plain)
     assert launches(far) == plain
+
+
+def experts(tokens, outs_of, top, n, k, weighted=False, apart=None):
+    routes = tokens * top
+    return ("w8_experts_matmul", [P, k if apart is None else apart, P, tokens, P, P, P, P, routes, outs_of, P if weighted else None,
+                                  P if weighted else None, top, P, n, n, k, 0, P, 1 << 45, None], -1)
+
+
+def route(tokens, of, top, kind=0):
+    return ("route_experts", [P, of, None, tokens, of, top, 0, 1, 1, 1, 1, 1.0, None, P, P, P, P, kind, P, 1 << 40, None], -1)
+
+
+def second(made):
+    if len(made) > 1 and "combine" not in made[1]["kernel"]:
+        return made[1]["kernel"].split("_")[1]
+    return None
+
+
+def test_sizes_take_their_kernels():
+    """The table of sizes that the GPU tests run, kernel by kernel."""
+    for table, call in ((sizes.MATMUL, matmul), (sizes.EXPERTS, experts)):
+        listed = [(key, s) for key, many in table.items() for s in many]
+        for (key, s), (status, made) in zip(listed, launches([call(*s) for key, s in listed])):
+            few = call is experts and "rows" in made[0]["kernel"] and made[0]["grid"][1] < s[1]
+            assert (sizes.name_of(made[0]["kernel"]), "few" if few else second(made)) == key and status == 0, (s, made)
+    far = [matmul(*s) for s in sizes.MATMUL_FAR] + [experts(*s[:5], apart=s[5]) for s in sizes.EXPERTS_FAR]
+    for call, (status, made) in zip(far, launches(far)):
+        assert status == 0 and made[0]["kernel"].endswith("true>"), (call, made)
+    listed = [(key, s) for key, many in sizes.ROUTE.items() for s in many]
+    for (key, s), (status, made) in zip(listed, launches([route(*s) for key, s in listed])):
+        assert status == 0 and tuple(m["kernel"].replace(m["kernel"][m["kernel"].find("<"):], "") if "experts" in m["kernel"]
+                                     else m["kernel"] for m in made) == key, (s, made)
+
+
+def test_every_kernel_has_sizes():
+    """What the table's calls launch, in either type, is every kernel of these operators that the library holds."""
+    calls = [call(*s) for table, call in ((sizes.MATMUL, matmul), (sizes.EXPERTS, experts)) for many in table.values() for s in many]
+    calls += [matmul(*s) for s in sizes.MATMUL_FAR] + [experts(*s[:5], apart=s[5]) for s in sizes.EXPERTS_FAR]
+    calls += [experts(*s, weighted=True) for s in sizes.EXPERTS["32x32", None]]
+    calls += [("w8_quantize", [P, k, P, P, 3, k, 0, None], -1) for k in (4096, 16384, 16400)]
+    other = [(name, args[:at] + [1] + args[at + 1:], -1) for name, args, _ in calls
+             for at in [{"w8_matmul": 11, "w8_experts_matmul": 17, "w8_quantize": 6}[name]]]
+    calls += other + [route(*s, kind=kind) for many in sizes.ROUTE.values() for s in many for kind in (0, 1, 2)]
+    launched = {m["kernel"] for status, made in launches(calls) for m in made}
+    held = {k for k in kernels() if k.startswith(("w8_", "route_"))}
+    assert len(held) > 50 and launched == held, (sorted(held - launched), sorted(launched - held))

@@ -1,0 +1,145 @@
+"""Every kernel of the 8-bit decoder operators on sizes that take it
+(decoder8_sizes.py), against float64; bounds as in the operators' own tests."""
+import numpy as np
+import pytest
+
+import decoder8_sizes as sizes
+import paper_2209_12982_amd as W
+from decoder_util import dtype, half
+from gpu_util import torch_dev
+from test_gpu_route_experts import check as check_routes
+from test_gpu_route_experts import logits_of, run
+from test_gpu_w8_experts import close, grouped, layer, products
+from test_gpu_w8_matmul import check, operands
+
+pytestmark = pytest.mark.gpu
+
+
+def cases(table):
+    return [pytest.param(s, id=f"{'-'.join(filter(None, key)).replace(' ', '_')}-{'x'.join(map(str, s))}")
+            for key, many in table.items() for s in many]
+
+
+@pytest.mark.parametrize("name", ["bf16", "fp16"])
+@pytest.mark.parametrize("size", cases(sizes.MATMUL))
+def test_matmul(size, name):
+    """With a workspace and without one, rows of y at 16 bytes and past it, nothing beside y written."""
+    torch = torch_dev()
+    m, n, k = size
+    rng = np.random.default_rng(m * 7919 + n * 31 + k)
+    x, xs, w, ws = operands(torch, rng, m, n, k, low=-128)
+    xs *= (1024 / k) ** 0.5
+    bias = half(torch, rng.normal(0, 1, n), name)[0] if n % 2 else None
+    need = W.w8_matmul_workspace_bytes(m, n, k)
+    room = torch.full((need + 16,), 255, dtype=torch.uint8, device="cuda")
+    wide = torch.empty((m + 2, n + 16), dtype=dtype(torch, name), device="cuda")
+    first = None
+    for left, space in ((8, room[:need]), (7, None)):
+        wide.fill_(7.0)
+        y = wide[1:m + 1, left:left + n]
+        y.fill_(float("nan"))
+        W.w8_matmul(x, xs, w, ws, y, bias=bias, workspace=space)
+        if first is None:
+            check(y, x, xs, w, ws, bias, name)
+            first = y.clone()
+        assert torch.equal(first, y), "another workspace gives another result"
+        assert (wide[0] == 7).all() and (wide[m + 1] == 7).all() and (wide[:, :left] == 7).all() and (wide[:, left + n:] == 7).all()
+    assert (room[need:] == 255).all()
+
+
+@pytest.mark.parametrize("m,n,k,apart", sizes.MATMUL_FAR)
+def test_matmul_of_far_rows(m, n, k, apart):
+    """Rows of x further apart in a tile than 32 bits hold."""
+    torch = torch_dev()
+    rng = np.random.default_rng(m + n + k)
+    x, xs, w, ws = operands(torch, rng, m, n, k)
+    xs *= (1024 / k) ** 0.5
+    far = torch.empty((m, apart), dtype=torch.int8, device="cuda")
+    far[:, :k] = x
+    y = torch.full((m, n), float("nan"), dtype=torch.bfloat16, device="cuda")
+    W.w8_matmul(far[:, :k], xs, w, ws, y)
+    check(y, x, xs, w, ws, None, "bf16")
+
+
+def check_experts(torch, rng, x, far, xs, w, ws, chosen, top, name):
+    """Products and weighted sums with all workspaces; x: the rows that `far` holds too."""
+    e, n, t = w.shape[0], w.shape[1], len(chosen)
+    order, ends, routes, begin = grouped(torch, chosen, e)
+    ref = products(x, xs, w, ws, routes, begin, t * top)
+    there = torch.from_numpy((chosen >= 0).reshape(-1)).cuda()
+    chosen = torch.from_numpy(chosen).cuda()
+    weights = torch.from_numpy(rng.uniform(0, 1, (t, top)).astype(np.float32)).cuda()
+    parts = torch.where(there[:, None], ref, 0.0).view(t, top, n) * weights.double()[..., None]
+    first = None
+    for more in (True, False):
+        need = W.w8_experts_matmul_workspace_bytes(t * top, n, False)
+        room = torch.full((need + 16,), 255, dtype=torch.uint8, device="cuda")
+        y = torch.full((t * top + 1, n), 77.0, dtype=dtype(torch, name), device="cuda")
+        W.w8_experts_matmul(far, xs, w, ws, order, ends, y[:-1], workspace=room[:need] if more else None)
+        assert (y[:-1][~there] == 77).all() and (y[-1] == 77).all() and (room[need:] == 255).all()
+        need = W.w8_experts_matmul_workspace_bytes(t * top, n, True) if more else t * top * n * 4
+        room = torch.full((need + 16,), 255, dtype=torch.uint8, device="cuda")
+        out = torch.full((t + 1, n), 77.0, dtype=dtype(torch, name), device="cuda")
+        W.w8_experts_matmul(far, xs, w, ws, order, ends, out[:-1], chosen=chosen, weights=weights, workspace=room[:need])
+        assert (out[-1] == 77).all() and (room[need:] == 255).all()
+        if first is None:
+            close(y[:-1][there], ref[there], ref[there].abs(), 3, name)
+            close(out[:-1], parts.sum(1), parts.abs().sum(1), 4 + top, name)
+            first = y, out
+        assert torch.equal(first[0], y) and torch.equal(first[1], out), "another workspace gives another result"
+
+
+@pytest.mark.parametrize("name", ["bf16", "fp16"])
+@pytest.mark.parametrize("size", cases(sizes.EXPERTS))
+def test_experts(size, name):
+    """Routes of uneven experts, some of them nobody's."""
+    torch = torch_dev()
+    t, e, top, n, k = size
+    rng = np.random.default_rng(t * 31 + e * 7 + n + k)
+    x, xs, w, ws, chosen = layer(torch, rng, t, e, top, n, k, True, skew=0.5)
+    xs *= (256 / k) ** 0.5
+    chosen[rng.integers(0, t, t // 8)] = -1
+    check_experts(torch, rng, x, x, xs, w, ws, chosen, top, name)
+
+
+@pytest.mark.parametrize("t,e,n,k", [(900, 64, 200, 272), (500, 512, 1000, 144), (37, 8, 33, 2064), (3000, 16, 257, 528), (5000, 4, 300, 1040)])
+def test_one_expert_has_all_routes(t, e, n, k):
+    """As uneven as routes can be: sets of rows one after the other, the most tiles that one expert can have, and none for others."""
+    torch = torch_dev()
+    rng = np.random.default_rng(t + e)
+    x, xs, w, ws, chosen = layer(torch, rng, t, e, 1, n, k, True)
+    chosen[:] = e - 2
+    check_experts(torch, rng, x, x, xs, w, ws, chosen, 1, "bf16")
+
+
+@pytest.mark.parametrize("shared", [True, False])
+@pytest.mark.parametrize("t,e,top,n,k,apart", sizes.EXPERTS_FAR)
+def test_experts_of_far_rows(t, e, top, n, k, apart, shared):
+    """Rows of x past 2^32 bytes, for each token and for each route."""
+    torch = torch_dev()
+    rng = np.random.default_rng(t + n)
+    x, xs, w, ws, chosen = layer(torch, rng, t, e, top, n, k, shared)
+    far = torch.empty((len(x), apart), dtype=torch.int8, device="cuda")
+    far[:, :k] = x
+    chosen[t // 2] = -1
+    check_experts(torch, rng, x, far[:, :k], xs, w, ws, chosen, top, "fp16")
+
+
+@pytest.mark.parametrize("name", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("size", cases(sizes.ROUTE))
+def test_route(size, name):
+    """The choice of some tokens against the oracle, the order against a stable sort of the choice."""
+    torch = torch_dev()
+    t, e, top = size
+    rng = np.random.default_rng(t * 31 + e + top)
+    logits, values = logits_of(torch, rng, t, e, name)
+    live = t - t // 9
+    got = run(torch, logits, top, live=live)
+    flat = got[0].reshape(-1)
+    there = np.flatnonzero(flat >= 0)
+    assert len(there) == live * top and (got[0][live:] == -1).all() and (got[1][live:] == 0).all()
+    want = there[np.argsort(flat[there], kind="stable")]
+    assert (got[2][:len(want)] == want).all() and (got[2][len(want):] == -7).all()
+    assert (got[3] == np.concatenate([[0], np.cumsum(np.bincount(flat[there], minlength=e))])).all()
+    rows = np.sort(rng.permutation(live)[:100])
+    check_routes(values[rows], [got[0][rows], got[1][rows], None, None], top)
