@@ -58,7 +58,7 @@ template <int TYPE, int NT, int V> void launch_rows(const Args& a, hipStream_t s
     const int n_tiles = (a.n + 16 * NT - 1) / (16 * NT);
     const bool few = 2 * a.routes <= a.experts && (a.experts - a.routes) * n_tiles >= 512;
     const dim3 grid((unsigned)n_tiles, (unsigned)(few ? a.routes : a.experts));
-    hipLaunchKernelGGL((w8_rows_kernel<TYPE, 1, NT, V, true>), grid, dim3(64 * V), 0, stream, a);
+    hipLaunchKernelGGL((w8_rows_kernel<TYPE, NT, V, true>), grid, dim3(64 * V), 0, stream, a);
 }
 template <int TYPE, class S, bool FAR = false> void launch_tiles(const Args& a, hipStream_t stream) {
     const int n_tiles = (a.n + S::kOuts - 1) / S::kOuts;

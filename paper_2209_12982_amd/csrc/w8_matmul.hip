@@ -27,10 +27,9 @@ int share_out(Args& a, int parts, int bk) {
     if (parts <= 1) a.part = nullptr;
     return parts;
 }
-template <int TYPE, int NT, int V> void launch_rows(Args a, hipStream_t stream) {
-    share_out(a, 1, 128);
+template <int TYPE, int NT, int V> void launch_rows(const Args& a, hipStream_t stream) {
     const dim3 grid((unsigned)((a.n + 16 * NT - 1) / (16 * NT)), (unsigned)((a.m + 15) / 16));
-    hipLaunchKernelGGL((w8_rows_kernel<TYPE, 1, NT, V, false>), grid, dim3(64 * V), 0, stream, a);
+    hipLaunchKernelGGL((w8_rows_kernel<TYPE, NT, V, false>), grid, dim3(64 * V), 0, stream, a);
 }
 template <int TYPE, class S, bool FAR = false> void launch_tiles(Args a, int parts, hipStream_t stream) {
     parts = share_out(a, parts, S::BK);

@@ -1,5 +1,6 @@
-// Few rows times 8-bit weights (at most 64 at a time): every byte of the weights is read once and used by one wave.
-// A workgroup has 16 NT outputs; its V waves share out k in steps of 128 bytes, and their sums meet in LDS.
+// Few rows times 8-bit weights, sixteen at a time: each time every byte of the weights is read once and used by one wave.  More
+// dense rows are more workgroups, which share the weights in the caches; an expert's rows have one workgroup, sixteen after
+// sixteen.  A workgroup has 16 NT outputs; its V waves share out k in steps of 128 bytes, and their sums meet in LDS.
 //
 // Rows of the weights are rows of the first operand of mfma 16x16x64, rows of x columns of the second.  Which part of k
 // stands where in an operand is free as long as both agree: a lane reads 32 neighbouring bytes of its row, the first 16 for
@@ -39,10 +40,10 @@ __device__ inline bool expert_with_rows(const Args& a, int which, int& expert, i
     return false;
 }
 
-template <int TYPE, int MT, int NT, int V, bool EXPERTS>
+template <int TYPE, int NT, int V, bool EXPERTS>
 __global__ __launch_bounds__(64 * V) void w8_rows_kernel(Args a) {
     typedef typename Half<TYPE>::type T;
-    constexpr int kRows = 16 * MT, kOuts = 16 * NT, kAhead = NT * MT >= 8 ? 1 : 2;     // steps whose loads are on their way together
+    constexpr int kRows = 16, kOuts = 16 * NT, kAhead = 2;  // steps whose loads are on their way together
     __shared__ int sums[kRows][kOuts + 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, quarter = lane >> 4;
@@ -63,15 +64,10 @@ __global__ __launch_bounds__(64 * V) void w8_rows_kernel(Args a) {
 #pragma unroll
     for (int i = 0; i < NT; ++i)
         w[i] = a.w + ((int64_t)expert * a.n + min(n0 + 16 * i + r, a.n - 1)) * a.k + 32 * quarter;
-    const int all = (a.k + 127) / 128;
-    const int first = EXPERTS ? 0 : (int)blockIdx.z * a.steps, last = EXPERTS ? all : min(first + a.steps, all);
+    const int last = (a.k + 127) / 128;
     for (int m0 = begin; m0 < end; m0 += kRows) {               // once, where they are no expert's
-        const int8_t* x[MT];
-#pragma unroll
-        for (int j = 0; j < MT; ++j) {
-            const int at = min(m0 + 16 * j + r, end - 1);
-            x[j] = a.x + (EXPERTS ? x_row(a, a.order[at]) : at) * a.x_stride + 32 * quarter;
-        }
+        const int own = min(m0 + r, end - 1);
+        const int8_t* x = a.x + (EXPERTS ? x_row(a, a.order[own]) : own) * a.x_stride + 32 * quarter;
         for (int o = threadIdx.x; o < kRows * kOuts; o += 64 * V) sums[o / kOuts][o % kOuts] = 0;
         // what a thread's results need beside their sums is asked for before the loop, not behind it
         constexpr int kMine = (kRows * kOuts + 64 * V - 1) / (64 * V);
@@ -88,13 +84,11 @@ __global__ __launch_bounds__(64 * V) void w8_rows_kernel(Args a) {
             bias[i] = !EXPERTS && a.bias ? (float)((const T*)a.bias)[c] : 0.f;
             if (EXPERTS && row[i] >= a.routes) row[i] = -1;
         }
-        i32x4 acc[NT][MT];
+        i32x4 acc[NT];
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-            for (int j = 0; j < MT; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
-        for (int s0 = first + wave; s0 < last; s0 += V * kAhead) {
-            i32x4 wv[kAhead][NT][2], xv[kAhead][MT][2];
+        for (int i = 0; i < NT; ++i) acc[i] = i32x4{0, 0, 0, 0};
+        for (int s0 = wave; s0 < last; s0 += V * kAhead) {
+            i32x4 wv[kAhead][NT][2], xv[kAhead][2];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const int64_t at = (int64_t)(s0 + u * V) * 128;
@@ -104,8 +98,7 @@ __global__ __launch_bounds__(64 * V) void w8_rows_kernel(Args a) {
                     const int64_t off = at + 16 * h;
 #pragma unroll
                     for (int i = 0; i < NT; ++i) wv[u][i][h] = *(const i32x4*)(there ? w[i] + off : (const int8_t*)kZeros);
-#pragma unroll
-                    for (int j = 0; j < MT; ++j) xv[u][j][h] = *(const i32x4*)(there ? x[j] + off : (const int8_t*)kZeros);
+                    xv[u][h] = *(const i32x4*)(there ? x + off : (const int8_t*)kZeros);
                 }
             }
 #pragma unroll
@@ -113,29 +106,19 @@ __global__ __launch_bounds__(64 * V) void w8_rows_kernel(Args a) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int i = 0; i < NT; ++i)
-#pragma unroll
-                        for (int j = 0; j < MT; ++j)
-                            acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[u][i][h], xv[u][j][h], acc[i][j], 0, 0, 0);
+                    for (int i = 0; i < NT; ++i) acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[u][i][h], xv[u][h], acc[i], 0, 0, 0);
         }
         __syncthreads();                                    // the zeros are there
 #pragma unroll
         for (int i = 0; i < NT; ++i)
 #pragma unroll
-            for (int j = 0; j < MT; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) atomicAdd(&sums[16 * j + r][16 * i + 4 * quarter + e], acc[i][j][e]);
+            for (int e = 0; e < 4; ++e) atomicAdd(&sums[r][16 * i + 4 * quarter + e], acc[i][e]);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
             if (row[i] < 0) continue;
             const int o = threadIdx.x + 64 * V * i, c = n0 + o % kOuts;
-            const int sum = sums[o / kOuts][o % kOuts];
-            if (!EXPERTS && a.part) {
-                a.part[((int64_t)blockIdx.z * a.m + row[i]) * a.n + c] = sum;
-                continue;
-            }
-            const float y = finish(sum, xs[i], ws[i], bias[i]);
+            const float y = finish(sums[o / kOuts][o % kOuts], xs[i], ws[i], bias[i]);
             if (EXPERTS && a.products)
                 a.products[(int64_t)row[i] * a.n + c] = y;
             else

@@ -74,9 +74,11 @@ ROUTE = {
 }
 
 
+ROWS = {"rows 16": "1, 16, ", "rows 16 few": "1, 8, ", "rows 32": "2, 4, "}
+
+
 def name_of(kernel):
     """The name above of a kernel of the library."""
-    for name, tile in TILES.items():
-        if tile in kernel:
+    for name, part in TILES.items() if "Tile<" in kernel else ROWS.items():
+        if part in kernel:
             return name
-    return {"1, 1, 16": "rows 16", "1, 1, 8,": "rows 16 few", "1, 2, 4,": "rows 32"}[kernel[kernel.index(",") + 2:][:8].strip()]
