@@ -34,16 +34,17 @@ template <int WN_, int WM_, int GN_, int GM_, int GK_, int BK_, int STAGES_> str
     static __device__ int swap(int row) { return BK >= 256 ? row & 15 : (BK == 128 ? (row >> 1) & 7 : (row >> 2) & 3); }
 };
 
-// 16 bytes a lane from base + off to LDS at dst + 16 lane, which is on its way until vmcnt says otherwise; in assembly
-// because the compiler would wait for all copies before each read of LDS.  A scalar base moves on from stage to stage
-// without vector instructions, which take issue slots from the matrix products.
-__device__ inline void copy16(const void* base, uint32_t off, uint32_t dst) {
-    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(dst) : "memory");
-}
 // An address that all lanes have alike, in scalar registers.
 __device__ inline const int8_t* uniform(const int8_t* p) {
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)p), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)p >> 32));
     return (const int8_t*)((uintptr_t)hi << 32 | lo);
+}
+// 16 bytes a lane from base + off to LDS at dst + 16 lane, which is on its way until vmcnt says otherwise; in assembly
+// because the compiler would wait for all copies before each read of LDS.  A scalar base moves on from stage to stage
+// without vector instructions, which take issue slots from the matrix products; that it is one is said here, where the
+// instruction needs it, and not left to what the compiler makes of the additions before.
+__device__ inline void copy16(const int8_t* base, uint32_t off, uint32_t dst) {
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(uniform(base)), "{m0}"(dst) : "memory");
 }
 __device__ inline void copy16_from(const void* from, uint32_t dst) {
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(dst) : "memory");

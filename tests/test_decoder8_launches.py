@@ -129,3 +129,23 @@ def test_every_kernel_has_sizes():
     launched = {m["kernel"] for status, made in launches(calls) for m in made}
     held = {k for k in kernels() if k.startswith(("w8_", "route_"))}
     assert len(held) > 50 and launched == held, (sorted(held - launched), sorted(launched - held))
+
+
+@pytest.mark.parametrize("level", ["-O1", "-O2"])
+def test_tiles_compile_at_other_levels(tmp_path, level):
+    """The assembly in the copies gets the registers that it names, whatever the optimizer leaves of the code around it."""
+    try:
+        hipcc = B.hipcc()
+    except RuntimeError:
+        pytest.skip("no hipcc")
+    source = tmp_path / "tiles.hip"
+    source.write_text("""
+#include "w8_tiles.h"
+template __global__ void w8::w8_tiles_kernel<WINO_BF16, w8::Tile256x256, false>(w8::Args, int, int);
+template __global__ void w8::w8_tiles_kernel<WINO_FP16, w8::Tile64x64, true>(w8::Args, int, int);
+template __global__ void w8::w8_tiles_kernel<WINO_FP16, w8::Tile64x128, true, true>(w8::Args, int, int);
+""")
+    flags = [level if f == "-O3" else f for f in B.HIP_FLAGS]
+    r = subprocess.run([hipcc, *flags, "--offload-device-only", "-I", B.CSRC, "-I", os.path.join(B.ROOT, "include"), "-c", str(source),
+                        "-o", str(tmp_path / "tiles.o")], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
