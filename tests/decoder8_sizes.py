@@ -40,6 +40,8 @@ MATMUL = {
 }
 # rows of x that lie `apart` bytes from each other: (m, n, k, apart)
 MATMUL_FAR = [(150, 6001, 1040, 1 << 27), (33, 300, 8192, 1 << 28)]
+# the same with the last offsets between 2^31 and 2^32
+MATMUL_NEAR = [(33, 300, 8192, 1 << 27), (140, 6001, 1040, 1 << 25)]
 
 # kernel, second launch; "few": workgroups for as many experts as there are routes -> (tokens, experts, top, n, k)
 EXPERTS = {
@@ -63,6 +65,7 @@ EXPERTS = {
 }
 # (tokens, experts, top, n, k, apart)
 EXPERTS_FAR = [(70, 3, 2, 131, 1040, 1 << 26), (300, 2, 1, 70, 640, 1 << 24)]
+EXPERTS_NEAR = [(62, 3, 2, 131, 1040, 1 << 26), (250, 2, 1, 70, 640, 1 << 24)]
 
 # launches with an order -> (tokens, experts, top)
 ROUTE = {

@@ -95,6 +95,19 @@ def route(tokens, of, top, kind=0):
     return ("route_experts", [P, of, None, tokens, of, top, 0, 1, 1, 1, 1, 1.0, None, P, P, P, P, kind, P, 1 << 40, None], -1)
 
 
+def test_other_grids_fit_a_launch():
+    calls = [experts(t, e, top, n, k, weighted) for t in (1, 100, 5000, 1 << 20) for e in (1, 60, 1024) for top in (1, 4)
+             for n in (1, 4096, 1 << 20) for k in (16, 65536) for weighted in (False, True)]
+    calls += [route(t, e, top) for t in (1, 33, 5000, 1 << 17, 1 << 22) for e in (1, 60, 256, 1024) for top in (1, 32) if top <= e]
+    calls += [("w8_quantize", [P, k, P, P, m, k, 0, None], -1) for m in (1, 1 << 20, (1 << 24) - 1) for k in (16, 1 << 20)]
+    done = launches(calls)
+    assert sum(status == 0 for status, made in done) > 150
+    for call, (status, made) in zip(calls, done):
+        assert status in (0, -2) and bool(made) == (status == 0), call
+        for m in made:
+            assert m["grid"][0] * m["threads"] < 2 ** 32 and max(m["grid"][1:]) < 2 ** 16 and m["shared"] <= 160 << 10, (call, m)
+
+
 def second(made):
     if len(made) > 1 and "combine" not in made[1]["kernel"]:
         return made[1]["kernel"].split("_")[1]
@@ -111,6 +124,9 @@ def test_sizes_take_their_kernels():
     far = [matmul(*s) for s in sizes.MATMUL_FAR] + [experts(*s[:5], apart=s[5]) for s in sizes.EXPERTS_FAR]
     for call, (status, made) in zip(far, launches(far)):
         assert status == 0 and made[0]["kernel"].endswith("true>"), (call, made)
+    near = [matmul(*s) for s in sizes.MATMUL_NEAR] + [experts(*s[:5], apart=s[5]) for s in sizes.EXPERTS_NEAR]
+    for call, (status, made) in zip(near, launches(near)):
+        assert status == 0 and made[0]["kernel"].endswith("false>") and "tiles" in made[0]["kernel"], (call, made)
     listed = [(key, s) for key, many in sizes.ROUTE.items() for s in many]
     for (key, s), (status, made) in zip(listed, launches([route(*s) for key, s in listed])):
         assert status == 0 and tuple(m["kernel"].replace(m["kernel"][m["kernel"].find("<"):], "") if "experts" in m["kernel"]

@@ -47,9 +47,9 @@ def test_matmul(size, name):
     assert (room[need:] == 255).all()
 
 
-@pytest.mark.parametrize("m,n,k,apart", sizes.MATMUL_FAR)
+@pytest.mark.parametrize("m,n,k,apart", sizes.MATMUL_FAR + sizes.MATMUL_NEAR)
 def test_matmul_of_far_rows(m, n, k, apart):
-    """Rows of x further apart in a tile than 32 bits hold."""
+    """Rows of x further apart in a tile than 32 bits hold, and just less."""
     torch = torch_dev()
     rng = np.random.default_rng(m + n + k)
     x, xs, w, ws = operands(torch, rng, m, n, k)
@@ -113,9 +113,9 @@ def test_one_expert_has_all_routes(t, e, n, k):
 
 
 @pytest.mark.parametrize("shared", [True, False])
-@pytest.mark.parametrize("t,e,top,n,k,apart", sizes.EXPERTS_FAR)
+@pytest.mark.parametrize("t,e,top,n,k,apart", sizes.EXPERTS_FAR + sizes.EXPERTS_NEAR)
 def test_experts_of_far_rows(t, e, top, n, k, apart, shared):
-    """Rows of x past 2^32 bytes, for each token and for each route."""
+    """Rows of x past 2^32 bytes, and past 2^31, for each token and for each route."""
     torch = torch_dev()
     rng = np.random.default_rng(t + n)
     x, xs, w, ws, chosen = layer(torch, rng, t, e, top, n, k, shared)
