@@ -777,7 +777,7 @@ wino_status route_experts(const void* logits, int64_t stride, const float* bias,
  *   workspace w8_experts_matmul_workspace_bytes(routes, n, weights != NULL)
  *             bytes or more, 16-byte aligned, scratch.  With weights, routes * n
  *             floats of it are needed; with less than the rest, or NULL, the
- *             same result comes more slowly.
+ *             same result comes more slowly (k up to 4096 does not use the rest).
  */
 size_t w8_experts_matmul_workspace_bytes(int32_t routes, int32_t n, int32_t combine);
 wino_status w8_experts_matmul(const int8_t* x, int64_t x_stride, const float* x_scales, int32_t x_rows, const int8_t* w,

@@ -42,10 +42,10 @@ template <int TYPE, class S, bool FAR = false> void launch_tiles(Args a, int par
 }
 
 // Which kernel takes a call and in how many parts of k: the shortest estimate.  Parts are joined by a second launch, which
-// pays where few outputs have long sums (8 rows by 764 x 15824: 9.4 us in 6 parts, 11.4 whole; 515 rows by 1024 x 16384 22.4
-// in 3, 31 whole); each is 1024 of k at least, and their sums 16 MiB at most.
-// The kernels for few rows are looked at for up to 256 of them, sixteen a workgroup (of 60 calls each of 33 to 64, 65 to 128 and 129
-// to 256 rows 31, 21 and 9 take them, and on average a call is 15, 8 and 4% shorter than with tiles for all).
+// pays where few outputs have long sums (8 rows by 764 x 15824: 9.3 us in 8 parts, 12.7 whole; 515 rows by 1024 x 16384 24
+// in 2, 32 whole); each is 1024 of k at least, and their sums 16 MiB at most.
+// The kernels for few rows are looked at for up to 256 of them, sixteen a workgroup (of 60 calls each of 33 to 64, 65 to 128 and
+// 129 to 256 rows 31, 21 and 9 take them, and on average a call is 13, 7 and 4% shorter than with tiles for all).
 constexpr int kMostFew = 256;
 struct Cut {
     Kernel kernel;

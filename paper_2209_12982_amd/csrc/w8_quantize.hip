@@ -11,7 +11,9 @@
 //
 // Memory bounds it: 2 bytes read and 1 written a value.  A workgroup takes a
 // row and holds it in registers between the maximum and the codes.  2048 rows
-// of 16384: 24 us, 4.2 TB/s.
+// of 16384: 22.4 us, 4.5 TB/s.  Short rows leave threads without work: 32768
+// rows of 2816 49 us, 5.6 TB/s in part from the last-level cache; of 1408 37,
+// 3.7 TB/s; of 768 25, 2.9 TB/s.
 #include <hip/hip_runtime.h>
 
 #include "mx4.h"

@@ -6,8 +6,8 @@
 // stands where in an operand is free as long as both agree: a lane reads 32 neighbouring bytes of its row, the first 16 for
 // one product and the rest for the next, so that the two loads of a wave take whole lines of 128 bytes.
 //
-// Memory bounds it.  One row by 4096 x 4096: 5.0 us, 3.4 TB/s with the start and end of the launch; 32 tokens to 6 of 64 experts,
-// 2816 x 2048: 63 us, 5.6 TB/s for the experts that some token has.
+// Memory bounds it.  One row by 4096 x 4096: 4.7 to 5.7 us, 3.0 to 3.6 TB/s with the start and end of the launch; 32
+// tokens to 6 of 64 experts, 2816 x 2048: 63 us, 5.6 TB/s for the experts that some token has.
 #pragma once
 #include "w8_device.h"
 
