@@ -7,8 +7,8 @@
 // 16 h + 4 q + e where operand row 8 q + 4 h + e is read: a lane's sixteen sums are then neighbouring outputs of one row.
 //
 // Measured: 8192 rows by 16384 x 4096 480 to 490 us, 2.25 to 2.29 POP/s, at the 1.6 to 1.7 GHz that the load leaves of the
-// clock, the matrix cores 58% of the cycles; 2048 by 4096 x 16384 133 to 137 us, 2.01 to
-// 2.07 POP/s; 48 by 16384 x 4096 13.2 us, bound by the weights' bytes.
+// clock, the matrix cores 58% of the cycles; 2048 by 4096 x 16384 133 to 137 us, 2.01 to 2.07 POP/s; 48 by 16384 x 4096 13.2 us,
+// bound by the weights' bytes.
 #pragma once
 #include <type_traits>
 
@@ -576,13 +576,14 @@ inline bool far(int64_t rows, int64_t stride, int64_t k) { return (rows - 1) * s
 // of the 256 compute units (rows: with 16 rows), and `pair` times that for two workgroups each (0: not for so many).  Chosen
 // for 900 measured calls of 1 to 8192 rows, 64 to 32768 outputs and k of 128 to 16384 such that the kernel of the shortest
 // estimate is as near to the shortest measured one as they go: 1.6% longer on average, 37% at most (1 row by 8192 x 16384: 29.4
-// us, 21.6 in tiles of 32 x 32; over three sets of weights, more than the caches hold, 30 and 29).  Those whose sums are shared out, for 330 more: of 400 others 122 take them then, in 0.94 of
-// the time without them on average, 0.77 to 1.17.  `full` of the rows for 220 more of 1 to 64 rows: of 180 others of 1 to 128
-// rows the choice is 2% longer than the shortest on average, 39% at most.
+// us, 21.6 in tiles of 32 x 32; over three sets of weights, more than the caches hold, 30 and 29).  Those
+// whose sums are shared out, for 330 more: of 400 others 122 take them then, in 0.94 of the time without them on average, 0.77 to
+// 1.17.  `full` of the rows for 220 more of 1 to 64 rows: of 180 others of 1 to 128 rows the choice is 2% longer than the shortest
+// on average, 39% at most.
 struct Form {
     int outs, rows;
     double start, step, pair, full;
-    double uneven;      // rows: in place of `full` for routes; an expert with more than its share has one workgroup for them all
+    double uneven;      // rows: in place of `full` for routes, as an expert with more than its share has one workgroup for all of them
 };
 constexpr Form kForms[kKernels] = {
     {256, 256, 12.7, 5.6, 1.73, 0.69}, {128, 256, 4.2, 4.3, 1.58, 0.98},
