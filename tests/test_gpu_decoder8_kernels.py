@@ -5,6 +5,8 @@ import pytest
 
 import decoder8_sizes as sizes
 import paper_2209_12982_amd as W
+from oracle import decoder8
+
 from decoder_util import dtype, half
 from gpu_util import torch_dev
 from test_gpu_route_experts import check as check_routes
@@ -143,3 +145,82 @@ def test_route(size, name):
     assert (got[3] == np.concatenate([[0], np.cumsum(np.bincount(flat[there], minlength=e))])).all()
     rows = np.sort(rng.permutation(live)[:100])
     check_routes(values[rows], [got[0][rows], got[1][rows], None, None], top)
+
+
+def ends_of(rows, some=300):
+    """The first rows, the last ones, and some between."""
+    step = max(1, rows // some)
+    return sorted(set(range(min(rows, 70))) | set(range(max(0, rows - 70), rows)) | set(range(0, rows, step)))
+
+
+@pytest.mark.parametrize("m,n,k", [(1 << 20, 40, 16), (1 << 20, 2100, 16), (3, 1 << 24, 16), (200, 5000000, 32)])
+def test_matmul_of_the_most_rows_and_outputs(m, n, k):
+    """Up to 2^20 rows, 2^24 outputs and more than 2^31 results."""
+    torch = torch_dev()
+    gen = torch.Generator("cuda").manual_seed(m + n)
+    x, w = (torch.randint(-127, 128, (rows, k), generator=gen, device="cuda", dtype=torch.int8) for rows in (m, n))
+    xs, ws = (0.01 + torch.rand(rows, generator=gen, device="cuda") for rows in (m, n))
+    y = torch.full((m, n), float("nan"), dtype=torch.bfloat16, device="cuda")
+    W.w8_matmul(x, xs, w, ws, y)
+    assert not torch.isnan(y.view(-1)[::977]).any()
+    rows, cols = (torch.tensor(ends_of(size), device="cuda") for size in (m, n))
+    check(y[rows][:, cols], x[rows], xs[rows], w[cols], ws[cols], None, "bf16")
+
+
+@pytest.mark.parametrize("m,k", [((1 << 24) - 1, 16), (3, 1 << 20)])
+def test_quantize_the_most_rows(m, k):
+    torch = torch_dev()
+    gen = torch.Generator("cuda").manual_seed(m)
+    x = torch.randn((m, k), generator=gen, device="cuda", dtype=torch.bfloat16)
+    codes = torch.full((m, k), 99, dtype=torch.int8, device="cuda")
+    scales = torch.full((m,), -1.0, device="cuda")
+    W.w8_quantize(x, codes, scales)
+    assert (scales > 0).all()
+    for i in ends_of(m, 20):
+        some = ends_of(k, 2000)
+        row = x[i].double().cpu().numpy()
+        top = np.argmax(np.abs(row))
+        want, scale = decoder8.quantize_row(np.append(row[some], row[top]))
+        assert (codes[i].cpu().numpy()[some] == want[:-1]).all() and scales[i] == np.float32(float(scale)), i
+
+
+@pytest.mark.parametrize("t,e,top", [(1 << 22, 5, 1), (1 << 17, 64, 32), (1 << 19, 1024, 8)])
+def test_route_the_most_tokens(t, e, top):
+    torch = torch_dev()
+    gen = torch.Generator("cuda").manual_seed(t + e)
+    logits = torch.randn((t, e), generator=gen, device="cuda", dtype=torch.float32)
+    got = run(torch, logits, top)
+    flat = got[0].reshape(-1)
+    assert flat.min() >= 0 and flat.max() < e
+    assert (got[2] == np.argsort(flat, kind="stable")).all()
+    assert (got[3] == np.concatenate([[0], np.cumsum(np.bincount(flat, minlength=e))])).all()
+    rows = ends_of(t, 50)
+    check_routes(logits[rows].double().cpu().numpy(), [got[0][rows], got[1][rows], None, None], top)
+
+
+@pytest.mark.parametrize("t,e,top,n,k", [(1 << 20, 3, 4, 33, 16), (1 << 21, 2, 2, 520, 16)])
+def test_experts_of_the_most_routes(t, e, top, n, k):
+    """2^22 routes, and more than 2^31 products."""
+    torch = torch_dev()
+    gen = torch.Generator("cuda").manual_seed(t + n)
+    x = torch.randint(-127, 128, (t, k), generator=gen, device="cuda", dtype=torch.int8)
+    w = torch.randint(-127, 128, (e, n, k), generator=gen, device="cuda", dtype=torch.int8)
+    xs, ws = 0.01 + torch.rand(t, generator=gen, device="cuda"), 0.01 + torch.rand((e, n), generator=gen, device="cuda")
+    chosen = torch.randint(0, e, (t, top), generator=gen, device="cuda", dtype=torch.int32)
+    flat = chosen.flatten()
+    order = torch.sort(flat, stable=True).indices.int()
+    ends = torch.cat((torch.zeros(1, device="cuda", dtype=torch.long), torch.bincount(flat, minlength=e).cumsum(0))).int()
+    weights = torch.rand((t, top), generator=gen, device="cuda")
+    rows = torch.tensor(ends_of(t), device="cuda")
+    ref = torch.stack([(x[rows].double()[:, None] * w[chosen[rows, j].long()].double()).sum(-1)
+                       * xs[rows].double()[:, None] * ws[chosen[rows, j].long()].double() for j in range(top)], 1)
+    y = torch.full((t * top, n), float("nan"), dtype=torch.bfloat16, device="cuda")
+    W.w8_experts_matmul(x, xs, w, ws, order, ends, y)
+    assert not torch.isnan(y.view(-1)[::977]).any()
+    close(y.view(t, top, n)[rows], ref, ref.abs(), 3, "bf16")
+    del y
+    room = torch.empty(W.w8_experts_matmul_workspace_bytes(t * top, n, True), dtype=torch.uint8, device="cuda")
+    out = torch.full((t, n), float("nan"), dtype=torch.bfloat16, device="cuda")
+    W.w8_experts_matmul(x, xs, w, ws, order, ends, out, chosen=chosen, weights=weights, workspace=room)
+    parts = ref * weights[rows].double()[..., None]
+    close(out[rows], parts.sum(1), parts.abs().sum(1), 4 + top, "bf16")
