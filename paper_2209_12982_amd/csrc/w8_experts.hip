@@ -89,7 +89,7 @@ Kernel choose(int64_t routes, int64_t experts, int64_t n, int64_t k, bool tail) 
         const int64_t all = (int64_t)(tiles * (double)(used * ((n + f.outs - 1) / f.outs)));
         // uneven routes have more tiles than that, and one more than 256 would cost these a second round
         if (f.pair == 0 && all > 200) continue;
-        double t = estimate((Kernel)i, all, k, used * n * k, (int64_t)std::min(each, 16.0), true);
+        double t = estimate((Kernel)i, all, k, used * n * k, (int64_t)std::min(each, 16.0));
         // tiles whose last ones are cut in parts of k take a part of the last round, and their join 20 us
         if (i == kTile256x256 && tail)
             t = std::min(t, std::max((f.start + f.step * (1 + f.full) * (double)k / 1024) * ((double)all / 256 + 0.1) + 20,

@@ -44,8 +44,8 @@ template <int TYPE, class S, bool FAR = false> void launch_tiles(Args a, int par
 // Which kernel takes a call and in how many parts of k: the shortest estimate.  Parts are joined by a second launch, which
 // pays where few outputs have long sums (8 rows by 764 x 15824: 9.3 us in 8 parts, 12.7 whole; 515 rows by 1024 x 16384 24
 // in 2, 32 whole); each is 1024 of k at least, and their sums 16 MiB at most.
-// The kernels for few rows are looked at for up to 256 of them, sixteen a workgroup (of 60 calls each of 33 to 64, 65 to 128 and
-// 129 to 256 rows 31, 21 and 9 take them, and on average a call is 13, 7 and 4% shorter than with tiles for all).
+// The kernels for few rows are looked at for up to 256 of them, sixteen a workgroup (of 36 calls of 33 to 64 rows, 84 of 65 to
+// 128 and 40 of 129 to 256 17, 38 and 15 take them, and on average a call is 12, 10 and 11% shorter than with tiles for all).
 constexpr int kMostFew = 256;
 struct Cut {
     Kernel kernel;
@@ -63,7 +63,7 @@ Cut cut(int64_t m, int64_t n, int64_t k) {
             if (parts > 1 && (i >= kRows16 || k < 1024 * parts || parts * m * n > 1 << 22)) break;
             if (f.pair == 0 && tiles * parts > 256) break;
             const double join = parts > 1 ? 1.95 + 0.17 * parts + 1.3e-6 * (double)(parts * m * n) : 0;
-            double t = estimate((Kernel)i, tiles * parts, k / parts, n * k, m, false) + join;
+            double t = estimate((Kernel)i, tiles * parts, k / parts, n * k, m) + join;
             if (i == kTile256x256 && parts == 1) t -= std::max(tail_gain(tiles, k), 0.0);
             if (least == 0 || t < least) least = t, best = Cut{(Kernel)i, parts};
         }

@@ -578,31 +578,28 @@ inline bool far(int64_t rows, int64_t stride, int64_t k) { return (rows - 1) * s
 // estimate is as near to the shortest measured one as they go: 1.6% longer on average, 37% at most (1 row by 8192 x 16384: 29.4
 // us, 21.6 in tiles of 32 x 32; over three sets of weights, more than the caches hold, 30 and 29).  Those
 // whose sums are shared out, for 330 more: of 400 others 122 take them then, in 0.94 of the time without them on average, 0.77 to
-// 1.17.  `full` of the rows for 220 more of 1 to 64 rows: of 180 others of 1 to 128 rows the choice is 2% longer than the shortest
-// on average, 39% at most.
+// 1.17.  Of 440 others of 1 to 256 rows the choice is 1.3% longer than the shortest on average, 28% at most.
 struct Form {
     int outs, rows;
     double start, step, pair, full;
-    double uneven;      // rows: in place of `full` for routes, as an expert with more than its share has one workgroup for all of them
 };
 constexpr Form kForms[kKernels] = {
     {256, 256, 12.7, 5.6, 1.73, 0.69}, {128, 256, 4.2, 4.3, 1.58, 0.98},
     {128, 128, 3.91, 2.27, 2.17, 0.78}, {128, 128, 3.14, 2.42, 1.3, 1.01}, {64, 128, 2.26, 1.67, 1.56, 0.7},
     {64, 64, 2.26, 1.58, 1.3, 0.38},    {32, 32, 2.32, 0.48, 1.24, 0.71},  {64, 128, 3.7, 1.13, 0, 0.62},
-    {64, 64, 2.8, 1.2, 0, 0.19},        {64, 32, 2.94, 0.716, 0, 0.2},     {16, 16, 1.1, 0.32, 1.84, 0.72, 1.37},
-    {16, 16, 0.26, 0.424, 1.76, 0.78, 1.16}, {32, 16, 0.46, 0.98, 1.5, 0.52, 1.24},
+    {64, 64, 2.8, 1.2, 0, 0.19},        {64, 32, 2.94, 0.716, 0, 0.2},     {16, 16, 1.1, 0.32, 1.84, 1.37},
+    {16, 16, 0.26, 0.424, 1.76, 1.16},  {32, 16, 0.46, 0.98, 1.5, 1.24},
 };
-// The time of a kernel that has so many tiles, for k of a part and so many bytes of weights; m: rows, of an expert with `routes`.
-inline double estimate(Kernel kernel, int64_t tiles, int64_t k, int64_t bytes, int64_t m, bool routes) {
+// The time of a kernel that has so many tiles, for k of a part and so many bytes of weights; m: rows, of an expert or of all.
+inline double estimate(Kernel kernel, int64_t tiles, int64_t k, int64_t bytes, int64_t m) {
     const Form& f = kForms[kernel];
     const int64_t rest = tiles % 512;
     const double rounds = f.pair * (double)(tiles / 512) + (rest == 0 ? 0 : (rest <= 256 ? 1 : f.pair));
-    const double full = kernel >= kRows16 && routes ? f.uneven : f.full;
-    const double fill = kernel >= kRows16 ? (double)m / 16 : (tiles < 256 ? (double)tiles / 256 : 1);
+    const double fill = kernel >= kRows16 ? (m < 16 ? (double)m / 16 : 1) : (tiles < 256 ? (double)tiles / 256 : 1);
     // Sixteen rows of 4096 bytes or a multiple lie in the same memory channels, and eight waves ask for half of them at a
     // time: one row by 4096 x 4096 7.2 us, by 16 waves 5.5; by 4096 x 4080 4.2 both.
     const double same = kernel == kRows16Few && k % 4096 == 0 ? 1.4 : 1;
-    const double t = (f.start + same * f.step * (1 + full * fill) * (double)k / 1024) * rounds, memory = (double)bytes / 5.2e6;
+    const double t = (f.start + same * f.step * (1 + f.full * fill) * (double)k / 1024) * rounds, memory = (double)bytes / 5.2e6;
     return t > memory ? t + 0.05 * memory : memory + 0.05 * t;      // what is less decides between equal ones
 }
 // What it gains (us) to cut the last of so many tiles of 256 x 256 in parts of k: a part of a round instead of a whole one, for

@@ -19,10 +19,10 @@ TILES = {
 
 # kernel, second launch -> (m, n, k)
 MATMUL = {
-    ("rows 16", None): [(1, 34, 12112), (3, 1, 7296), (19, 1201, 6208)],
+    ("rows 16", None): [(1, 34, 12112), (4, 1, 9984), (41, 27, 4096), (110, 478, 5696)],
     ("rows 16 few", None): [(1, 35, 944), (11, 1, 640), (23, 341, 80), (47, 571, 1648), (113, 399, 192), (191, 69, 208)],
     ("rows 32", None): [(1, 16147, 1088), (2, 28536, 640), (8, 15070, 112), (31, 16340, 16)],
-    ("32x32", None): [(41, 61, 4784), (58, 3, 3328), (331, 1, 64)],
+    ("32x32", None): [(19, 58, 5648), (15, 114, 6656), (74, 1325, 2352), (331, 1, 64)],
     ("32x32", "join"): [(9, 40, 13200), (32, 4, 8192)],
     ("64x64", None): [(319, 919, 528), (55, 6089, 512), (395, 1, 16)],
     ("64x128", None): [(1214, 1011, 544), (325, 3020, 512), (86, 8598, 16), (2048, 1024, 1024)],
