@@ -70,11 +70,11 @@ template <int TYPE, class S, bool FAR = false> void launch_tiles(const Args& a, 
 }
 
 // The shortest estimate for routes that are spread evenly: the host does not know how they are.  Uneven ones mostly take less, as
-// fewer experts are read (us; even, and as uneven as can be): 1000 tokens to one of 64 74, 15; 128 to 8 of 64 74, 16.  They take more
+// fewer experts are read (us; even, and as uneven as can be): 1000 tokens to one of 64 74, 16; 128 to 8 of 64 74, 16.  They take more
 // where tiles need another round: 512 to 2 of 8 16, 25; 4096 to 8 of 64 with a tenth of the routes on one 259 for 243.  An expert
 // with r rows on average has r / rows tiles and half a one more, or one.  Measured (us): 4096 tokens to 8 of 64 experts, n 2816, k 2048:
 // 256 x 256 249, two 128 x 128 297, 128 x 256 337; 2000 to 2 of 8, 4096 x 8192: 187 with the last tiles in parts and 220
-// without, 210, 218; 256 to 6 of 64: 102, 87, 91, 64 x 64 79; 32 to 6 of 64: rows of 32 outputs 62, 64 x 64 67; one to 2 of 8,
+// without, 210, 218; 256 to 6 of 64: 102, 87, 91, 64 x 64 79; 32 to 6 of 64: rows of 32 outputs 60, 64 x 64 67; one to 2 of 8,
 // 1024 x 2048: rows of 16 outputs 4.5.
 Kernel choose(int64_t routes, int64_t experts, int64_t n, int64_t k, bool tail) {
     const int64_t used = std::min(routes, experts);

@@ -575,8 +575,7 @@ inline bool far(int64_t rows, int64_t stride, int64_t k) { return (rows - 1) * s
 // What a kernel takes (us): `start` beside the loop, `step` for 1024 of k, `step` times 1 + `full` with a workgroup on each
 // of the 256 compute units (rows: with 16 rows), and `pair` times that for two workgroups each (0: not for so many).  Chosen
 // for 900 measured calls of 1 to 8192 rows, 64 to 32768 outputs and k of 128 to 16384 such that the kernel of the shortest
-// estimate is as near to the shortest measured one as they go: 1.6% longer on average, 37% at most (1 row by 8192 x 16384: 29.4
-// us, 21.6 in tiles of 32 x 32; over three sets of weights, more than the caches hold, 30 and 29).  Those
+// estimate is as near to the shortest measured one as they go: 1.6% longer on average, 37% at most.  Those
 // whose sums are shared out, for 330 more: of 400 others 122 take them then, in 0.94 of the time without them on average, 0.77 to
 // 1.17.  Of 440 others of 1 to 256 rows the choice is 1.3% longer than the shortest on average, 28% at most.
 struct Form {
@@ -597,7 +596,7 @@ inline double estimate(Kernel kernel, int64_t tiles, int64_t k, int64_t bytes, i
     const double rounds = f.pair * (double)(tiles / 512) + (rest == 0 ? 0 : (rest <= 256 ? 1 : f.pair));
     const double fill = kernel >= kRows16 ? (m < 16 ? (double)m / 16 : 1) : (tiles < 256 ? (double)tiles / 256 : 1);
     // Sixteen rows of 4096 bytes or a multiple lie in the same memory channels, and eight waves ask for half of them at a
-    // time: one row by 4096 x 4096 7.2 us, by 16 waves 5.5; by 4096 x 4080 4.2 both.
+    // time: one row by 4096 x 4096 5.5 us, by 16 waves 5.2; by 4096 x 4112 4.8 and 4.9.
     const double same = kernel == kRows16Few && k % 4096 == 0 ? 1.4 : 1;
     const double t = (f.start + same * f.step * (1 + f.full * fill) * (double)k / 1024) * rounds, memory = (double)bytes / 5.2e6;
     return t > memory ? t + 0.05 * memory : memory + 0.05 * t;      // what is less decides between equal ones
